@@ -61,7 +61,8 @@ enum {
   DOMINO_DEV_BAD_TOKEN = 1,       /* an anchor / forced / tree token id outside [0, vocab) (clamped) */
   DOMINO_DEV_BAD_CTX_LEN = 2,     /* ctx_lens[b] outside [n_new, max_ctx] (clamped) */
   DOMINO_DEV_BAD_TREE = 4,        /* a node_parent entry that is not an earlier node (ignored) */
-  DOMINO_DEV_BARRIER_TIMEOUT = 8  /* a bounded cross-workgroup wait of the rollout exceeded its spin bound */
+  DOMINO_DEV_BARRIER_TIMEOUT = 8, /* a bounded cross-workgroup wait of the rollout exceeded its spin bound */
+  DOMINO_DEV_BAD_PARAM = 16       /* a row's temperature, top_p, min_p, uniform or weight out of its range */
 };
 
 /*
@@ -388,6 +389,104 @@ domino_status domino_verify_sample(int32_t batch, int32_t block, int32_t vocab, 
                                    int32_t *accept_len, int32_t *accepted_nodes, int32_t *out_tokens,
                                    void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Rows of logits: their top entries, the loss that trains on such entries, and
+ * drawing a token from them.  For the three calls below
+ *  logits          device [rows] rows of vocab values, fp32 or bf16, ld elements
+ *                  apart (ld >= vocab; a row may start at any value's address).
+ *                  NaN counts as -inf.  Entries are ordered by (value desc, id asc);
+ *                  the zeros of both signs are equal.
+ *  rows            >= 1; rows and vocab as far as the message of DOMINO_ERR_UNSUPPORTED
+ *  workspace       device, >= the call's *_workspace_bytes query (0 for arguments that
+ *                  the call refuses), aligned to 8 bytes; its first word is the
+ *                  call's error word
+ */
+
+/* Bytes of workspace domino_top_logits needs. */
+size_t domino_top_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
+
+/*
+ * The first k entries of every row, and what the others weigh: of a teacher's
+ * row (domino_target_verify's logits), what distillation keeps.
+ *  k               in [1, min(vocab, 1024)]; vocab at most 327680
+ *  temperature     T > 0 (finite); it only acts on rest
+ *  top_ids         device int32 [rows][k], in order
+ *  top_vals        device fp32 [rows][k]: their logits (not divided by T)
+ *  rest            optional device fp32 [rows]: log of the sum over every other id
+ *                  of exp(logit / T); -inf where there is none above -inf
+ */
+domino_status domino_top_logits(int32_t rows, int32_t vocab, int32_t k, const void *logits, domino_dtype logits_dtype,
+                                int64_t ld, float temperature, int32_t *top_ids, float *top_vals, float *rest,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace domino_distill_loss needs. */
+size_t domino_distill_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
+
+/*
+ * Distillation from a teacher's top entries: the loss of a row of student logits l
+ * (the final_logits or base_logits of domino_train_forward) and its gradient.
+ * With p the softmax of (t_1 / T, .., t_k / T, rest_t) over the row's k entries and one
+ * bucket of all other ids, and q the student's distribution softmax(l / T) over the
+ * same buckets,
+ *   row_loss = T^2 (sum_i p_i log(p_i / q_i) + p_rest log(p_rest / q_rest)),
+ *   loss     = sum_r w_r row_loss_r / sum_r w_r
+ * (a bucket with p = 0 adds nothing; one with p > 0 = q makes the row's loss inf).
+ *  k               in [1, min(vocab, 1024)]
+ *  teacher_ids     device int32 [rows][k], distinct; -1: no entry.  An id outside
+ *                  [-1, vocab) or given twice sets DOMINO_DEV_BAD_TOKEN, and the
+ *                  row's loss and gradient are NaN
+ *  teacher_vals    device fp32 [rows][k]: t (NaN counts as -inf)
+ *  teacher_rest    optional device fp32 [rows]: rest_t, as domino_top_logits gives it
+ *                  at the same T; NULL: -inf, the teacher is its entries alone
+ *                  A row whose teacher has no weight at all has loss and gradient 0.
+ *  temperature     T > 0 (finite)
+ *  row_weights     optional device fp32 [rows]: w >= 0 and finite, NULL: 1.  A row of
+ *                  weight 0 adds nothing to the loss and its gradient is 0, whatever it
+ *                  holds; another value sets DOMINO_DEV_BAD_PARAM and counts as 0.
+ *                  The loss is 0 where all are 0.
+ *  grad_scale      finite factor of the gradient
+ *  loss            device fp32 [1]
+ *  row_loss        optional device fp32 [rows] (without the weights)
+ *  grad            optional device [rows] rows of vocab values of the logits' type, ld_grad
+ *                  apart (>= vocab): grad_scale * dloss/dl.  It may be logits itself
+ *                  (with ld_grad = ld), and overlap them in no other way.
+ * Deterministic: no floating-point atomics.
+ */
+domino_status domino_distill_loss(int32_t rows, int32_t vocab, int32_t k, const void *logits, domino_dtype logits_dtype,
+                                  int64_t ld, const int32_t *teacher_ids, const float *teacher_vals,
+                                  const float *teacher_rest, float temperature, const float *row_weights,
+                                  float grad_scale, float *loss, float *row_loss, void *grad, int64_t ld_grad,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace domino_sample_logits needs. */
+size_t domino_sample_logits_workspace_bytes(int32_t rows, int32_t vocab);
+
+/*
+ * One token of every row, drawn with the caller's uniforms (e.g. the first token after
+ * a prompt, or plain decoding beside speculative cycles).  Per row, with e_v =
+ * exp((l_v - max l) / T) and sums over the first entries of the order:
+ *   n_k = top_k (0 or less: every entry);
+ *   n_p = the least n >= 1 whose sum of e is at least top_p times that of the first n_k (1: every entry);
+ *   n_m = the number of entries with e >= min_p (0: every entry);
+ * the first n = min(n_k, n_p, n_m) are kept, S the sum of their e; the token is the
+ * first whose running sum exceeds u S, its log-probability log(e / S).  Logits of +inf
+ * share all the weight.  e is held to 2^-45 (a lighter entry is never drawn) and summed as whole
+ * numbers, so the token does not depend on the order of the sums.
+ *  vocab           at most 327680
+ *  temperature     optional device fp32 [rows]: T >= 0, finite; NULL: 1.  0: the first
+ *                  entry of the order, whatever the filters
+ *  top_k           optional device int32 [rows]
+ *  top_p, min_p    optional device fp32 [rows], in [0, 1]
+ *  uniforms        device fp32 [rows]: u in [0, 1)
+ *  tokens          device int32 [rows]; -1 for a row without a logit above -inf, and for
+ *                  one with a parameter out of its range (DOMINO_DEV_BAD_PARAM)
+ *  logprobs        optional device fp32 [rows]; -inf and NaN for those two
+ */
+domino_status domino_sample_logits(int32_t rows, int32_t vocab, const void *logits, domino_dtype logits_dtype, int64_t ld,
+                                   const float *temperature, const int32_t *top_k, const float *top_p,
+                                   const float *min_p, const float *uniforms, int32_t *tokens, float *logprobs,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
 /* Philox-4x32-10 (Salmon et al., SC 2011) of n explicit counters: counters
  * device uint32 [n][4], key = (key lo, key hi) 32-bit words, out device uint32
  * [n][4].  The generator behind the sampled calls, for callers and tests that
@@ -395,7 +494,7 @@ domino_status domino_verify_sample(int32_t batch, int32_t block, int32_t vocab, 
 domino_status domino_philox4x32_10(const uint32_t *counters, uint64_t key, uint32_t *out, int32_t n,
                                    void *stream);
 
-/* Copy the device error word at the start of a draft or verify workspace to
+/* Copy the device error word at the start of a workspace to
  * *out (synchronises `stream`).  Returns DOMINO_ERR_DEVICE when it is set. */
 domino_status domino_workspace_error(const void *workspace, void *stream, int32_t *out);
 

@@ -22,7 +22,7 @@ DOMINO_ERR_HIP = -4
 DOMINO_ERR_DEVICE = -5
 DOMINO_F32, DOMINO_BF16 = 0, 1
 
-DEV_BAD_TOKEN, DEV_BAD_CTX_LEN, DEV_BAD_TREE, DEV_BARRIER_TIMEOUT = 1, 2, 4, 8
+DEV_BAD_TOKEN, DEV_BAD_CTX_LEN, DEV_BAD_TREE, DEV_BARRIER_TIMEOUT, DEV_BAD_PARAM = 1, 2, 4, 8, 16
 
 KERNEL_CLASSES = ["embed", "norm", "qkv", "rope", "attn", "wo", "gateup", "down", "lmhead", "w1h",
                   "headloop", "ctxproj", "trainloss"]
@@ -94,6 +94,13 @@ def load() -> C.CDLL:
         "domino_verify_sample": (i32, [i32, i32, i32, P, P, C.c_int, P, C.c_float, C.c_uint64, P, P, P, P, sz,
                                        P]),
         "domino_philox4x32_10": (i32, [P, C.c_uint64, P, i32, P]),
+        "domino_top_logits_workspace_bytes": (sz, [i32, i32, i32]),
+        "domino_top_logits": (i32, [i32, i32, i32, P, C.c_int, C.c_int64, C.c_float, P, P, P, P, sz, P]),
+        "domino_distill_workspace_bytes": (sz, [i32, i32, i32]),
+        "domino_distill_loss": (i32, [i32, i32, i32, P, C.c_int, C.c_int64, P, P, P, C.c_float, P, C.c_float, P, P, P,
+                                      C.c_int64, P, sz, P]),
+        "domino_sample_logits_workspace_bytes": (sz, [i32, i32]),
+        "domino_sample_logits": (i32, [i32, i32, P, C.c_int, C.c_int64, P, P, P, P, P, P, P, P, sz, P]),
         "domino_train_workspace_bytes": (sz, [P, i32, i32, i32]),
         "domino_target_create": (i32, [C.POINTER(domino_config), C.POINTER(domino_weights), C.POINTER(P)]),
         "domino_target_workspace_bytes": (sz, [P, i32, i32, i32]),
@@ -116,7 +123,9 @@ def exported_symbols():
             "domino_verify_accept", "domino_workspace_error", "domino_workspace_clear_error",
             "domino_profile_enable", "domino_profile_read", "domino_profile_reset",
             "domino_draft_step_sampled", "domino_verify_sample_workspace_bytes", "domino_verify_sample",
-            "domino_philox4x32_10", "domino_train_workspace_bytes", "domino_train_forward",
+            "domino_philox4x32_10", "domino_top_logits_workspace_bytes", "domino_top_logits",
+            "domino_distill_workspace_bytes", "domino_distill_loss", "domino_sample_logits_workspace_bytes",
+            "domino_sample_logits", "domino_train_workspace_bytes", "domino_train_forward",
             "domino_target_create", "domino_target_workspace_bytes", "domino_target_verify", "domino_target_commit",
             "domino_debug_set_poll_limit", "domino_debug_last_paths", "domino_verify_accept_noalloc"]
 
@@ -317,6 +326,97 @@ def domino_verify_sample(node_token, target_logits, draft_logits, temperature, s
 def domino_philox4x32_10(counters, key, out, stream=None):
     _check(load().domino_philox4x32_10(_ptr(counters), int(key) & (2**64 - 1), _ptr(out),
                                        int(counters.shape[0]), _stream(stream)))
+
+
+def _rows(logits):
+    """(rows, vocab, row stride, domino_dtype) of a 2-D tensor of logits whose rows are dense."""
+    import torch
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or \
+            (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "logits must be a 2-D fp32 or bf16 tensor with dense rows")
+    ld = logits.stride(0) if logits.shape[0] > 1 else max(logits.stride(0), logits.shape[1])
+    return logits.shape[0], logits.shape[1], ld, DOMINO_BF16 if logits.dtype == torch.bfloat16 else DOMINO_F32
+
+
+def _check_array(name, t, like, dtype, n):
+    """An optional per-row array: dense, of `dtype`, n elements, on the logits' device."""
+    if t is None:
+        return
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != like.device:
+        raise DominoError(DOMINO_ERR_INVALID_ARG,
+                          f"{name} must be a contiguous {dtype} tensor of {n} elements on {like.device}")
+
+
+def _check_device(logits):
+    """Work is launched on the current device: tensors of another one are refused."""
+    import torch
+    if not logits.is_cuda or logits.device.index != torch.cuda.current_device():
+        raise DominoError(DOMINO_ERR_INVALID_ARG, f"logits must be on the current device, not on {logits.device}")
+
+
+def domino_top_logits_workspace_bytes(rows, vocab, k) -> int:
+    return int(load().domino_top_logits_workspace_bytes(rows, vocab, k))
+
+
+def domino_top_logits(logits, top_ids, top_vals, workspace, rest=None, temperature=1.0, stream=None):
+    """logits [rows, vocab] with dense rows; top_ids int32 and top_vals fp32 [rows, k]; rest fp32 [rows]."""
+    import torch
+    n, V, ld, dt = _rows(logits)
+    k = top_ids.shape[-1]
+    _check_array("top_ids", top_ids, logits, torch.int32, n * k)
+    _check_array("top_vals", top_vals, logits, torch.float32, n * k)
+    _check_array("rest", rest, logits, torch.float32, n)
+    _check_device(logits)
+    _check(load().domino_top_logits(n, V, k, _ptr(logits), dt, ld, float(temperature), _ptr(top_ids), _ptr(top_vals),
+                                    _ptr(rest), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                    _stream(stream)))
+
+
+def domino_distill_workspace_bytes(rows, vocab, k) -> int:
+    return int(load().domino_distill_workspace_bytes(rows, vocab, k))
+
+
+def domino_distill_loss(logits, teacher_ids, teacher_vals, loss, workspace, teacher_rest=None, temperature=1.0,
+                        row_weights=None, grad_scale=1.0, row_loss=None, grad=None, stream=None):
+    """logits [rows, vocab] with dense rows; teacher_ids int32 and teacher_vals fp32 [rows, k]; grad as logits."""
+    import torch
+    n, V, ld, dt = _rows(logits)
+    k = teacher_ids.shape[-1]
+    _check_array("teacher_ids", teacher_ids, logits, torch.int32, n * k)
+    _check_array("teacher_vals", teacher_vals, logits, torch.float32, n * k)
+    for name, t, size in (("teacher_rest", teacher_rest, n), ("row_weights", row_weights, n), ("row_loss", row_loss, n),
+                          ("loss", loss, 1)):
+        _check_array(name, t, logits, torch.float32, size)
+    ld_grad = 0
+    if grad is not None:
+        gn, gv, ld_grad, gdt = _rows(grad)
+        if (gn, gv, gdt, grad.device) != (n, V, dt, logits.device):
+            raise DominoError(DOMINO_ERR_INVALID_ARG, "grad must have the logits' shape, type and device")
+    _check_device(logits)
+    _check(load().domino_distill_loss(n, V, k, _ptr(logits), dt, ld, _ptr(teacher_ids), _ptr(teacher_vals),
+                                      _ptr(teacher_rest), float(temperature), _ptr(row_weights), float(grad_scale),
+                                      _ptr(loss), _ptr(row_loss), _ptr(grad), ld_grad, _ptr(workspace),
+                                      workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def domino_sample_logits_workspace_bytes(rows, vocab) -> int:
+    return int(load().domino_sample_logits_workspace_bytes(rows, vocab))
+
+
+def domino_sample_logits(logits, uniforms, tokens, workspace, temperature=None, top_k=None, top_p=None, min_p=None,
+                         logprobs=None, stream=None):
+    """logits [rows, vocab] with dense rows; every other array [rows] (top_k and tokens int32, the rest fp32)."""
+    import torch
+    n, V, ld, dt = _rows(logits)
+    for name, t in (("uniforms", uniforms), ("temperature", temperature), ("top_p", top_p), ("min_p", min_p),
+                    ("logprobs", logprobs)):
+        _check_array(name, t, logits, torch.float32, n)
+    for name, t in (("tokens", tokens), ("top_k", top_k)):
+        _check_array(name, t, logits, torch.int32, n)
+    _check_device(logits)
+    _check(load().domino_sample_logits(n, V, _ptr(logits), dt, ld, _ptr(temperature), _ptr(top_k), _ptr(top_p),
+                                       _ptr(min_p), _ptr(uniforms), _ptr(tokens), _ptr(logprobs), _ptr(workspace),
+                                       workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def domino_build_tree(topk_ids, anchor, ctx_lens, node_token, node_parent, node_depth, node_pos,

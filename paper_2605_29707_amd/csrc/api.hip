@@ -1285,6 +1285,141 @@ domino_status domino_verify_sample(int32_t batch, int32_t block, int32_t vocab, 
   return DOMINO_OK;
 }
 
+// ---- rows of logits
+namespace {
+constexpr long kMaxBlocks = (1L << 24) - 2;  // workgroups of 256 threads a grid holds
+
+domino_status check_rows(int32_t rows, int32_t vocab, const void *logits, domino_dtype dtype, int64_t ld) {
+  if (rows < 1) return fail(DOMINO_ERR_INVALID_ARG, "rows must be >= 1");
+  if (vocab < 1) return fail(DOMINO_ERR_INVALID_ARG, "vocab must be >= 1");
+  if (dtype != DOMINO_F32 && dtype != DOMINO_BF16) return fail(DOMINO_ERR_INVALID_ARG, "bad logits dtype");
+  if (!logits) return fail(DOMINO_ERR_INVALID_ARG, "logits is NULL");
+  if ((uintptr_t)logits % (dtype == DOMINO_BF16 ? 2 : 4)) return fail(DOMINO_ERR_INVALID_ARG, "logits is not aligned to its type");
+  if (ld < vocab) return fail(DOMINO_ERR_INVALID_ARG, "ld must be at least vocab");
+  return DOMINO_OK;
+}
+bool rows_supported(int32_t rows, int32_t vocab) {
+  return rows >= 1 && vocab >= 1 && vocab <= kRowsMaxVocab && rows <= kMaxBlocks / 64;
+}
+bool distill_supported(int32_t rows, int32_t vocab, int32_t k) {
+  return rows >= 1 && vocab >= 1 && k >= 1 && k <= 1024 && k <= vocab &&
+         (long)rows * (((long)vocab + 4095) / 4096) <= kMaxBlocks;
+}
+domino_status check_workspace(const void *ws, size_t have, size_t need) {
+  if (!ws) return fail(DOMINO_ERR_WORKSPACE, "workspace is NULL");
+  if ((uintptr_t)ws % 8) return fail(DOMINO_ERR_WORKSPACE, "workspace is not aligned to 8 bytes");
+  if (have < need) return fail(DOMINO_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", have, need);
+  return DOMINO_OK;
+}
+bool temperature_ok(float t) { return t > 0.f && std::isfinite(t) && 1.0f / t <= 1e30f; }
+}  // namespace
+
+size_t domino_top_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t k) {
+  if (!rows_supported(rows, vocab) || k < 1 || k > 1024 || k > vocab) return 0;
+  return rows_ws_bytes(rows, vocab);
+}
+
+domino_status domino_top_logits(int32_t rows, int32_t vocab, int32_t k, const void *logits, domino_dtype logits_dtype,
+                                int64_t ld, float temperature, int32_t *top_ids, float *top_vals, float *rest,
+                                void *workspace, size_t workspace_bytes, void *stream) {
+  if (domino_status s = check_rows(rows, vocab, logits, logits_dtype, ld); s != DOMINO_OK) return s;
+  if (k < 1 || k > 1024 || k > vocab) return fail(DOMINO_ERR_INVALID_ARG, "k must be in [1, 1024] and at most vocab");
+  if (!temperature_ok(temperature)) return fail(DOMINO_ERR_INVALID_ARG, "temperature must be positive and finite");
+  if (!top_ids || !top_vals) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (!rows_supported(rows, vocab))
+    return fail(DOMINO_ERR_UNSUPPORTED, "vocab must be at most %d and rows at most %ld", kRowsMaxVocab, kMaxBlocks / 64);
+  if (domino_status s = check_workspace(workspace, workspace_bytes, rows_ws_bytes(rows, vocab)); s != DOMINO_OK) return s;
+  RowsArgs a = {};
+  a.rows = rows;
+  a.V = vocab;
+  a.logits = logits;
+  a.ld = (size_t)ld;
+  a.T = temperature;
+  launch_top_logits(a, logits_dtype == DOMINO_BF16, k, top_ids, top_vals, rest, workspace, (hipStream_t)stream);
+  hipError_t he = hipGetLastError();
+  if (he != hipSuccess) return fail(DOMINO_ERR_HIP, "top_logits launch: %s", hipGetErrorString(he));
+  return DOMINO_OK;
+}
+
+size_t domino_sample_logits_workspace_bytes(int32_t rows, int32_t vocab) {
+  return rows_supported(rows, vocab) ? rows_ws_bytes(rows, vocab) : 0;
+}
+
+domino_status domino_sample_logits(int32_t rows, int32_t vocab, const void *logits, domino_dtype logits_dtype, int64_t ld,
+                                   const float *temperature, const int32_t *top_k, const float *top_p,
+                                   const float *min_p, const float *uniforms, int32_t *tokens, float *logprobs,
+                                   void *workspace, size_t workspace_bytes, void *stream) {
+  if (domino_status s = check_rows(rows, vocab, logits, logits_dtype, ld); s != DOMINO_OK) return s;
+  if (!uniforms || !tokens) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (!rows_supported(rows, vocab))
+    return fail(DOMINO_ERR_UNSUPPORTED, "vocab must be at most %d and rows at most %ld", kRowsMaxVocab, kMaxBlocks / 64);
+  if (domino_status s = check_workspace(workspace, workspace_bytes, rows_ws_bytes(rows, vocab)); s != DOMINO_OK) return s;
+  RowsArgs a = {};
+  a.rows = rows;
+  a.V = vocab;
+  a.logits = logits;
+  a.ld = (size_t)ld;
+  a.temps = temperature;
+  a.T = 1.f;
+  const SampleArgs p = {top_k, top_p, min_p, uniforms, tokens, logprobs};
+  launch_sample_logits(a, logits_dtype == DOMINO_BF16, p, workspace, (hipStream_t)stream);
+  hipError_t he = hipGetLastError();
+  if (he != hipSuccess) return fail(DOMINO_ERR_HIP, "sample_logits launch: %s", hipGetErrorString(he));
+  return DOMINO_OK;
+}
+
+size_t domino_distill_workspace_bytes(int32_t rows, int32_t vocab, int32_t k) {
+  return distill_supported(rows, vocab, k) ? distill_layout(rows, vocab, k).bytes : 0;
+}
+
+domino_status domino_distill_loss(int32_t rows, int32_t vocab, int32_t k, const void *logits, domino_dtype logits_dtype,
+                                  int64_t ld, const int32_t *teacher_ids, const float *teacher_vals,
+                                  const float *teacher_rest, float temperature, const float *row_weights,
+                                  float grad_scale, float *loss, float *row_loss, void *grad, int64_t ld_grad,
+                                  void *workspace, size_t workspace_bytes, void *stream) {
+  if (domino_status s = check_rows(rows, vocab, logits, logits_dtype, ld); s != DOMINO_OK) return s;
+  if (k < 1 || k > 1024 || k > vocab) return fail(DOMINO_ERR_INVALID_ARG, "k must be in [1, 1024] and at most vocab");
+  if (!temperature_ok(temperature)) return fail(DOMINO_ERR_INVALID_ARG, "temperature must be positive and finite");
+  if (!std::isfinite(grad_scale)) return fail(DOMINO_ERR_INVALID_ARG, "grad_scale must be finite");
+  if (!teacher_ids || !teacher_vals || !loss) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (grad && ((uintptr_t)grad % (logits_dtype == DOMINO_BF16 ? 2 : 4) || ld_grad < vocab))
+    return fail(DOMINO_ERR_INVALID_ARG, "grad is not aligned to its type, or ld_grad is less than vocab");
+  if (grad == logits && ld_grad != ld) return fail(DOMINO_ERR_INVALID_ARG, "grad in the logits' place needs ld_grad = ld");
+  if (!distill_supported(rows, vocab, k))
+    return fail(DOMINO_ERR_UNSUPPORTED, "rows x ceil(vocab / 4096) must be at most %ld", kMaxBlocks);
+  const DistillLayout l = distill_layout(rows, vocab, k);
+  if (domino_status s = check_workspace(workspace, workspace_bytes, l.bytes); s != DOMINO_OK) return s;
+  char *ws = (char *)workspace;
+  DistillArgs a = {};
+  a.rows = rows;
+  a.V = vocab;
+  a.k = k;
+  a.nch = l.nch;
+  a.logits = logits;
+  a.ld = (size_t)ld;
+  a.ids = teacher_ids;
+  a.t_vals = teacher_vals;
+  a.t_rest = teacher_rest;
+  a.weights = row_weights;
+  a.T = temperature;
+  a.c = (float)(1.44269504088896340736 / (double)temperature);
+  a.grad_scale = grad_scale;
+  a.grad = grad;
+  a.ld_grad = (size_t)ld_grad;
+  a.loss = loss;
+  a.row_loss = row_loss ? row_loss : (float *)(ws + l.row_loss);
+  a.err = (int32_t *)ws;
+  a.wsum = (double *)(ws + l.wsum);
+  a.part = (float2 *)(ws + l.part);
+  a.z = (float *)(ws + l.z);
+  a.stat = (float2 *)(ws + l.stat);
+  a.share = (double *)(ws + l.share);
+  launch_distill(a, logits_dtype == DOMINO_BF16, (hipStream_t)stream);
+  hipError_t he = hipGetLastError();
+  if (he != hipSuccess) return fail(DOMINO_ERR_HIP, "distill_loss launch: %s", hipGetErrorString(he));
+  return DOMINO_OK;
+}
+
 domino_status domino_philox4x32_10(const uint32_t *counters, uint64_t key, uint32_t *out, int32_t n, void *stream) {
   if (n < 0) return fail(DOMINO_ERR_INVALID_ARG, "n must be >= 0");
   if (n > 0 && (!counters || !out)) return fail(DOMINO_ERR_INVALID_ARG, "counters/out is NULL");

@@ -141,7 +141,8 @@ enum : int32_t {
   DEV_BAD_TOKEN = 1,
   DEV_BAD_CTX_LEN = 2,
   DEV_BAD_TREE = 4,
-  DEV_BARRIER_TIMEOUT = 8
+  DEV_BARRIER_TIMEOUT = 8,
+  DEV_BAD_PARAM = 16
 };
 
 DEVI void raise_error(int32_t *err, int32_t bit) { atomicOr(err, bit); }

@@ -1,0 +1,305 @@
+// Distillation from a teacher's top entries: loss and gradient.
+//
+// A row has V student logits l and k teacher entries (id i, logit t_i), with the
+// log-sum-exp rest_t of the teacher's other ids (-inf when it is not given).  Both
+// distributions are taken over k + 1 buckets, the entries and one bucket of every
+// other id:
+//   p = softmax(t_1 / T, .., t_k / T, rest_t)
+//   q_i = exp(l_i / T) / Z,  q_rest = R / Z,  R = sum_{v not an entry} exp(l_v / T),
+//   Z = R + sum_i exp(l_i / T)
+//   row_loss = T^2 (sum_i p_i log(p_i / q_i) + p_rest log(p_rest / q_rest))
+//   loss = sum_r w_r row_loss_r / W,  W = sum_r w_r
+//   dloss/dl_i = T w_r / W (q_i - p_i)
+//   dloss/dl_v = T w_r / W (exp(l_v / T) / R) (q_rest - p_rest),  v not an entry
+// R is summed over the other ids alone, never as a total less the entries, so that
+// it keeps its precision where the entries hold nearly everything.
+//
+// Three launches:
+//   part  (row, chunk of the vocabulary): max and sum of exp of the chunk's values that
+//         are no entries (a bit each in LDS marks the entries), and the entries' values
+//   row   a workgroup a row: R, Z, the loss and the gradients of the entries
+//   grad  (row, chunk): the gradient, the entries' own through LDS; its last workgroup
+//         adds the rows' losses.  Without a gradient that workgroup is all there is.
+#include "common.h"
+#include "kernels.h"
+#include "rows.h"
+
+namespace dk {
+
+constexpr int kDsThreads = 256;
+constexpr int kDsChunk = 4096;  // vocabulary ids a workgroup
+constexpr int kDsWaves = kDsThreads / 64;
+
+template <typename LT>
+constexpr int kDsVecs = kDsChunk / kDsThreads / RowVec<LT>::N;
+
+// this thread's vectors of chunk ch: vector q at ids id0 + q * step
+template <typename LT>
+DEVI void ds_load(const LT *row, uint32_t c0, uint32_t V, u32x4 (&x)[kDsVecs<LT>]) {
+  constexpr int N = RowVec<LT>::N;
+  if (c0 + kDsChunk <= V) {  // workgroup-uniform: every load goes out at once
+#pragma unroll
+    for (int q = 0; q < kDsVecs<LT>; ++q) x[q] = row_load(row + c0 + (q * kDsThreads + threadIdx.x) * N);
+  } else {
+#pragma unroll
+    for (int q = 0; q < kDsVecs<LT>; ++q) x[q] = row_load_end(row, c0 + (q * kDsThreads + threadIdx.x) * N, V);
+  }
+}
+
+// a weight that counts: not negative, finite; anything else counts as 0
+DEVI float ds_weight(float w) { return w >= 0.f && w < INFINITY ? w : 0.f; }
+
+// the N bits of the vector at in-chunk place `at` (a multiple of N)
+template <int N>
+DEVI uint32_t ds_bits(const uint32_t *bits, uint32_t at) {
+  return (bits[at >> 5] >> (at & 31)) & ((1u << N) - 1u);
+}
+
+// (1) One chunk of one row.  An id given twice, or outside [-1, V), is marked by a NaN
+// (as its max: errors are raised by the next launch, since this one clears the error
+// word).  The workgroup after the last chunk adds the rows' weights.
+template <typename LT>
+__global__ __launch_bounds__(kDsThreads) void distill_part_kernel(DistillArgs a, int chunks) {
+  constexpr int N = RowVec<LT>::N, NV = kDsVecs<LT>;
+  const int row = blockIdx.x / a.nch, ch = blockIdx.x % a.nch, tid = threadIdx.x;
+  __shared__ uint32_t bits[kDsChunk / 32];
+  __shared__ float red[2][kDsWaves];
+  __shared__ double redw[2][kDsWaves];
+  __shared__ int bad;
+  if ((int)blockIdx.x == chunks) {
+    double W = 0.0, odd = 0.0;
+    for (int r = tid; r < a.rows; r += kDsThreads) {
+      const float w = a.weights ? a.weights[r] : 1.f;
+      if (ds_weight(w) == w) W += w;
+      else odd = 1.0;
+    }
+    W = block_reduce_sum<kDsWaves>(W, redw[0]);
+    odd = block_reduce_sum<kDsWaves>(odd, redw[1]);
+    if (tid == 0) {
+      *a.err = 0;
+      a.wsum[0] = W;
+      a.wsum[1] = odd;
+    }
+    return;
+  }
+  const uint32_t c0 = (uint32_t)ch * kDsChunk, V = a.V;
+  const LT *lr = (const LT *)a.logits + (size_t)row * a.ld;
+  u32x4 x[NV];
+  ds_load<LT>(lr, c0, V, x);
+  if (tid < kDsChunk / 32) bits[tid] = 0;
+  if (tid == 0) bad = 0;
+  __syncthreads();
+  for (int i = tid; i < a.k; i += kDsThreads) {
+    const int id = a.ids[(size_t)row * a.k + i];
+    const uint32_t at = (uint32_t)id - c0;
+    if (id >= 0 && id < a.V) {
+      if (at < kDsChunk) {
+        const uint32_t bit = 1u << (at & 31);
+        if (atomicOr(&bits[at >> 5], bit) & bit) bad = 1;
+        a.z[(size_t)row * a.k + i] = order_val(to_f32(lr[id]));
+      }
+    } else if (ch == 0 && id != -1) {
+      bad = 1;
+    }
+  }
+  __syncthreads();
+  float m = -INFINITY;
+#pragma unroll
+  for (int q = 0; q < NV; ++q) {
+    const uint32_t mine = ds_bits<N>(bits, (q * kDsThreads + tid) * N);
+    if (mine) {  // few lanes: the entries out of the sum
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (mine >> e & 1) RowVec<LT>::set(x[q], e, RowVec<LT>::low());
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) m = fmaxf(m, RowVec<LT>::get(x[q], e));
+  }
+  m = block_reduce_max<kDsWaves>(m, red[0]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float s = 0.f;
+#pragma unroll
+  for (int q = 0; q < NV; ++q)
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      s += __builtin_amdgcn_exp2f((order_val(RowVec<LT>::get(x[q], e)) - ref) * a.c);
+  s = block_reduce_sum<kDsWaves>(s, red[1]);
+  if (tid == 0) a.part[(size_t)row * a.nch + ch] = make_float2(bad ? NAN : m, s);
+}
+
+// (2) One row, in 64 bits: a few hundred values, and differences of logarithms.
+__global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs a) {
+  const int row = blockIdx.x, tid = threadIdx.x;
+  __shared__ float redf[4][kDsWaves];
+  __shared__ double red[4][kDsWaves];
+  const float2 *part = a.part + (size_t)row * a.nch;
+  const int32_t *ids = a.ids + (size_t)row * a.k;
+  const float *tv = a.t_vals + (size_t)row * a.k;
+  float *z = a.z + (size_t)row * a.k;
+  const double inv_t = 1.0 / (double)a.T;
+  const double W = a.wsum[0];
+  const float w = ds_weight(a.weights ? a.weights[row] : 1.f);
+  // maxima: the other ids', the entries', the teacher's
+  float mr = -INFINITY, mz = -INFINITY, mt = -INFINITY;
+  float odd = 0.f;
+  for (int c = tid; c < a.nch; c += kDsThreads) {
+    const float x = part[c].x;
+    if (x != x) odd = 1.f;
+    mr = fmaxf(mr, x);
+  }
+  for (int i = tid; i < a.k; i += kDsThreads) {
+    if (ids[i] < 0 || ids[i] >= a.V) continue;
+    mz = fmaxf(mz, z[i]);
+    mt = fmaxf(mt, tv[i]);
+  }
+  mr = block_reduce_max<kDsWaves>(mr, redf[0]);
+  mz = block_reduce_max<kDsWaves>(mz, redf[1]);
+  mt = block_reduce_max<kDsWaves>(mt, redf[2]);
+  const bool bad = block_reduce_max<kDsWaves>(odd, redf[3]) != 0.f;
+  const float rt = a.t_rest ? order_val(a.t_rest[row]) : -INFINITY;
+  // sums relative to the maxima: R / exp(mr / T); Z / exp(m / T); the teacher's over the larger of its two parts
+  double R = 0.0, E = 0.0, P = 0.0;
+  const double tm = fmax((double)mt * inv_t, (double)rt);
+  const float m = fmaxf(mr, mz);
+  for (int c = tid; c < a.nch; c += kDsThreads) {
+    const float2 p = part[c];
+    if (p.x != -INFINITY) R += (double)p.y * exp(((double)p.x - mr) * inv_t);  // (NaN in a row of +inf)
+  }
+  for (int i = tid; i < a.k; i += kDsThreads) {
+    if (ids[i] < 0 || ids[i] >= a.V) continue;
+    if (z[i] != -INFINITY) E += exp(((double)z[i] - m) * inv_t);
+    const double t = (double)order_val(tv[i]) * inv_t;
+    if (t != -INFINITY) P += exp(t - tm);
+  }
+  R = block_reduce_sum<kDsWaves>(R, red[0]);
+  E = block_reduce_sum<kDsWaves>(E, red[1]);
+  P = block_reduce_sum<kDsWaves>(P, red[2]);
+  if (rt != -INFINITY) P += exp((double)rt - tm);
+  // logarithms relative to the maxima: beside values near the type's lowest log(V) would be lost
+  const double r_m = ((double)mr - m) * inv_t;
+  double Z = E;
+  if (R != 0.0) Z += R * exp(r_m);
+  const double log_Z = log(Z), log_P = log(P);      // Z = 0: no student logit above -inf
+  const bool none = tm == -INFINITY;                // the teacher says nothing of this row
+  const double scale = W > 0.0 && !none ? (double)a.T * (double)w / W * (double)a.grad_scale : 0.0;
+  double kl = 0.0;
+  for (int i = tid; i < a.k; i += kDsThreads) {
+    double g = 0.0;
+    if (ids[i] >= 0 && ids[i] < a.V) {
+      const double lp = ((double)order_val(tv[i]) * inv_t - tm) - log_P;
+      const double lq = z[i] == -INFINITY ? -INFINITY : ((double)z[i] - m) * inv_t - log_Z;
+      const double p = exp(lp);
+      if (!none && p != 0.0) kl += p * (lp - lq);
+      g = scale * (exp(lq) - p);
+    }
+    z[i] = scale == 0.0 ? 0.f : bad ? NAN : (float)g;  // the entry's value is read, its gradient takes its place
+  }
+  kl = block_reduce_sum<kDsWaves>(kl, red[3]);
+  if (tid == 0) {
+    const double lpr = ((double)rt - tm) - log_P, lqr = R == 0.0 ? -INFINITY : r_m + (log(R) - log_Z);
+    const double pr = none || rt == -INFINITY ? 0.0 : exp(lpr);
+    if (!none && pr != 0.0) kl += pr * (lpr - lqr);
+    const double loss = bad ? NAN : none ? 0.0 : (double)a.T * (double)a.T * kl;
+    if (bad) raise_error(a.err, DEV_BAD_TOKEN);
+    if (row == 0 && a.wsum[1] != 0.0) raise_error(a.err, DEV_BAD_PARAM);
+    a.row_loss[row] = (float)loss;
+    a.share[row] = w > 0.f ? (double)w / W * loss : 0.0;
+    // of any other id: exp((l - mr) / T) times this
+    const double coef = scale == 0.0 ? 0.0 : bad ? NAN : R == 0.0 ? 0.0 : scale * (exp(lqr) - pr) / R;
+    a.stat[row] = make_float2(mr == -INFINITY ? 0.f : mr, (float)coef);
+  }
+}
+
+// (3) The gradient of one chunk of one row; the workgroup after the last chunk adds the losses.
+template <typename LT>
+__global__ __launch_bounds__(kDsThreads) void distill_grad_kernel(DistillArgs a, int chunks) {
+  constexpr int N = RowVec<LT>::N, NV = kDsVecs<LT>;
+  const int tid = threadIdx.x;
+  __shared__ uint32_t bits[kDsChunk / 32];
+  __shared__ float own[kDsChunk];
+  __shared__ double red[kDsWaves];
+  if ((int)blockIdx.x == chunks) {
+    double s = 0.0;
+    for (int r = tid; r < a.rows; r += kDsThreads) s += a.share[r];
+    s = block_reduce_sum<kDsWaves>(s, red);
+    if (tid == 0) *a.loss = (float)s;
+    return;
+  }
+  const int row = blockIdx.x / a.nch, ch = blockIdx.x % a.nch;
+  const uint32_t c0 = (uint32_t)ch * kDsChunk, V = a.V;
+  const LT *lr = (const LT *)a.logits + (size_t)row * a.ld;
+  LT *gr = (LT *)a.grad + (size_t)row * a.ld_grad;
+  u32x4 x[NV];
+  ds_load<LT>(lr, c0, V, x);
+  if (tid < kDsChunk / 32) bits[tid] = 0;
+  __syncthreads();
+  const float2 st = a.stat[row];
+  for (int i = tid; i < a.k; i += kDsThreads) {
+    const uint32_t at = (uint32_t)a.ids[(size_t)row * a.k + i] - c0;
+    if (at < kDsChunk) {
+      atomicOr(&bits[at >> 5], 1u << (at & 31));
+      own[at] = a.z[(size_t)row * a.k + i];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < NV; ++q) {
+    const uint32_t at = (q * kDsThreads + tid) * N;
+    const uint32_t mine = ds_bits<N>(bits, at);
+    u32x4 y = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float v = order_val(RowVec<LT>::get(x[q], e));
+      const float g = __builtin_amdgcn_exp2f((v - st.x) * a.c) * st.y;
+      LT o;
+      store_as(&o, st.y == 0.f ? 0.f : g);
+      RowVec<LT>::set(y, e, o);
+    }
+    if (mine) {  // few lanes: the entries' own
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (mine >> e & 1) {
+          LT o;
+          store_as(&o, own[at + e]);
+          RowVec<LT>::set(y, e, o);
+        }
+    }
+    if (c0 + at + N <= V) {
+      row_store(gr + c0 + at, y);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (c0 + at + e < V) gr[c0 + at + e] = RowVec<LT>::at(y, e);
+    }
+  }
+}
+
+// [error word, padded to 256][weights' sum, padded to 256][chunk pairs][entries: value, then gradient][rows: stat, share of the loss, loss]
+DistillLayout distill_layout(int rows, int V, int k) {
+  DistillLayout l;
+  const size_t n = rows;
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  l.nch = (int)(((long)V + kDsChunk - 1) / kDsChunk);
+  l.wsum = 256;
+  l.part = 512;
+  l.z = l.part + up(n * l.nch * sizeof(float2));
+  l.stat = l.z + up(n * k * sizeof(float));
+  l.share = l.stat + up(n * sizeof(float2));
+  l.row_loss = l.share + up(n * sizeof(double));
+  l.bytes = l.row_loss + up(n * sizeof(float));
+  return l;
+}
+
+void launch_distill(const DistillArgs &a, bool bf16, hipStream_t st) {
+  const int chunks = a.rows * a.nch;
+  auto go = [&](auto part, auto grad) {
+    hipLaunchKernelGGL(part, dim3(chunks + 1), dim3(kDsThreads), 0, st, a, chunks);
+    hipLaunchKernelGGL(distill_row_kernel, dim3(a.rows), dim3(kDsThreads), 0, st, a);
+    const int n = a.grad ? chunks : 0;
+    hipLaunchKernelGGL(grad, dim3(n + 1), dim3(kDsThreads), 0, st, a, n);
+  };
+  if (bf16) go(distill_part_kernel<bf16_t>, distill_grad_kernel<bf16_t>);
+  else go(distill_part_kernel<float>, distill_grad_kernel<float>);
+}
+
+}  // namespace dk

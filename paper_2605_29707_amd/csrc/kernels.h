@@ -253,6 +253,58 @@ void launch_verify_sample(int bs, int B, int V, const int32_t *node_token, const
                           int32_t *accepted_nodes, int32_t *out_tokens, void *ws, hipStream_t st);
 void launch_philox_words(const uint32_t *ctr, uint64_t key, uint32_t *out, int n, hipStream_t st);
 
+// ---- rows of logits: top entries and filtered sampling (logits.hip)
+constexpr int kRowsMaxVocab = 327680;  // ten groups of 32 ids in the registers of each of 1024 threads
+struct RowsArgs {
+  int rows, V;
+  const void *logits;  // rows ld elements apart
+  size_t ld;
+  const float *temps;  // optional [rows], else T for every row
+  float T;
+  // set at launch, from the workspace
+  int32_t *err;
+  float2 *groups;      // [rows][G]: (max, sum of exp) of every 32 ids
+  int G, nch;          // workgroups a row of the first launch
+};
+struct SampleArgs {
+  const int32_t *top_k;  // optional [rows] each
+  const float *top_p, *min_p;
+  const float *uniforms;  // [rows]
+  int32_t *tokens;
+  float *logprobs;       // optional
+};
+size_t rows_ws_bytes(int rows, int V);
+void launch_top_logits(RowsArgs a, bool bf16, int k, int32_t *ids, float *vals, float *rest, void *ws, hipStream_t st);
+void launch_sample_logits(RowsArgs a, bool bf16, const SampleArgs &p, void *ws, hipStream_t st);
+
+// ---- distillation from a teacher's top entries (distill.hip)
+struct DistillArgs {
+  int rows, V, k, nch;
+  const void *logits;
+  size_t ld;
+  const int32_t *ids;     // [rows][k], -1: none
+  const float *t_vals;    // [rows][k]
+  const float *t_rest;    // optional [rows]
+  const float *weights;   // optional [rows]
+  float T, c, grad_scale; // c = log2(e) / T
+  void *grad;             // optional, rows ld_grad elements apart
+  size_t ld_grad;
+  float *loss, *row_loss;
+  // workspace
+  int32_t *err;
+  double *wsum;           // [2]: the weights' sum; not 0 if one was out of range
+  float2 *part;           // [rows][nch]: (max, sum of exp) of a chunk's values that are no entries
+  float *z;               // [rows][k]: the entries' logits, then their gradients
+  float2 *stat;           // [rows]: the other ids' max and factor of the gradient
+  double *share;          // [rows]: what the row adds to the loss
+};
+struct DistillLayout {
+  int nch;
+  size_t wsum, part, z, stat, share, row_loss, bytes;
+};
+DistillLayout distill_layout(int rows, int V, int k);
+void launch_distill(const DistillArgs &a, bool bf16, hipStream_t st);
+
 // misc
 void launch_to_f32(const void *src, bool bf16, float *dst, size_t n, hipStream_t st);
 // Y[r][n] += bias[n] for r < rows, n < N (row stride N)
