@@ -35,6 +35,9 @@ constexpr int kSelRegs = kRowsMaxVocab / (kGroup * kSelThreads);  // group maxim
 static_assert(kRowsMaxVocab % (kGroup * kSelThreads) == 0, "whole registers of groups");
 constexpr int kTopMax = 1024;     // entries at most: one a thread
 constexpr int kListMax = 2048;    // candidates sorted in LDS
+constexpr int kSelMax = 2048;     // groups read
+constexpr uint32_t kIdMask = 0xfffffu;
+static_assert(kRowsMaxVocab <= kIdMask, "ids in 20 bits");
 
 // log2(e) / T, kept finite: a difference of 0 has to stay 0
 DEVI float row_scale(float T) { return fminf(kRowLog2e / T, 1e30f); }
@@ -85,15 +88,17 @@ __global__ __launch_bounds__(kGrThreads) void row_groups_kernel(RowsArgs a) {
 // ---------------------------------------------------------------------------
 // (2) selection within a row
 // ---------------------------------------------------------------------------
+// What bounds it is the chain of steps of one workgroup, and the first run of each
+// instruction, which comes from memory: loops stay loops where that costs nothing (a first
+// version with every loop unrolled, 74 to 280 KB of code, took 23 us for one row).
 struct SelShared {
   unsigned long long list[kListMax];  // keys: order_key of the value, complement of the id
-  unsigned long long cnt[2][kSelWaves];
-  int sel[kTopMax];                   // the selected groups
-  int gcnt[kSelRegs * kSelWaves];
-  float redf[2][kSelWaves];
+  int sel[kSelMax];                   // the selected groups
+  uint32_t hist[kSelThreads];
+  uint32_t wave[2][kSelWaves];
+  float redf[kSelWaves];
   double redd[kSelWaves];
-  unsigned long long redu[kSelWaves];
-  uint32_t mm[2][kSelWaves];
+  uint32_t hit[3];
   int n;
 };
 
@@ -101,79 +106,94 @@ DEVI unsigned long long entry_key(float v, uint32_t id) { return ((unsigned long
 DEVI float entry_value(unsigned long long k) { return order_key_value((uint32_t)(k >> 32)); }
 DEVI uint32_t entry_id(unsigned long long k) { return 0xffffffffu - (uint32_t)k; }
 
-// the largest t with at least `want` of the workgroup's numbers >= t, two bits a
-// step from the highest bit in which the numbers can differ.  count(t1, t2, t3)
-// gives a wave's numbers >= each, packed by 20 bits; [lo, hi] holds them all.
-template <typename Count>
-DEVI uint32_t kth_largest(uint32_t lo, uint32_t hi, int want, SelShared &sh, Count count) {
-  if (lo >= hi) return hi;
-  int shift = (31 - __builtin_clz(lo ^ hi)) & ~1;
-  uint32_t t = shift == 30 ? 0u : hi & ~((4u << shift) - 1u);
-  for (int it = 0; shift >= 0; shift -= 2, it ^= 1) {
-    const uint32_t t1 = t | (1u << shift), t2 = t | (2u << shift), t3 = t | (3u << shift);
-    const unsigned long long c = count(t1, t2, t3);
-    if ((threadIdx.x & 63) == 0) sh.cnt[it][threadIdx.x >> 6] = c;
-    __syncthreads();
-    unsigned long long s = 0;
+// inclusive running sum over the workgroup's threads; `red` is free again after the next barrier
+template <typename T>
+DEVI T block_scan(T v, T *red) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int w = 0; w < kSelWaves; ++w) s += sh.cnt[it][w];
-    const int n1 = (int)(s & 0xfffff), n2 = (int)(s >> 20 & 0xfffff), n3 = (int)(s >> 40);
-    t = n3 >= want ? t3 : n2 >= want ? t2 : n1 >= want ? t1 : t;
+  for (int o = 1; o < 64; o <<= 1) {
+    const T y = __shfl_up(v, o, 64);
+    if (lane >= o) v += y;
   }
-  __syncthreads();  // sh.cnt is free again
-  return t;
-}
-DEVI unsigned long long pack3(int a, int b, int c) {
-  return (unsigned long long)a | (unsigned long long)b << 20 | (unsigned long long)c << 40;
-}
-// a count over the workgroup, from each wave's
-DEVI int block_count(int wave_n, int slot, SelShared &sh) {
-  if ((threadIdx.x & 63) == 0) sh.cnt[slot][threadIdx.x >> 6] = wave_n;
+  if (lane == 63) red[wave] = v;
   __syncthreads();
-  unsigned long long s = 0;
-#pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) s += sh.cnt[slot][w];
-  __syncthreads();
-  return (int)s;
-}
-// (min, max) over the workgroup
-DEVI void block_range(uint32_t &lo, uint32_t &hi, SelShared &sh) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
-    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
-  }
-  if ((threadIdx.x & 63) == 0) {
-    sh.mm[0][threadIdx.x >> 6] = lo;
-    sh.mm[1][threadIdx.x >> 6] = hi;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) {
-    lo = min(lo, sh.mm[0][w]);
-    hi = max(hi, sh.mm[1][w]);
-  }
-  __syncthreads();
+  T base = 0;
+  for (int w = 0; w < wave; ++w) base += red[w];
+  return base + v;
 }
 
-// sh.list[0 .. n) in descending order (keys are distinct), n <= kListMax.  Up to 512 each
-// key counts those before it; more by a bitonic network.
+// Those with a key above `key`, or with this key and an id up to `id`.
+struct Cut {
+  uint32_t key, id;
+  DEVI bool has(uint32_t k, uint32_t i) const { return k > key || (k == key && i <= id); }
+};
+
+// A cut that takes at least `want` items, and at most `cap` (want <= cap): by counts in 1024
+// equal parts of [lo, hi], which holds the key of the want-th, and again of the part that holds
+// it while there are more than `cap` up to its end; among equal keys the same by ids.
+// each(f) calls f(key, id) for every item.
+template <typename Each>
+DEVI Cut cut_at(uint32_t lo, uint32_t hi, int want, int cap, SelShared &sh, Each each) {
+  const int tid = threadIdx.x;
+  bool by_id = false;
+  uint32_t key = 0;
+  int above = 0;  // items beyond hi
+  while (true) {
+    const uint32_t range = hi - lo;
+    const int shift = range < kSelThreads ? 0 : 22 - __builtin_clz(range);
+    sh.hist[tid] = 0;
+    __syncthreads();
+    each([&](uint32_t k, uint32_t id) {
+      const uint32_t x = by_id ? kIdMask - id : k;
+      if (x >= lo && x <= hi && (!by_id || k == key)) atomicAdd(&sh.hist[kSelThreads - 1 - ((x - lo) >> shift)], 1u);
+    });
+    __syncthreads();
+    const int c = sh.hist[tid];
+    const int n = above + block_scan<uint32_t>(c, sh.wave[0]);
+    if (n >= want && n - c < want) {  // one thread of all
+      sh.hit[0] = kSelThreads - 1 - tid;
+      sh.hit[1] = n;
+      sh.hit[2] = n - c;
+    }
+    __syncthreads();
+    const uint32_t part = lo + (sh.hit[0] << shift);
+    const int upto = sh.hit[1], before = sh.hit[2];
+    if (upto <= cap) return by_id ? Cut{key, kIdMask - part} : Cut{part, 0xffffffffu};
+    above = before;
+    if (shift > 0) {
+      hi = min(hi, part + ((1u << shift) - 1u));
+      lo = part;
+    } else {  // (a part of ids holds one item: it would have been taken)
+      by_id = true;
+      key = part;
+      lo = 0;
+      hi = kIdMask;
+    }
+  }
+}
+
+// sh.list[0 .. n) in descending order (keys are distinct).  Up to 256 a key counts those before
+// it (n^2 / 64 reads of 4 cycles), by several threads where there are enough; more by a bitonic
+// network, whose short steps stay within a wave and need no barrier.
 DEVI void sort_list(int n, SelShared &sh) {
   const int tid = threadIdx.x;
   __syncthreads();
-  if (n <= 512) {
+  if (n <= 256) {
+    const int lg = n <= 64 ? 4 : n <= 128 ? 3 : 2, i = tid >> lg, parts = 1 << lg;
     unsigned long long k = 0;
     int r = 0;
-    if (tid < n) {
-      k = sh.list[tid];
-      for (int i = 0; i < n; ++i) r += sh.list[i] > k;
+    if (i < n) {
+      k = sh.list[i];
+      for (int j = tid & (parts - 1); j < n; j += parts) r += sh.list[j] > k;
     }
+    for (int o = 1; o < parts; o <<= 1) r += __shfl_xor(r, o, 64);
     __syncthreads();
-    if (tid < n) sh.list[r] = k;
+    if (i < n && (tid & (parts - 1)) == 0) sh.list[r] = k;
     __syncthreads();
     return;
   }
-  const int size = n <= 1024 ? 1024 : 2048;
+  int size = 512;
+  while (size < n) size <<= 1;
   for (int i = n + tid; i < size; i += kSelThreads) sh.list[i] = 0;
   __syncthreads();
   for (int len = 2; len <= size; len <<= 1)
@@ -187,219 +207,195 @@ DEVI void sort_list(int n, SelShared &sh) {
           sh.list[j] = x;
         }
       }
-      __syncthreads();
+      // a wave's 128 keys are its own up to steps of 64
+      if (step > 64 || (step == 1 && len >= 128)) __syncthreads();
+      else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
     }
+  __syncthreads();
 }
 
-// push of the lanes whose `on` is set; sh.n counts (past kListMax nothing is stored)
-DEVI void push_list(bool on, unsigned long long key, SelShared &sh) {
-  const unsigned long long mk = __ballot(on);
-  if (!mk) return;
-  const int lane = threadIdx.x & 63;
-  int at = 0;
-  if (lane == 0) at = atomicAdd(&sh.n, __popcll(mk));
-  at = __builtin_amdgcn_readfirstlane(at) + __popcll(mk & ((1ull << lane) - 1));
-  if (on && at < kListMax) sh.list[at] = key;
-}
-
-// The first C entries of a row, sorted, in sh.list; with REST also their complement's
-// sum: max in rest_m, sum of exp((l - rest_m) / T) in rest_s.  C <= min(V, kTopMax).
-template <typename LT, bool REST>
+// The first C entries of a row, sorted, in sh.list; of the others the largest value (rest_m)
+// and the sum of exp((l - rest_m) / T) (rest_s).  C <= min(V, kTopMax).
+template <typename LT>
 DEVI void select_top(const LT *lr, const float2 *groups, int V, int G, int C, float c, SelShared &sh, float &rest_m,
                      double &rest_s) {
   constexpr int N = RowVec<LT>::N, LPG = kGroup / N;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // the groups' maxima, group i * 1024 + tid in register i
+  // the groups, group i * 1024 + tid in register i
   uint32_t gk[kSelRegs];
+  float gs[kSelRegs];
   const int nr = (G + kSelThreads - 1) / kSelThreads;
+  uint32_t hi = 0;
 #pragma unroll
   for (int i = 0; i < kSelRegs; ++i) {
     gk[i] = 0;  // (no value has the key 0)
+    gs[i] = 0.f;
     if (i < nr) {
       const int g = i * kSelThreads + tid;
-      if (g < G) gk[i] = order_key(groups[g].x);
+      if (g < G) {
+        const float2 x = groups[g];
+        gk[i] = order_key(x.x);
+        gs[i] = x.y;
+      }
+      hi = max(hi, gk[i]);
     }
   }
-  const int take = min(C, G);  // groups to read
-  uint32_t gt = 0;             // the key of the last of them
-  int over = 0;                // of those with just this key, how many are read
-  if (take < G) {
-    uint32_t lo = 0xffffffffu, hi = 0;
-#pragma unroll
-    for (int i = 0; i < kSelRegs; ++i)
-      if (gk[i]) {
-        lo = min(lo, gk[i]);
-        hi = max(hi, gk[i]);
-      }
-    block_range(lo, hi, sh);
-    gt = kth_largest(lo, hi, take, sh, [&](uint32_t t1, uint32_t t2, uint32_t t3) {
-      int n1 = 0, n2 = 0, n3 = 0;
-#pragma unroll
-      for (int i = 0; i < kSelRegs; ++i)
-        if (i < nr) {
-          n1 += __popcll(__ballot(gk[i] >= t1));
-          n2 += __popcll(__ballot(gk[i] >= t2));
-          n3 += __popcll(__ballot(gk[i] >= t3));
-        }
-      return pack3(n1, n2, n3);
-    });
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < kSelRegs; ++i)
-      if (i < nr) n += __popcll(__ballot(gk[i] > gt));
-    over = take - block_count(n, 0, sh);
+  // Bounds of the C-th group's key.  From below: the least of 1024 / s maxima, each of the groups
+  // of s threads, with 1024 / s >= C of them (where every thread has one).
+  uint32_t lo = hi;
+  if (G >= kSelThreads) {
+    for (int s = 1; s < 64 && kSelThreads / (2 * s) >= C; s <<= 1) lo = max(lo, (uint32_t)__shfl_xor((int)lo, s, 64));
+  } else if (lo == 0) {
+    lo = 0xffffffffu;  // (a thread without a group)
   }
-  // Places in group order (so that sums over the groups have one order): first those
-  // with the last key are counted, then the chosen ones.
-  uint32_t chosen = 0;  // a bit a register
-  for (int pass = take < G ? 0 : 1; pass < 2; ++pass) {
 #pragma unroll
-    for (int i = 0; i < kSelRegs; ++i)
-      if (i < nr) {
-        const bool on = pass == 0 ? gk[i] == gt : take == G ? gk[i] != 0 : gk[i] > gt || (chosen >> i & 1);
-        const int n = __popcll(__ballot(on));
-        if (lane == 0) sh.gcnt[i * kSelWaves + wave] = n;
-      }
-    __syncthreads();
-    if (wave == 0) {  // exclusive running sums over (register, wave)
-      int base = 0;
-      for (int j0 = 0; j0 < nr * kSelWaves; j0 += 64) {
-        const int n = j0 + lane < nr * kSelWaves ? sh.gcnt[j0 + lane] : 0;
-        int x = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const int y = __shfl_up(x, o, 64);
-          if (lane >= o) x += y;
-        }
-        if (j0 + lane < nr * kSelWaves) sh.gcnt[j0 + lane] = base + x - n;
-        base += __shfl(x, 63, 64);
-      }
-    }
-    __syncthreads();
-    const unsigned long long below = (1ull << lane) - 1;
-#pragma unroll
-    for (int i = 0; i < kSelRegs; ++i)
-      if (i < nr) {
-        const bool on = pass == 0 ? gk[i] == gt : take == G ? gk[i] != 0 : gk[i] > gt || (chosen >> i & 1);
-        const int at = sh.gcnt[i * kSelWaves + wave] + __popcll(__ballot(on) & below);
-        if (pass == 0) {
-          if (on && at < over) chosen |= 1u << i;
-        } else {
-          if (on) sh.sel[at] = i * kSelThreads + tid;
-          if (on) chosen |= 1u << i;
-        }
-      }
-    __syncthreads();
+  for (int o = 32; o >= 1; o >>= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
   }
-  // their values, from memory in each pass (the caches hold them; 32 values a thread
-  // in registers beside the groups' maxima spill): vector u is part u % LPG of group u / LPG
-  const int nu = take * LPG;
-  auto each = [&](auto f) {  // f(value, its key, id, is one)
-    constexpr int U = 4;
-#pragma unroll 1
-    for (int u0 = 0; u0 < nu; u0 += U * kSelThreads) {
-      u32x4 x[U];
-      uint32_t id0[U];
+  if (lane == 0) {
+    sh.wave[0][wave] = lo;
+    sh.wave[1][wave] = hi;
+  }
+  __syncthreads();
+#pragma unroll 4
+  for (int w = 0; w < kSelWaves; ++w) {
+    lo = min(lo, sh.wave[0][w]);
+    hi = max(hi, sh.wave[1][w]);
+  }
+  auto every_group = [&](auto f) {
 #pragma unroll
-      for (int q = 0; q < U; ++q) {
-        const int u = u0 + q * kSelThreads + tid;
-        id0[q] = 0x7fffffffu;  // past every row: no value of it counts
-        if (u < nu) {
-          id0[q] = (uint32_t)sh.sel[u / LPG] * kGroup + (u % LPG) * N;
-          x[q] = row_load_end(lr, id0[q], V);
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < U; ++q)
-        if (u0 + q * kSelThreads < nu) {  // uniform
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const uint32_t id = id0[q] + e;
-            const float v = RowVec<LT>::get(x[q], e);
-            f(v, order_key(v), id, id < (uint32_t)V);
-          }
-        }
-    }
+    for (int i = 0; i < kSelRegs; ++i)
+      if (i < nr && gk[i]) f(gk[i], (uint32_t)(i * kSelThreads + tid));
   };
-  // Those that can be among the first C: not behind the last group's maximum.  Where they are
-  // more than the list holds, the C-th value itself, then the C-th id of that value.
-  uint32_t et = gt, eid = 0xffffffffu;  // entries with a key above et, or et and an id up to eid
-  for (int tries = 0;; ++tries) {
-    if (tid == 0) sh.n = 0;
-    __syncthreads();
-    each([&](float, uint32_t k, uint32_t id, bool in) {
-      push_list(in && (k > et || (k == et && id <= eid)), ((unsigned long long)k << 32) | (0xffffffffu - id), sh);
-    });
-    __syncthreads();
-    if (sh.n <= kListMax || tries == 2) break;
-    uint32_t lo = 0xffffffffu, hi = 0;
-    if (tries == 0) {
-      each([&](float, uint32_t k, uint32_t, bool in) {
-        if (in) {
-          lo = min(lo, k);
-          hi = max(hi, k);
-        }
-      });
-      block_range(lo, hi, sh);
-      lo = max(lo, et);
-      et = kth_largest(lo, hi, C, sh, [&](uint32_t t1, uint32_t t2, uint32_t t3) {
-        int n1 = 0, n2 = 0, n3 = 0;
-        each([&](float, uint32_t k, uint32_t, bool in) {
-          n1 += __popcll(__ballot(in && k >= t1));
-          n2 += __popcll(__ballot(in && k >= t2));
-          n3 += __popcll(__ballot(in && k >= t3));
-        });
-        return pack3(n1, n2, n3);
-      });
-    } else {
-      int n = 0;
-      each([&](float, uint32_t k, uint32_t, bool in) { n += __popcll(__ballot(in && k > et)); });
-      const int left = C - block_count(n, 0, sh);
-      // the left-th smallest id, as the left-th largest of the complements
-      eid = 0xfffffu - kth_largest(0, 0xfffffu, left, sh, [&](uint32_t t1, uint32_t t2, uint32_t t3) {
-              int n1 = 0, n2 = 0, n3 = 0;
-              each([&](float, uint32_t k, uint32_t id, bool in) {
-                const uint32_t r = 0xfffffu - id;
-                n1 += __popcll(__ballot(in && k == et && r >= t1));
-                n2 += __popcll(__ballot(in && k == et && r >= t2));
-                n3 += __popcll(__ballot(in && k == et && r >= t3));
-              });
-              return pack3(n1, n2, n3);
-            });
-    }
-  }
-  const int n = min(sh.n, kListMax);
-  sort_list(n, sh);
-  if (!REST) return;
-  // The rest: the groups not read, the values not listed, the list behind C.
-  float m = -INFINITY;
-  float2 gs[kSelRegs];
+  Cut gc = {0, 0xffffffffu};
+  if (G > kSelMax || C < G) gc = cut_at(lo, hi, min(C, G), kSelMax, sh, every_group);
+  // their list, by waves
+  uint32_t chosen = 0;
+  int nw = 0;
 #pragma unroll
   for (int i = 0; i < kSelRegs; ++i)
     if (i < nr) {
-      const int g = i * kSelThreads + tid;
-      gs[i] = g < G && !(chosen >> i & 1) ? groups[g] : make_float2(-INFINITY, 0.f);
-      m = fmaxf(m, gs[i].x);
+      const bool on = gk[i] && gc.has(gk[i], i * kSelThreads + tid);
+      chosen |= on ? 1u << i : 0u;
+      nw += __popcll(__ballot(on));
     }
-  each([&](float v, uint32_t k, uint32_t id, bool in) {
-    if (in && !(k > et || (k == et && id <= eid))) m = fmaxf(m, v);
-  });
+  __syncthreads();
+  if (lane == 0) sh.wave[0][wave] = nw;
+  if (tid == 0) sh.n = 0;
+  __syncthreads();
+  int at = 0, nsel = 0;
+#pragma unroll 4
+  for (int w = 0; w < kSelWaves; ++w) {
+    const int x = sh.wave[0][w];
+    if (w < wave) at += x;
+    nsel += x;
+  }
+#pragma unroll
+  for (int i = 0; i < kSelRegs; ++i)
+    if (i < nr) {
+      const unsigned long long mk = __ballot(chosen >> i & 1);
+      if (chosen >> i & 1) sh.sel[at + __popcll(mk & ((1ull << lane) - 1))] = i * kSelThreads + tid;
+      at += __popcll(mk);
+    }
+  __syncthreads();
+  // Their values: vector u is part u % LPG of group u / LPG.  The first kHeld a thread (256 groups)
+  // stay in registers from pass to pass; where there are more, every pass loads them again.
+  constexpr int kHeld = LPG / 4;
+  const int nu = nsel * LPG;
+  u32x4 x[kHeld];
+  uint32_t id0[kHeld];
+  auto load = [&](int u0) {
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q) {
+      const int u = u0 + q * kSelThreads + tid;
+      id0[q] = 0x7fffffffu;  // past every row: no value of it counts
+      if (u < nu) {
+        id0[q] = (uint32_t)sh.sel[u / LPG] * kGroup + (u % LPG) * N;
+        x[q] = row_load_end(lr, id0[q], V);
+      }
+    }
+  };
+  load(0);
+  auto every_vec = [&](auto f) {  // f(vector, its first id)
+    if (nu > kHeld * kSelThreads) load(0);
+#pragma unroll 1
+    for (int u0 = 0;;) {
+#pragma unroll
+      for (int q = 0; q < kHeld; ++q)
+        if (id0[q] < (uint32_t)V) f(x[q], id0[q]);
+      u0 += kHeld * kSelThreads;
+      if (u0 >= nu) break;
+      load(u0);
+    }
+  };
+  auto every_value = [&](auto f) {  // f(key, id)
+    every_vec([&](const u32x4 &y, uint32_t id) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (id + e < (uint32_t)V) f(order_key(RowVec<LT>::get(y, e)), id + e);
+    });
+  };
+  // The values that can be among the first C: those the cut of the groups' maxima takes by their
+  // key; where they are more than the list holds, those of a cut of their own.
+  Cut ec = {gc.key, 0xffffffffu};
+  float m;
+  for (bool cut = gc.key == 0 && V > kListMax;; cut = true) {  // (no cut of the groups: every value)
+    if (cut) {
+      lo = max(ec.key, 1u);
+      ec = cut_at(lo, hi, C, kListMax, sh, every_value);
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+    }
+    m = -INFINITY;
+    every_vec([&](const u32x4 &y, uint32_t id) {
+      uint32_t on = 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float v = RowVec<LT>::get(y, e);
+        const bool in = id + e < (uint32_t)V, has = in && ec.has(order_key(v), id + e);
+        on |= has ? 1u << e : 0u;
+        if (in && !has) m = fmaxf(m, v);
+      }
+      if (on) {
+        int to = atomicAdd(&sh.n, __popc(on));
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (on >> e & 1) {
+            if (to < kListMax) sh.list[to] = entry_key(RowVec<LT>::get(y, e), id + e);
+            ++to;
+          }
+      }
+    });
+    __syncthreads();
+    if (sh.n <= kListMax) break;
+  }
+  const int n = sh.n;
+  sort_list(n, sh);
+  // The rest: the groups not read, the values not listed, the list behind C.
+#pragma unroll
+  for (int i = 0; i < kSelRegs; ++i)
+    if (i < nr && gk[i] && !(chosen >> i & 1)) m = fmaxf(m, order_key_value(gk[i]));
   if (n > C) m = fmaxf(m, entry_value(sh.list[C]));
-  m = block_reduce_max<kSelWaves>(m, sh.redf[0]);
+  m = block_reduce_max<kSelWaves>(m, sh.redf);
   double s = 0.0;
   if (m > -INFINITY) {  // uniform
+    float t = 0.f;
+    auto add = [&](float v, float by) { t += by * __builtin_amdgcn_exp2f(fminf((fmaxf(v, -INFINITY) - m) * c, 0.f)); };
 #pragma unroll
     for (int i = 0; i < kSelRegs; ++i)
-      if (i < nr && gs[i].x > -INFINITY)
-        s += (double)gs[i].y * (double)__builtin_amdgcn_exp2f(fminf((gs[i].x - m) * c, 0.f));
-    float t = 0.f;
-    each([&](float v, uint32_t k, uint32_t id, bool in) {
-      if (in && !(k > et || (k == et && id <= eid)))
-        t += __builtin_amdgcn_exp2f(fminf((fmaxf(v, -INFINITY) - m) * c, 0.f));
+      if (i < nr && gk[i] && !(chosen >> i & 1)) add(order_key_value(gk[i]), gs[i]);
+    s = t;
+    t = 0.f;
+    every_vec([&](const u32x4 &y, uint32_t id) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float v = RowVec<LT>::get(y, e);
+        if (id + e < (uint32_t)V && !ec.has(order_key(v), id + e)) add(v, 1.f);
+      }
     });
+    for (int i = C + tid; i < n; i += kSelThreads) add(entry_value(sh.list[i]), 1.f);
     s += t;
-    for (int i = C + tid; i < n; i += kSelThreads)
-      s += __builtin_amdgcn_exp2f(fminf((entry_value(sh.list[i]) - m) * c, 0.f));
   }
   rest_m = m;
   rest_s = block_reduce_sum<kSelWaves>(s, sh.redd);
@@ -415,8 +411,7 @@ __global__ __launch_bounds__(kSelThreads) void top_select_kernel(RowsArgs a, int
   const float c = row_scale(a.T);
   float rm = 0.f;
   double rs = 0.0;
-  if (rest) select_top<LT, true>(lr, groups, a.V, a.G, k, c, sh, rm, rs);
-  else select_top<LT, false>(lr, groups, a.V, a.G, k, c, sh, rm, rs);
+  select_top<LT>(lr, groups, a.V, a.G, k, c, sh, rm, rs);
   if (tid < k) {
     const unsigned long long key = sh.list[tid];
     ids[(size_t)row * k + tid] = (int32_t)entry_id(key);
@@ -468,61 +463,59 @@ struct SampleRow {
 };
 
 struct SampleShared {
-  unsigned long long mass[kBins];   // of the whole row by bins
-  uint32_t count[kBins];
   union {
-    struct {
+    SelShared sel;
+    struct {                          // a bin of the whole row, by parts
       unsigned long long mass[kSplit];
       uint32_t count[kSplit];
     } part;
-    SelShared sel;
+  };
+  union {
+    unsigned long long run[kTopMax];  // running sums of the first entries
+    struct {                          // the whole row by bins
+      unsigned long long mass[kBins];
+      uint32_t count[kBins];
+    } row;
   };
   unsigned long long redu[2][kSelWaves];
-  unsigned long long hit[4];
-  int hit_i;
+  unsigned long long hit[3];
+  int hit_i, first[4];
 };
-
-// inclusive running sum over the threads of the workgroup
-DEVI unsigned long long block_scan(unsigned long long v, unsigned long long *red) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned long long y = __shfl_up(v, o, 64);
-    if (lane >= o) v += y;
-  }
-  if (lane == 63) red[wave] = v;
-  __syncthreads();
-  unsigned long long base = 0;
-#pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) base += w < wave ? red[w] : 0ull;
-  __syncthreads();
-  return base + v;
-}
+static_assert(sizeof(SampleShared) <= 65536, "two workgroups a CU, static LDS");
 
 // Where a running sum in the order ends: after n entries of together `mass`, the last one `key`.
 struct Prefix {
   unsigned long long n, mass, key;
 };
 
-// f(value, id) for every value of the row, four 16-byte loads in flight a thread
+// f(value, id, is one) for every value of the row; the next 16-byte loads are on their way meanwhile
 template <typename LT, typename F>
 DEVI void each_of_row(const LT *lr, uint32_t V, F f) {
-  constexpr int N = RowVec<LT>::N, U = 4;
-  const uint32_t step = kSelThreads * N;
-  uint32_t v0 = threadIdx.x * N;
-  for (; v0 - threadIdx.x * N + U * step <= V; v0 += U * step) {
-    u32x4 x[U];
+  constexpr int N = RowVec<LT>::N, U = 2;
+  constexpr uint32_t step = kSelThreads * N;
+  u32x4 x[U], y[U];
+  auto load = [&](u32x4 (&z)[U], uint32_t c0) {
+    if (c0 + U * step <= V) {  // uniform
 #pragma unroll
-    for (int q = 0; q < U; ++q) x[q] = row_load(lr + v0 + q * step);
+      for (int q = 0; q < U; ++q) z[q] = row_load(lr + c0 + q * step + threadIdx.x * N);
+    } else {
+#pragma unroll
+      for (int q = 0; q < U; ++q) z[q] = row_load_end(lr, c0 + q * step + threadIdx.x * N, V);
+    }
+  };
+  load(x, 0);
+#pragma unroll 1
+  for (uint32_t c0 = 0; c0 < V; c0 += U * step) {
+    load(y, c0 + U * step);
 #pragma unroll
     for (int q = 0; q < U; ++q)
 #pragma unroll
-      for (int e = 0; e < N; ++e) f(RowVec<LT>::get(x[q], e), v0 + q * step + e, true);
-  }
-  for (; v0 - threadIdx.x * N < V; v0 += step) {
-    const u32x4 x = row_load_end(lr, v0, V);
+      for (int e = 0; e < N; ++e) {
+        const uint32_t id = c0 + q * step + threadIdx.x * N + e;
+        f(RowVec<LT>::get(x[q], e), id, id < V);
+      }
 #pragma unroll
-    for (int e = 0; e < N; ++e) f(RowVec<LT>::get(x, e), v0 + e, v0 + e < V);
+    for (int q = 0; q < U; ++q) x[q] = y[q];
   }
 }
 
@@ -572,8 +565,8 @@ DEVI Prefix find_in_row(const LT *lr, uint32_t V, const SampleRow &s, bool by_co
   Digits at = {0, 0, 0};
   unsigned long long n0 = 0, m0 = 0;  // before the part in work
   for (int level = 0;; ++level) {
-    unsigned long long *mass = level == 0 ? sh.mass : sh.part.mass;
-    uint32_t *count = level == 0 ? sh.count : sh.part.count;
+    unsigned long long *mass = level == 0 ? sh.row.mass : sh.part.mass;
+    uint32_t *count = level == 0 ? sh.row.count : sh.part.count;
     const int bins = level == 0 ? kBins : kSplit;
     if (level > 0) {
       for (int i = tid; i < kSplit; i += kSelThreads) {
@@ -633,7 +626,10 @@ DEVI Prefix find_in_row(const LT *lr, uint32_t V, const SampleRow &s, bool by_co
     each_of_row(lr, V, [&](float v, uint32_t id, bool in) {
       const Digits d = digits_of(s, v, id);
       const bool on = in && d.y < (uint32_t)kBins << 11 && near(d, at, level + 1) && s.weight(order_val(v));
-      push_list(on, entry_key(v, id), sh.sel);
+      if (on) {
+        const int to = atomicAdd(&sh.sel.n, 1);
+        if (to < kListMax) sh.sel.list[to] = entry_key(v, id);
+      }
     });
     __syncthreads();
     const int n = sh.sel.n;
@@ -674,16 +670,17 @@ __global__ __launch_bounds__(kSelThreads) void sample_kernel(RowsArgs a, SampleA
   const LT *lr = (const LT *)a.logits + (size_t)row * a.ld;
   const float2 *groups = a.groups + (size_t)row * a.G;
   // the row's parameters; one out of range leaves the row without a token
-  float T = a.temps ? a.temps[row] : 1.f, u = p.uniforms[row];
-  const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
+  float T = a.temps ? a.temps[row] : 1.f;
+  const float u = p.uniforms[row], top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
   int top_k = p.top_k ? p.top_k[row] : 0;
-  const bool ok = T >= 0.f && T < INFINITY && u >= 0.f && u < 1.f && top_p >= 0.f && top_p <= 1.f && min_p >= 0.f &&
-                  min_p <= 1.f;
-  if (!ok) {
+  auto finish = [&](int token, float logprob) {  // one thread
+    p.tokens[row] = token;
+    if (p.logprobs) p.logprobs[row] = logprob;
+  };
+  if (!(T >= 0.f && T < INFINITY && u >= 0.f && u < 1.f && top_p >= 0.f && top_p <= 1.f && min_p >= 0.f && min_p <= 1.f)) {
     if (tid == 0) {
       raise_error(a.err, DEV_BAD_PARAM);
-      p.tokens[row] = -1;
-      if (p.logprobs) p.logprobs[row] = NAN;
+      finish(-1, NAN);
     }
     return;
   }
@@ -691,109 +688,83 @@ __global__ __launch_bounds__(kSelThreads) void sample_kernel(RowsArgs a, SampleA
     top_k = 1;
     T = 1.f;
   }
-  const bool has_k = top_k > 0 && top_k < a.V;
+  const bool has_k = top_k > 0 && top_k < a.V, use_p = top_p < 1.f, use_m = min_p > 0.f;
   const int C = min(a.V, has_k && top_k <= kTopMax ? top_k : kSampleTop);
   float rm = 0.f;
   double rs = 0.0;
-  select_top<LT, true>(lr, groups, a.V, a.G, C, row_scale(T), sh.sel, rm, rs);
+  select_top<LT>(lr, groups, a.V, a.G, C, row_scale(T), sh.sel, rm, rs);
   SampleRow s;
   s.m = entry_value(sh.sel.list[0]);
   s.cd = 1.44269504088896340736 / (double)T;
   s.cf = fminf((float)(s.cd * (double)(1 << (kBinsLog + 11))), 1e30f);
   if (s.m == -INFINITY) {  // nothing to draw from
-    if (tid == 0) {
-      p.tokens[row] = -1;
-      if (p.logprobs) p.logprobs[row] = -INFINITY;
-    }
+    if (tid == 0) finish(-1, -INFINITY);
     return;
   }
-  // running sums over the first C; entries of no weight end them
+  constexpr double kOne = (double)(1ull << kWeightBits);
+  auto logprob = [&](float v, unsigned long long total) {
+    return (float)((v == s.m ? 0.0 : ((double)v - (double)s.m) / (double)T) - log((double)total / kOne));
+  };
+  // running sums over the first C, and the first of them that ...
   const unsigned long long key = tid < C ? sh.sel.list[tid] : 0ull;
   const float v = tid < C ? entry_value(key) : -INFINITY;
   const unsigned long long w = tid < C ? s.weight(v) : 0ull;
-  __syncthreads();  // (the list's memory is used again below)
+  if (tid < 4) sh.first[tid] = C;
   const unsigned long long run = block_scan(w, sh.redu[0]);
-  auto at_thread = [&](int t) {  // `run` of thread t
-    if (tid == t) sh.hit[3] = run;
-    __syncthreads();
-    const unsigned long long x = sh.hit[3];
-    __syncthreads();
-    return x;
-  };
-  // first thread (< C) whose `on` is set, C if none
-  auto first = [&](bool on) {
-    if (tid == 0) sh.hit_i = C;
-    __syncthreads();
+  if (tid < C) sh.run[tid] = run;
+  auto first = [&](int slot, bool on) {
     const unsigned long long mk = __ballot(on && tid < C);
-    if (mk && (tid & 63) == 0) atomicMin(&sh.hit_i, (tid & ~63) + __ffsll((unsigned long long)mk) - 1);
-    __syncthreads();
-    const int x = sh.hit_i;
-    __syncthreads();
-    return x;
+    if (mk && (tid & 63) == 0) atomicMin(&sh.first[slot], (tid & ~63) + __ffsll(mk) - 1);
   };
-  const unsigned long long sum_c = at_thread(C - 1);
-  const int weighty = first(w == 0ull);          // entries with a weight among the first C
-  const bool all = C == a.V || weighty < C;      // no weight lies behind them
-  // the whole row's sum: of the first C exactly, of the rest from the groups' sums
-  double rest = 0.0;
-  if (!all && rs != 0.0) rest = rs * exp2((rm - (double)s.m) * s.cd) * (double)(1ull << kWeightBits);
-  const bool use_p = top_p < 1.f, use_m = min_p > 0.f;
   const double min_d = use_m ? -log((double)min_p) * (double)T : INFINITY;  // max - l up to this stays
   auto stays = [&](float x) { return x == s.m || (double)s.m - (double)x <= min_d; };
-  const unsigned long long kUnknown = ~0ull;
-  unsigned long long keep = all ? weighty : kUnknown, keep_mass = all ? sum_c : kUnknown;
-  unsigned long long whole = all ? sum_c : (unsigned long long)((double)sum_c + rest);
-  bool decided = true;
-  // prefix of n <= C entries
-  auto shorten = [&](int n) {
+  first(0, w == 0ull);
+  first(1, !stays(v));
+  __syncthreads();
+  const unsigned long long sum_c = sh.run[C - 1], kUnknown = ~0ull;
+  const int weighty = sh.first[0], n_m = sh.first[1];  // C: all of them
+  const bool all = C == a.V || weighty < C;            // no weight lies behind the first C
+  // the whole row's sum: of the first C exactly, of the rest from the groups' sums
+  unsigned long long whole = sum_c;
+  if (!all && rs != 0.0) whole += (unsigned long long)(rs * exp2(((double)rm - (double)s.m) * s.cd) * kOne);
+  unsigned long long keep = all ? weighty : kUnknown, total = all ? sum_c : kUnknown;
+  auto shorten = [&](int n) {  // n in [1, C]
     if ((unsigned long long)n < keep) {
       keep = n;
-      keep_mass = at_thread(n - 1);
+      total = sh.run[n - 1];
     }
   };
+  bool decided = true;
   if (has_k && top_k <= C) {
     shorten(top_k);
-    whole = keep_mass;
+    whole = total;
   }
-  const bool whole_known = !has_k || top_k <= C || all;
   if (use_p) {
-    if (whole_known) {
-      const unsigned long long want = (unsigned long long)ceil((double)top_p * (double)whole);
-      const int n = first(run >= want) + 1;
-      if (n <= C) shorten(n);
-    } else {
-      decided = false;
-    }
+    if (!has_k || top_k <= C || all) first(2, run >= (unsigned long long)ceil((double)top_p * (double)whole));
+    else decided = false;  // the sum of the first top_k is not known
+    __syncthreads();
+    if (sh.first[2] < C) shorten(sh.first[2] + 1);
   }
-  if (use_m) {
-    const int n = first(!stays(v));
-    if (n < C) shorten(n);
-  }
-  // keep unknown: no filter ends within the first C.  Without any, the draw may still fall there.
-  unsigned long long total = keep_mass;
+  if (use_m && n_m < C) shorten(n_m);
+  // no filter ends within the first C: without any, the draw may still fall there
   if (keep == kUnknown) {
     total = whole;
     if (use_p || use_m || has_k) decided = false;
   }
   if (decided) {
-    const unsigned long long target = (unsigned long long)floor((double)u * (double)total);
-    int i = first(run > target);
-    if (keep != kUnknown) i = min(i, (int)keep - 1);
+    first(3, run > (unsigned long long)floor((double)u * (double)total));
+    __syncthreads();
+    const int i = keep == kUnknown ? sh.first[3] : min(sh.first[3], (int)keep - 1);
     if (i < C) {
-      if (tid == i) {
-        p.tokens[row] = (int32_t)entry_id(key);
-        if (p.logprobs)
-          p.logprobs[row] =
-              v == s.m ? (float)-log((double)total / (double)(1ull << kWeightBits))
-                       : (float)(((double)v - (double)s.m) / (double)T - log((double)total / (double)(1ull << kWeightBits)));
-      }
+      if (tid == i) finish((int)entry_id(key), logprob(v, total));
       return;
     }
   }
+  __syncthreads();
   // The whole row.
   for (int i = tid; i < kBins; i += kSelThreads) {
-    sh.mass[i] = 0;
-    sh.count[i] = 0;
+    sh.row.mass[i] = 0;
+    sh.row.count[i] = 0;
   }
   __syncthreads();
   unsigned long long mn = 0, mm = 0;
@@ -803,9 +774,9 @@ __global__ __launch_bounds__(kSelThreads) void sample_kernel(RowsArgs a, SampleA
     if (in && d.y < (uint32_t)kBins << 11) {
       const unsigned long long wx = s.weight(x);
       if (wx) {
-        atomicAdd(&sh.mass[d.y >> 11], wx);
-        atomicAdd(&sh.count[d.y >> 11], 1u);
-        if (stays(x)) {
+        atomicAdd(&sh.row.mass[d.y >> 11], wx);
+        atomicAdd(&sh.row.count[d.y >> 11], 1u);
+        if (use_m && stays(x)) {
           ++mn;
           mm += wx;
         }
@@ -815,42 +786,37 @@ __global__ __launch_bounds__(kSelThreads) void sample_kernel(RowsArgs a, SampleA
   __syncthreads();
   unsigned long long tn = 0, tm = 0;
   for (int i = tid; i < kBins; i += kSelThreads) {
-    tn += sh.count[i];
-    tm += sh.mass[i];
+    tn += sh.row.count[i];
+    tm += sh.row.mass[i];
   }
   keep = block_reduce_sum<kSelWaves>(tn, sh.redu[0]);
-  keep_mass = block_reduce_sum<kSelWaves>(tm, sh.redu[1]);
+  total = block_reduce_sum<kSelWaves>(tm, sh.redu[1]);
   __syncthreads();
   mn = block_reduce_sum<kSelWaves>(mn, sh.redu[0]);
   mm = block_reduce_sum<kSelWaves>(mm, sh.redu[1]);
   __syncthreads();
-  if (has_k && (unsigned long long)top_k < keep) {
-    const Prefix f = find_in_row(lr, a.V, s, true, top_k - 1, sh);
-    keep = f.n;
-    keep_mass = f.mass;
-  }
-  if (use_p) {
-    const unsigned long long want = (unsigned long long)ceil((double)top_p * (double)keep_mass);
-    if (want > 0) {
-      const Prefix f = find_in_row(lr, a.V, s, false, min(want, keep_mass) - 1, sh);
-      if (f.n < keep) {
-        keep = f.n;
-        keep_mass = f.mass;
-      }
+  // top-k, top-p, then (the shorter of it and min-p kept) the draw
+#pragma unroll 1
+  for (int step = 0; step < 3; ++step) {
+    unsigned long long target;
+    if (step == 0) {
+      if (!has_k || (unsigned long long)top_k >= keep) continue;
+      target = top_k - 1;
+    } else if (step == 1) {
+      target = (unsigned long long)ceil((double)top_p * (double)total);
+      if (!use_p) continue;
+      target = target == 0 ? 0 : min(target, total) - 1;
+    } else {
+      if (use_m && mn < keep) total = mm;
+      target = min((unsigned long long)floor((double)u * (double)total), total - 1);
     }
-  }
-  if (use_m && mn < keep) {
-    keep = mn;
-    keep_mass = mm;
-  }
-  const unsigned long long target = min((unsigned long long)floor((double)u * (double)keep_mass), keep_mass - 1);
-  const Prefix f = find_in_row(lr, a.V, s, false, target, sh);
-  if (tid == 0) {
-    const float x = entry_value(f.key);
-    p.tokens[row] = (int32_t)entry_id(f.key);
-    if (p.logprobs)
-      p.logprobs[row] = (float)((x == s.m ? 0.0 : ((double)x - (double)s.m) / (double)T) -
-                                log((double)keep_mass / (double)(1ull << kWeightBits)));
+    const Prefix f = find_in_row(lr, a.V, s, step == 0, target, sh);
+    if (step == 2) {
+      if (tid == 0) finish((int)entry_id(f.key), logprob(entry_value(f.key), total));
+    } else if (f.n < keep) {
+      keep = f.n;
+      total = f.mass;
+    }
   }
 }
 

@@ -47,15 +47,37 @@ template <typename LT>
 DEVI void row_store(LT *p, const u32x4 &x) {
   __builtin_memcpy(p, &x, 16);
 }
-// the vector at v0 of a row of V values, -inf past its end
+// The vector at v0 < V of a row of V values, -inf past its end.  Where it crosses the end the row's
+// last 16 bytes are loaded and moved down, in a few instructions: this code is in many loops.
 template <typename LT>
 DEVI u32x4 row_load_end(const LT *row, uint32_t v0, uint32_t V) {
   constexpr int N = RowVec<LT>::N;
+  constexpr uint32_t kLow = RowVec<LT>::kLow;
   if (v0 + N <= V) return row_load(row + v0);
-  u32x4 x = {RowVec<LT>::kLow, RowVec<LT>::kLow, RowVec<LT>::kLow, RowVec<LT>::kLow};
+  u32x4 x = {kLow, kLow, kLow, kLow};
+  if (v0 >= V) return x;
+  const uint32_t by = v0 + N - V;  // values past the end
+  if (V >= N) {
+    x = row_load(row + (V - N));
+    if (by & (N / 2)) x = u32x4{x[2], x[3], kLow, kLow};
+    if (by & (N / 4)) x = u32x4{x[1], x[2], x[3], kLow};
+    if (N == 8 && (by & 1)) {
 #pragma unroll
-  for (int e = 0; e < N; ++e)
-    if (v0 + e < V) RowVec<LT>::set(x, e, row[v0 + e]);
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_alignbit(e < 3 ? x[e + 1] : kLow, x[e], 16);
+    }
+  } else {  // (v0 = 0, fewer values than a vector has)
+#pragma unroll 1
+    for (uint32_t i = V; i-- > 0;) {
+      const u32x4 y = x;
+      if (N == 8) {
+#pragma unroll
+        for (int e = 3; e >= 0; --e) x[e] = __builtin_amdgcn_alignbit(y[e], e > 0 ? y[e - 1] : 0u, 16);
+      } else {
+        x = u32x4{0, y[0], y[1], y[2]};
+      }
+      RowVec<LT>::set(x, 0, row[i]);
+    }
+  }
   return x;
 }
 
