@@ -1342,7 +1342,7 @@ domino_status domino_top_logits(int32_t rows, int32_t vocab, int32_t k, const vo
 }
 
 size_t domino_sample_logits_workspace_bytes(int32_t rows, int32_t vocab) {
-  return rows_supported(rows, vocab) ? rows_ws_bytes(rows, vocab) : 0;
+  return rows_supported(rows, vocab) ? draw_ws_bytes(rows, vocab) : 0;
 }
 
 domino_status domino_sample_logits(int32_t rows, int32_t vocab, const void *logits, domino_dtype logits_dtype, int64_t ld,
@@ -1353,7 +1353,7 @@ domino_status domino_sample_logits(int32_t rows, int32_t vocab, const void *logi
   if (!uniforms || !tokens) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
   if (!rows_supported(rows, vocab))
     return fail(DOMINO_ERR_UNSUPPORTED, "vocab must be at most %d and rows at most %ld", kRowsMaxVocab, kMaxBlocks / 64);
-  if (domino_status s = check_workspace(workspace, workspace_bytes, rows_ws_bytes(rows, vocab)); s != DOMINO_OK) return s;
+  if (domino_status s = check_workspace(workspace, workspace_bytes, draw_ws_bytes(rows, vocab)); s != DOMINO_OK) return s;
   RowsArgs a = {};
   a.rows = rows;
   a.V = vocab;
@@ -1361,7 +1361,13 @@ domino_status domino_sample_logits(int32_t rows, int32_t vocab, const void *logi
   a.ld = (size_t)ld;
   a.temps = temperature;
   a.T = 1.f;
-  const SampleArgs p = {top_k, top_p, min_p, uniforms, tokens, logprobs};
+  SampleArgs p = {};
+  p.top_k = top_k;
+  p.top_p = top_p;
+  p.min_p = min_p;
+  p.uniforms = uniforms;
+  p.tokens = tokens;
+  p.logprobs = logprobs;
   launch_sample_logits(a, logits_dtype == DOMINO_BF16, p, workspace, (hipStream_t)stream);
   hipError_t he = hipGetLastError();
   if (he != hipSuccess) return fail(DOMINO_ERR_HIP, "sample_logits launch: %s", hipGetErrorString(he));

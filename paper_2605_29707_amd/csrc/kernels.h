@@ -253,7 +253,7 @@ void launch_verify_sample(int bs, int B, int V, const int32_t *node_token, const
                           int32_t *accepted_nodes, int32_t *out_tokens, void *ws, hipStream_t st);
 void launch_philox_words(const uint32_t *ctr, uint64_t key, uint32_t *out, int n, hipStream_t st);
 
-// ---- rows of logits: top entries and filtered sampling (logits.hip)
+// ---- rows of logits: their groups and top entries (logits.hip)
 constexpr int kRowsMaxVocab = 327680;  // ten groups of 32 ids in the registers of each of 1024 threads
 struct RowsArgs {
   int rows, V;
@@ -266,16 +266,30 @@ struct RowsArgs {
   float2 *groups;      // [rows][G]: (max, sum of exp) of every 32 ids
   int G, nch;          // workgroups a row of the first launch
 };
+size_t rows_ws_bytes(int rows, int V);
+RowsArgs launch_row_groups(RowsArgs a, bool bf16, void *ws, hipStream_t st);  // a with its workspace set
+void launch_top_logits(RowsArgs a, bool bf16, int k, int32_t *ids, float *vals, float *rest, void *ws, hipStream_t st);
+
+// ---- filtered sampling (draw.hip)
+struct DrawSums {  // of one row, over its workgroups: whole numbers, so their order does not matter
+  unsigned long long mass[2944];
+  uint32_t count[2944];
+  unsigned long long stays;
+  uint32_t done, pad;
+};
 struct SampleArgs {
   const int32_t *top_k;  // optional [rows] each
   const float *top_p, *min_p;
   const float *uniforms;  // [rows]
   int32_t *tokens;
   float *logprobs;       // optional
+  // set at launch, from the workspace
+  uint32_t *state;       // [rows]: 0, or the key of the maximum of a row that the first entries do not decide
+  DrawSums *sums;        // [rows]
+  int slices;            // workgroups a row of the last launch
 };
-size_t rows_ws_bytes(int rows, int V);
-void launch_top_logits(RowsArgs a, bool bf16, int k, int32_t *ids, float *vals, float *rest, void *ws, hipStream_t st);
-void launch_sample_logits(RowsArgs a, bool bf16, const SampleArgs &p, void *ws, hipStream_t st);
+size_t draw_ws_bytes(int rows, int V);
+void launch_sample_logits(RowsArgs a, bool bf16, SampleArgs p, void *ws, hipStream_t st);
 
 // ---- distillation from a teacher's top entries (distill.hip)
 struct DistillArgs {
