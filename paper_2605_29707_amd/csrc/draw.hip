@@ -36,24 +36,22 @@ constexpr int kWholeThreads = 1024;
 constexpr int kWholeWaves = kWholeThreads / 64;
 constexpr double kOne = (double)(1ull << kWeightBits);
 
-// round(2^44 2^-x), x >= 0.  2^f on [-1/2, 1/2] by its Taylor sum to the 11th power, whose next
-// term is 2^-50; the rest is exact or rounded to 53 bits.
+// round(2^44 2^-x) for 0 <= x < 2^10.  2^f on [-1/2, 1/2] as 1 + f q(f), q interpolating (2^f - 1) / f at the
+// zeros of the Chebyshev polynomial of degree 8: 2^-38.8 of the value off at most, and exactly 1 at 0.
+// The whole part of x is rounded off by adding 1.5 2^52, which leaves it in the low word.
 DEVI unsigned long long weight_of(double x) {
-  if (!(x < kWeightBits + 1.5)) return 0ull;
-  const double n = rint(x), t = (n - x) * 0.69314718055994530942;
-  double p = 1.0 / 39916800.0;
-  p = fma(p, t, 1.0 / 3628800.0);
-  p = fma(p, t, 1.0 / 362880.0);
-  p = fma(p, t, 1.0 / 40320.0);
-  p = fma(p, t, 1.0 / 5040.0);
-  p = fma(p, t, 1.0 / 720.0);
-  p = fma(p, t, 1.0 / 120.0);
-  p = fma(p, t, 1.0 / 24.0);
-  p = fma(p, t, 1.0 / 6.0);
-  p = fma(p, t, 0.5);
-  p = fma(p, t, 1.0);
-  p = fma(p, t, 1.0);
-  const double scale = __longlong_as_double((unsigned long long)(1023 + kWeightBits - (int)n) << 52);
+  const double big = 6755399441055744.0, r = x + big, f = (r - big) - x;
+  const int n = (int)(uint32_t)__double_as_longlong(r);
+  double p = 1.325080551750225e-06;
+  p = fma(p, f, 1.5303700711365693e-05);
+  p = fma(p, f, 0.00015403475186530786);
+  p = fma(p, f, 0.0013333478473685416);
+  p = fma(p, f, 0.00961812913523614);
+  p = fma(p, f, 0.055504109063258665);
+  p = fma(p, f, 0.24022650695888503);
+  p = fma(p, f, 0.6931471805568324);
+  p = fma(p, f, 1.0);
+  const double scale = __hiloint2double((1023 + kWeightBits - n) << 20, 0);
   // adding 2^52 rounds to a whole number in the low bits
   return (unsigned long long)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & ((1ull << 52) - 1);
 }
@@ -92,8 +90,11 @@ struct DrawRow {
   // of a value that is no NaN; logits of +inf have all the weight
   DEVI unsigned long long weight(float v) const {
     if (m == INFINITY) return v == m ? 1ull << kWeightBits : 0ull;
-    return weight_of(((double)m - (double)v) * cd);
+    const double x = ((double)m - (double)v) * cd;
+    return x < kWeightBits + 2 ? weight_of(x) : 0ull;
   }
+  // above every weight of a bin
+  DEVI unsigned long long weight_at(int bin) const { return weight_of((double)bin / (1 << kBinsLog)) + (1ull << (kWeightBits - 20)); }
   DEVI bool stays(float v) const { return v == m || (double)m - (double)v <= min_d; }
   DEVI float logprob(float v, unsigned long long total) const {
     return (float)((v == m ? 0.0 : ((double)v - (double)m) / (double)T) - log((double)total / kOne));
@@ -202,11 +203,10 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
       return;
     }
   }
-  // for the next launch: the row's maximum, and its sums cleared
-  if (tid == 0) p.state[row] = order_key(d.m);
-  if (p.slices > 1) {
-    uint32_t *g = (uint32_t *)(p.sums + row);
-    for (int i = tid; i < (int)(sizeof(DrawSums) / 4); i += kSelThreads) g[i] = 0;
+  // for the next launch
+  if (tid == 0) {
+    p.state[row] = order_key(d.m);
+    p.done[row] = 0;
   }
 }
 
@@ -214,23 +214,29 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
 // the whole row
 // ---------------------------------------------------------------------------
 struct WholeShared {
+  unsigned long long mass[kBins];  // the row by bins
   union {
-    alignas(16) unsigned long long list[kListMax + 2];
-    struct {                     // a bin by parts
+    struct {
+      alignas(16) unsigned long long list[kListMax + 2];
+      union {
+        alignas(16) unsigned long long draw[kListMax + 2];  // a second list, of the draw's bin
+        uint32_t count[kBins];                              // (for top-k, which comes before the draw)
+      };
+    };
+    struct {                       // a bin by parts
       unsigned long long mass[kSplit];
       uint32_t count[kSplit];
     } part;
   };
-  unsigned long long mass[kBins];  // the row by bins
-  uint32_t count[kBins];           // (where top-k is on)
   unsigned long long redu[2][kWholeWaves];
-  unsigned long long hit[3];
-  int hit_i, n, last;
+  unsigned long long hit[2];
+  int hit_i, last, n[2], wave_n[2][kWholeWaves];
 };
 static_assert(sizeof(WholeShared) <= 65536, "two workgroups a CU, static LDS");
+constexpr int kBinsPer = (kBins + kWholeThreads - 1) / kWholeThreads;  // bins a thread
+constexpr int kSeg = kListMax / kWholeWaves;                          // a wave's part of a list while it is collected
 
 // f(value, id) for the values of ids [v0, v1); the next 16-byte loads are on their way meanwhile.
-// NaN comes as -inf.
 template <typename LT, typename F>
 DEVI void each_of_row(const LT *lr, uint32_t V, uint32_t v0, uint32_t v1, F f) {
   constexpr int N = RowVec<LT>::N, U = 2;
@@ -254,7 +260,7 @@ DEVI void each_of_row(const LT *lr, uint32_t V, uint32_t v0, uint32_t v1, F f) {
       const uint32_t id = c0 + q * step + threadIdx.x * N;
       if (id < v1) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) f(fmaxf(RowVec<LT>::get(x[q], e), -INFINITY), id + e);
+        for (int e = 0; e < N; ++e) f(RowVec<LT>::get(x[q], e), id + e);
       }
     }
 #pragma unroll
@@ -267,9 +273,12 @@ DEVI void each_of_row(const LT *lr, uint32_t V, uint32_t v0, uint32_t v1, F f) {
 struct Digits {
   uint32_t y, k, id;
 };
-// the distance in parts of a bin, not above what 24 bits hold (max = +inf: NaN for its equals, which are at 0)
-DEVI float distance(const DrawRow &s, float v) { return fminf(fmaxf((s.m - v) * s.cf, 0.f), 1.6e7f); }
 constexpr float kFar = (float)(kBins << kSplitLog);
+// the distance in parts of a bin; NaN and -inf are far.  INF: the maximum is +inf
+template <bool INF>
+DEVI float distance(const DrawRow &s, float v) {
+  return INF ? (v == INFINITY ? 0.f : kFar) : (s.m - v) * s.cf;
+}
 DEVI bool near(const Digits &a, const Digits &b, int level) {
   const uint32_t my = level == 0 ? 0u : level == 1 ? ~2047u : ~0u;
   const uint32_t mk = level < 3 ? 0u : level == 3 ? ~0u << 21 : level == 4 ? ~0u << 10 : ~0u;
@@ -298,217 +307,359 @@ DEVI void set_digit(Digits &a, int level, uint32_t d) {
   }
 }
 
+// Bounds of the values whose distance is in [from, to) parts, a little wider: the distance is off by
+// 2^-23 of itself, less than a part.
+struct Between {
+  float lo, hi;
+  template <bool INF>
+  DEVI static Between of(const DrawRow &s, uint32_t from, uint32_t to) {
+    if (INF) return {INFINITY, INFINITY};
+    const double top = (double)s.m - ((double)from - 2.0) / (double)s.cf, end = (double)s.m - ((double)to + 2.0) / (double)s.cf;
+    return {(float)(end - fabs(end) * 0x1p-22), (float)(top + fabs(top) * 0x1p-22)};
+  }
+  DEVI bool has(float v) const { return v >= lo && v <= hi; }
+};
+// f(value, its digits) of the entries whose distance is in [from, to) parts
+template <typename LT, bool INF, typename F>
+DEVI void each_between(const LT *lr, uint32_t V, const DrawRow &s, uint32_t from, uint32_t to, F f) {
+  const Between near_by = Between::of<INF>(s, from, to);
+  each_of_row(lr, V, 0, V, [&](float v, uint32_t id) {
+    if (near_by.has(v)) {
+      const float y = distance<INF>(s, v);
+      if (y >= (float)from && y < (float)to) f(v, Digits{(uint32_t)y, ~order_key(v), id});
+    }
+  });
+}
+// Collects the values between the bounds of A in sh.list, and (TWO) of B in sh.draw, by waves: each has a
+// part of its own, so that no lane waits for a place.  false if one does not hold them.
+template <typename LT, bool TWO>
+DEVI bool collect(const LT *lr, uint32_t V, const Between &A, const Between &B, WholeShared &sh) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int na = 0, nb = 0;
+  each_of_row(lr, V, 0, V, [&](float v, uint32_t id) {
+    auto put = [&](bool on, unsigned long long *list, int &n) {
+      const unsigned long long mk = __ballot(on);
+      if (on) {
+        const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mk >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mk, 0));
+        if (at < kSeg) list[wave * kSeg + at] = (unsigned long long)__float_as_uint(v) << 32 | id;
+      }
+      n += __popcll(mk);
+    };
+    put(A.has(v), sh.list, na);
+    if (TWO) put(B.has(v), sh.draw, nb);
+  });
+  if (lane == 0) {
+    sh.wave_n[0][wave] = na;
+    sh.wave_n[1][wave] = nb;
+  }
+  __syncthreads();
+  bool ok = true;
+  for (int w = 0; w < kWholeWaves; ++w) ok = ok && sh.wave_n[0][w] <= kSeg && sh.wave_n[1][w] <= kSeg;
+  return ok;
+}
+// The entries of a collected list that `on` takes (by digits) and that have a weight, as keys in descending order; their number.
+template <bool INF, typename On>
+DEVI int pack_list(const DrawRow &s, unsigned long long *list, const int *wave_n, WholeShared &sh, int slot, On on) {
+  constexpr int kTwo = kListMax / kWholeThreads;
+  const int tid = threadIdx.x;
+  unsigned long long k[kTwo];
+#pragma unroll
+  for (int j = 0; j < kTwo; ++j) {
+    const int i = j * kWholeThreads + tid;
+    k[j] = 0;
+    if (i % kSeg < wave_n[i / kSeg]) {
+      const unsigned long long x = list[i];
+      const float v = __uint_as_float((uint32_t)(x >> 32)), y = distance<INF>(s, v);
+      if (y < kFar && on(Digits{(uint32_t)y, ~order_key(v), (uint32_t)x}) && s.weight(v)) k[j] = entry_key(v, (uint32_t)x);
+    }
+  }
+  if (tid == 0) sh.n[slot] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kTwo; ++j)
+    if (k[j]) list[atomicAdd(&sh.n[slot], 1)] = k[j];
+  __syncthreads();
+  const int n = sh.n[slot];
+  sort_list<kWholeWaves>(n, list);
+  return n;
+}
+
 // Where a running sum in the order ends: the sum and the last entry.
 struct Prefix {
   unsigned long long mass, key;
 };
 
-// The shortest prefix of the whole row's order whose count (by_count) or sum is above `target`; one exists.
-template <typename LT>
-DEVI Prefix find_in_row(const LT *lr, uint32_t V, const DrawRow &s, bool by_count, unsigned long long target,
+// Where the running sum of a sorted list (or its count, from n0) that starts at m0 passes `target`; it does.
+DEVI Prefix pass_in_list(const DrawRow &s, const unsigned long long *list, int n, bool by_count, unsigned long long target,
+                         unsigned long long m0, unsigned long long n0, WholeShared &sh) {
+  constexpr int kTwo = kListMax / kWholeThreads;
+  const int tid = threadIdx.x;
+  unsigned long long w[kTwo], ws = 0;
+#pragma unroll
+  for (int j = 0; j < kTwo; ++j) {
+    const int i = tid * kTwo + j;
+    w[j] = i < n ? s.weight(entry_value(list[i])) : 0ull;
+    ws += w[j];
+  }
+  unsigned long long e = block_scan<kWholeWaves>(ws, sh.redu[0]) - ws + m0;
+#pragma unroll
+  for (int j = 0; j < kTwo; ++j) {
+    const int i = tid * kTwo + j;
+    if (i < n) {
+      const unsigned long long a0 = by_count ? n0 + i : e, a1 = by_count ? a0 + 1 : e + w[j];
+      if (a0 <= target && target < a1) {
+        sh.hit[0] = e + w[j];
+        sh.hit[1] = list[i];
+      }
+      e += w[j];
+    }
+  }
+  __syncthreads();
+  const Prefix p = {sh.hit[0], sh.hit[1]};
+  __syncthreads();
+  return p;
+}
+
+// The bin (or part of one) in which a running sum passes a target, and the sum and count before it.
+struct Bin {
+  int i;
+  unsigned long long m0, n0;
+};
+DEVI Bin pass_in_bins(const unsigned long long *mass, const uint32_t *count, int bins, bool by_count, unsigned long long target,
+                      unsigned long long em, unsigned long long en, WholeShared &sh) {
+#pragma unroll
+  for (int j = 0; j < kBinsPer; ++j) {
+    const int b = threadIdx.x * kBinsPer + j;
+    if (b < bins) {
+      const unsigned long long mb = mass[b], a0 = by_count ? en : em, a1 = a0 + (by_count ? count[b] : mb);
+      if (a0 <= target && target < a1) {  // one bin of all
+        sh.hit[0] = en;
+        sh.hit[1] = em;
+        sh.hit_i = b;
+      }
+      em += mb;
+      if (by_count) en += count[b];
+    }
+  }
+  __syncthreads();
+  const Bin r = {sh.hit_i, sh.hit[1], sh.hit[0]};
+  __syncthreads();
+  return r;
+}
+
+// The shortest prefix of the whole row's order whose count (by_count) or sum is above `target`, which
+// is passed in `bin`: its entries, or, while they are too many for the list, those of a part of it.
+template <typename LT, bool INF>
+DEVI Prefix find_in_row(const LT *lr, uint32_t V, const DrawRow &s, bool by_count, unsigned long long target, Bin bin,
                         WholeShared &sh) {
   const int tid = threadIdx.x;
   Digits at = {0, 0, 0};
-  unsigned long long n0 = 0, m0 = 0;  // before the part in work
-  // f(value, its digits) of the entries with a weight that agree with `at` before `level`
-  auto each_near = [&](int level, auto f) {
-    const float from = (float)at.y, to = (float)(at.y + (level == 1 ? kSplit : 1));
-    each_of_row(lr, V, 0, V, [&](float v, uint32_t id) {
-      const float y = distance(s, v);
-      if (y >= from && y < to) {
-        const Digits d = {(uint32_t)y, ~order_key(v), id};
-        if (near(d, at, level)) f(v, d);
-      }
-    });
-  };
   for (int level = 0;; ++level) {
-    unsigned long long *mass = level == 0 ? sh.mass : sh.part.mass;
-    uint32_t *count = level == 0 ? sh.count : sh.part.count;
-    const int bins = level == 0 ? kBins : kSplit;
-    if (level > 0) {
-      for (int i = tid; i < kSplit; i += kWholeThreads) {
-        mass[i] = 0;
-        count[i] = 0;
-      }
+    set_digit(at, level, bin.i);
+    const uint32_t from = at.y, to = at.y + (level == 0 ? kSplit : 1);
+    if (collect<LT, false>(lr, V, Between::of<INF>(s, from, to), {}, sh)) {
+      const int n = pack_list<INF>(s, sh.list, sh.wave_n[0], sh, 0, [&](const Digits &d) { return near(d, at, level + 1); });
+      return pass_in_list(s, sh.list, n, by_count, target, bin.m0, bin.n0, sh);
+    }
+    if (level >= 2) {
+      // (the bounds take neighbours too: the entries themselves may be few)
       __syncthreads();
-      each_near(level, [&](float v, const Digits &d) {
-        const unsigned long long w = s.weight(v);
-        if (w) {
-          atomicAdd(&mass[digit_of(d, level)], w);
-          atomicAdd(&count[digit_of(d, level)], 1u);
+      if (tid == 0) sh.n[0] = 0;
+      __syncthreads();
+      each_between<LT, INF>(lr, V, s, from, to, [&](float v, const Digits &d) {
+        if (near(d, at, level + 1) && s.weight(v)) {
+          const int i = atomicAdd(&sh.n[0], 1);
+          if (i < kListMax) sh.list[i] = entry_key(v, d.id);
         }
       });
       __syncthreads();
-    }
-    // the digit in which the target is passed: kPer of them a thread
-    constexpr int kPer = (kBins + kWholeThreads - 1) / kWholeThreads;
-    unsigned long long pm = 0, pn = 0;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int b = tid * kPer + j;
-      if (b < bins) {
-        pm += mass[b];
-        if (by_count) pn += count[b];
+      const int n = sh.n[0];
+      if (n <= kListMax) {  // (at the last level a part is one entry)
+        sort_list<kWholeWaves>(n, sh.list);
+        return pass_in_list(s, sh.list, n, by_count, target, bin.m0, bin.n0, sh);
       }
     }
-    unsigned long long em = block_scan<kWholeWaves>(pm, sh.redu[0]) - pm + m0, en = n0;
-    if (by_count) en += block_scan<kWholeWaves>(pn, sh.redu[1]) - pn;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int b = tid * kPer + j;
-      if (b < bins) {
-        const unsigned long long a0 = by_count ? en : em, a1 = a0 + (by_count ? count[b] : mass[b]);
-        if (a0 <= target && target < a1) {  // one bin of all
-          sh.hit[0] = en;
-          sh.hit[1] = em;
-          sh.hit_i = b;
+    __syncthreads();
+    for (int i = tid; i < kSplit; i += kWholeThreads) {
+      sh.part.mass[i] = 0;
+      sh.part.count[i] = 0;
+    }
+    __syncthreads();
+    each_between<LT, INF>(lr, V, s, from, to, [&](float v, const Digits &d) {
+      if (near(d, at, level + 1)) {
+        const unsigned long long w = s.weight(v);
+        if (w) {
+          atomicAdd(&sh.part.mass[digit_of(d, level + 1)], w);
+          atomicAdd(&sh.part.count[digit_of(d, level + 1)], 1u);
         }
-        em += mass[b];
-        if (by_count) en += count[b];
-      }
-    }
-    if (tid == 0) sh.n = 0;
-    __syncthreads();
-    n0 = sh.hit[0];
-    m0 = sh.hit[1];
-    set_digit(at, level, sh.hit_i);
-    __syncthreads();
-    // its entries, sorted, with their running sums
-    each_near(level + 1, [&](float v, const Digits &d) {
-      if (s.weight(v)) {
-        const int to = atomicAdd(&sh.n, 1);
-        if (to < kListMax) sh.list[to] = entry_key(v, d.id);
       }
     });
     __syncthreads();
-    const int n = sh.n;
-    if (n > kListMax) continue;  // (at the last level a part is one entry)
-    sort_list<kWholeWaves>(n, sh.list);
-    constexpr int kTwo = kListMax / kWholeThreads;
-    unsigned long long w[kTwo], ws = 0;
-#pragma unroll
-    for (int j = 0; j < kTwo; ++j) {
-      const int i = tid * kTwo + j;
-      w[j] = i < n ? s.weight(entry_value(sh.list[i])) : 0ull;
-      ws += w[j];
+    unsigned long long pm = 0, pn = 0;
+    for (int b = tid * kBinsPer; b < min((tid + 1) * kBinsPer, kSplit); ++b) {
+      pm += sh.part.mass[b];
+      pn += sh.part.count[b];
     }
-    unsigned long long e = block_scan<kWholeWaves>(ws, sh.redu[0]) - ws + m0;
-#pragma unroll
-    for (int j = 0; j < kTwo; ++j) {
-      const int i = tid * kTwo + j;
-      if (i < n) {
-        const unsigned long long a0 = by_count ? n0 + i : e, a1 = by_count ? a0 + 1 : e + w[j];
-        if (a0 <= target && target < a1) {
-          sh.hit[0] = e + w[j];
-          sh.hit[1] = sh.list[i];
-        }
-        e += w[j];
-      }
-    }
-    __syncthreads();
-    const Prefix p = {sh.hit[0], sh.hit[1]};
-    __syncthreads();
-    return p;
+    const unsigned long long em = bin.m0 + block_scan<kWholeWaves>(pm, sh.redu[0]) - pm;
+    const unsigned long long en = bin.n0 + block_scan<kWholeWaves>(pn, sh.redu[1]) - pn;
+    bin = pass_in_bins(sh.part.mass, sh.part.count, kSplit, by_count, target, em, en, sh);
   }
 }
 
-template <typename LT>
-__global__ __launch_bounds__(kWholeThreads) void draw_whole_kernel(RowsArgs a, SampleArgs p) {
-  __shared__ WholeShared sh;
+template <typename LT, bool INF>
+DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, int row, int slice, WholeShared &sh) {
   constexpr int N = RowVec<LT>::N;
-  const int row = blockIdx.x / p.slices, slice = blockIdx.x % p.slices, tid = threadIdx.x;
-  const uint32_t state = p.state[row];
-  if (state == 0) return;  // the first entries have decided
+  const int tid = threadIdx.x;
   const LT *lr = (const LT *)a.logits + (size_t)row * a.ld;
-  DrawRow d;
-  d.read(a, p, row);
-  d.set_max(order_key_value(state));
   for (int i = tid; i < kBins; i += kWholeThreads) {
     sh.mass[i] = 0;
     sh.count[i] = 0;
   }
   __syncthreads();
-  unsigned long long mm = 0;  // the sum that stays under min-p
   const uint32_t len = ((uint32_t)a.V / p.slices / N + 1) * N, v0 = slice * len, v1 = min((uint32_t)a.V, v0 + len);
-  if (v0 < v1)
+  auto add = [&](auto counted) {
     each_of_row(lr, a.V, v0, v1, [&](float x, uint32_t) {
-      const float y = distance(d, x);
+      const float y = distance<INF>(d, x);
       if (y < kFar) {
-        const unsigned long long w = d.weight(x);
-        if (w) {
-          const int b = (int)y >> kSplitLog;
+        const int b = (int)y >> kSplitLog;
+        const unsigned long long w = INF ? 1ull << kWeightBits : weight_of(((double)d.m - (double)x) * d.cd);
+        if constexpr (decltype(counted)::value) {
+          if (w) {
+            atomicAdd(&sh.mass[b], w);
+            atomicAdd(&sh.count[b], 1u);
+          }
+        } else {
           atomicAdd(&sh.mass[b], w);
-          if (d.has_k) atomicAdd(&sh.count[b], 1u);
-          if (d.use_m && d.stays(x)) mm += w;
         }
       }
     });
+  };
+  if (v0 < v1) {
+    if (d.has_k) add(std::true_type{});
+    else add(std::false_type{});
+  }
   __syncthreads();
-  mm = block_reduce_sum<kWholeWaves>(mm, sh.redu[0]);
   if (p.slices > 1) {
-    // to memory; the last workgroup to add its own takes all of them up again
-    DrawSums *g = p.sums + row;
+    // To memory; the last workgroup of the row adds them all up.  Stores and loads are device-scope ones,
+    // complete when the count of the storing thread's drains: 64 rows at once took 17 to 37 us by
+    // 64-bit atomics into one place, and as long by plain stores between fences, which write back and
+    // drop the whole cache of an XCD.
+    DrawSums *g = p.sums + (size_t)row * p.slices;
     for (int i = tid; i < kBins; i += kWholeThreads) {
-      if (sh.mass[i]) atomicAdd(&g->mass[i], sh.mass[i]);
-      if (d.has_k && sh.count[i]) atomicAdd(&g->count[i], sh.count[i]);
+      __hip_atomic_store(&g[slice].mass[i], sh.mass[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (d.has_k) __hip_atomic_store(&g[slice].count[i], sh.count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    if (tid == 0 && mm) atomicAdd(&g->stays, mm);
-    __threadfence();
+    __builtin_amdgcn_s_waitcnt(0);  // this thread's sums are there
     __syncthreads();
-    if (tid == 0) sh.last = atomicAdd(&g->done, 1u) == (unsigned)p.slices - 1;
+    if (tid == 0)
+      sh.last = __hip_atomic_fetch_add(&p.done[row], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)p.slices - 1;
     __syncthreads();
     if (!sh.last) return;
-    __threadfence();
     for (int i = tid; i < kBins; i += kWholeThreads) {
-      sh.mass[i] = __hip_atomic_load(&g->mass[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (d.has_k) sh.count[i] = __hip_atomic_load(&g->count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      unsigned long long m = 0;
+      uint32_t n = 0;
+#pragma unroll 4
+      for (int q = 0; q < p.slices; ++q) m += __hip_atomic_load(&g[q].mass[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (d.has_k)
+        for (int q = 0; q < p.slices; ++q) n += __hip_atomic_load(&g[q].count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      sh.mass[i] = m;
+      sh.count[i] = n;
     }
-    mm = __hip_atomic_load(&g->stays, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
   }
-  unsigned long long tn = 0, tm = 0;
-  for (int i = tid; i < kBins; i += kWholeThreads) {
-    tn += sh.count[i];
-    tm += sh.mass[i];
+  // what lies before each thread's bins, and in all of them
+  unsigned long long pm = 0, pn = 0;
+  for (int b = tid * kBinsPer; b < min((tid + 1) * kBinsPer, kBins); ++b) {
+    pm += sh.mass[b];
+    pn += sh.count[b];
   }
-  const unsigned long long entries = block_reduce_sum<kWholeWaves>(tn, sh.redu[1]);
-  unsigned long long total = block_reduce_sum<kWholeWaves>(tm, sh.redu[0]);
+  const unsigned long long em = block_scan<kWholeWaves>(pm, sh.redu[0]), en = block_scan<kWholeWaves>(pn, sh.redu[1]);
+  if (tid == kWholeThreads - 1) {
+    sh.hit[0] = en;
+    sh.hit[1] = em;
+  }
   __syncthreads();
-  // top-k, top-p, then (the shorter of it and min-p kept) the draw
-#pragma unroll 1
-  for (int step = 0; step < 3; ++step) {
-    unsigned long long target;
-    if (step == 0) {
-      if (!d.has_k || (unsigned long long)d.top_k >= entries) continue;
-      target = d.top_k - 1;
-    } else if (step == 1) {
-      if (!d.use_p) continue;
-      target = (unsigned long long)ceil((double)d.top_p * (double)total);
-      target = target == 0 ? 0 : min(target, total) - 1;
-    } else {
-      if (d.use_m) total = min(total, mm);
-      target = min((unsigned long long)floor((double)d.u * (double)total), total - 1);
-    }
-    const Prefix f = find_in_row(lr, a.V, d, step == 0, target, sh);
-    if (step < 2) total = f.mass;
-    else if (tid == 0) d.finish(p, row, (int)entry_id(f.key), d.logprob(entry_value(f.key), total));
+  const unsigned long long entries = sh.hit[0];
+  unsigned long long total = sh.hit[1];
+  __syncthreads();
+  auto bin_of = [&](bool by_count, unsigned long long target) {
+    return pass_in_bins(sh.mass, sh.count, kBins, by_count, target, em - pm, en - pn, sh);
+  };
+  auto done = [&](const Prefix &f) {
+    if (tid == 0) d.finish(p, row, (int)entry_id(f.key), d.logprob(entry_value(f.key), total));
+  };
+  auto drawn = [&](unsigned long long sum) { return min((unsigned long long)floor((double)d.u * (double)sum), sum - 1); };
+  if (d.has_k && (unsigned long long)d.top_k < entries) {
+    const unsigned long long target = d.top_k - 1;
+    total = find_in_row<LT, INF>(lr, a.V, d, true, target, bin_of(true, target), sh).mass;
   }
+  if (d.use_p) {
+    const unsigned long long want = (unsigned long long)ceil((double)d.top_p * (double)total);
+    const unsigned long long target = want == 0 ? 0 : min(want, total) - 1;
+    const Bin bin = bin_of(false, target);
+    // The kept sum is target + 1 at least, and less than the weight of the bin's first part above it: where
+    // the draw falls into one bin in both cases, one pass collects both bins.
+    const unsigned long long most = min(total, target + 1 + d.weight_at(bin.i));
+    const Bin first = bin_of(false, drawn(target + 1)), last = bin_of(false, drawn(most));
+    if (!d.use_m && first.i == last.i) {
+      const uint32_t fa = (uint32_t)bin.i << kSplitLog, fb = (uint32_t)first.i << kSplitLog;
+      if (collect<LT, true>(lr, a.V, Between::of<INF>(d, fa, fa + kSplit), Between::of<INF>(d, fb, fb + kSplit), sh)) {
+        const int n = pack_list<INF>(d, sh.list, sh.wave_n[0], sh, 0, [&](const Digits &x) { return x.y >> kSplitLog == (uint32_t)bin.i; });
+        const int k = pack_list<INF>(d, sh.draw, sh.wave_n[1], sh, 1, [&](const Digits &x) { return x.y >> kSplitLog == (uint32_t)first.i; });
+        total = pass_in_list(d, sh.list, n, false, target, bin.m0, bin.n0, sh).mass;
+        done(pass_in_list(d, sh.draw, k, false, drawn(total), first.m0, first.n0, sh));
+        return;
+      }
+      __syncthreads();
+    }
+    total = find_in_row<LT, INF>(lr, a.V, d, false, target, bin, sh).mass;
+  }
+  if (d.use_m) {
+    // the sum that stays under min-p: whole bins, and of the bins around the border the entries that stay
+    const double border = d.min_d * (double)d.cf / kSplit;
+    const int b0 = INF ? 0 : (int)fmin(fmax(border - 1.0, 0.0), (double)kBins), b1 = INF ? 1 : min(b0 + 3, kBins);
+    unsigned long long mm = 0;
+    for (int b = tid; b < b0; b += kWholeThreads) mm += sh.mass[b];
+    if (b0 < kBins)
+      each_between<LT, INF>(lr, a.V, d, b0 << kSplitLog, b1 << kSplitLog, [&](float v, const Digits &) {
+        if (d.stays(v)) mm += d.weight(v);
+      });
+    total = min(total, block_reduce_sum<kWholeWaves>(mm, sh.redu[0]));
+    __syncthreads();
+  }
+  const unsigned long long target = drawn(total);
+  done(find_in_row<LT, INF>(lr, a.V, d, false, target, bin_of(false, target), sh));
+}
+
+template <typename LT>
+__global__ __launch_bounds__(kWholeThreads) void draw_whole_kernel(RowsArgs a, SampleArgs p) {
+  __shared__ WholeShared sh;
+  const int row = blockIdx.x / p.slices, slice = blockIdx.x % p.slices;
+  const uint32_t state = p.state[row];
+  if (state == 0) return;  // the first entries have decided
+  DrawRow d;
+  d.read(a, p, row);
+  d.set_max(order_key_value(state));
+  if (d.m == INFINITY) draw_whole<LT, true>(a, p, d, row, slice, sh);
+  else draw_whole<LT, false>(a, p, d, row, slice, sh);
 }
 
 // Workgroups a row of the last launch: for few rows as many as cut a row of 128K ids to 8K each (64
 // rows of 128256 fp32 logits, the flat ones 120 us with one workgroup), for many enough to fill the chip.
 static int draw_slices(int rows, int V) { return std::max(1, std::min({16, 1024 / rows, V / 8192})); }
 
-// [error word and groups][state][sums, where a row has several workgroups]
+// [error word and groups][state, workgroups done: per row][sums, where a row has several workgroups]
 struct DrawLayout {
-  size_t state, sums, bytes;
+  size_t state, done, sums, bytes;
 };
 static DrawLayout draw_layout(int rows, int V) {
   DrawLayout l;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const int slices = draw_slices(rows, V);
   l.state = up(rows_ws_bytes(rows, V));
-  l.sums = up(l.state + (size_t)rows * 4);
-  l.bytes = l.sums + (draw_slices(rows, V) > 1 ? (size_t)rows * sizeof(DrawSums) : 0);
+  l.done = l.state + (size_t)rows * 4;
+  l.sums = up(l.done + (size_t)rows * 4);
+  l.bytes = l.sums + (slices > 1 ? (size_t)rows * slices * sizeof(DrawSums) : 0);
   return l;
 }
 size_t draw_ws_bytes(int rows, int V) { return draw_layout(rows, V).bytes; }
@@ -516,6 +667,7 @@ size_t draw_ws_bytes(int rows, int V) { return draw_layout(rows, V).bytes; }
 void launch_sample_logits(RowsArgs a, bool bf16, SampleArgs p, void *ws, hipStream_t st) {
   const DrawLayout l = draw_layout(a.rows, a.V);
   p.state = (uint32_t *)((char *)ws + l.state);
+  p.done = (uint32_t *)((char *)ws + l.done);
   p.sums = (DrawSums *)((char *)ws + l.sums);
   p.slices = draw_slices(a.rows, a.V);
   a = launch_row_groups(a, bf16, ws, st);

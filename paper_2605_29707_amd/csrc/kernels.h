@@ -271,11 +271,9 @@ RowsArgs launch_row_groups(RowsArgs a, bool bf16, void *ws, hipStream_t st);  //
 void launch_top_logits(RowsArgs a, bool bf16, int k, int32_t *ids, float *vals, float *rest, void *ws, hipStream_t st);
 
 // ---- filtered sampling (draw.hip)
-struct DrawSums {  // of one row, over its workgroups: whole numbers, so their order does not matter
+struct DrawSums {  // of one workgroup's part of a row: whole numbers, so their order does not matter
   unsigned long long mass[2944];
   uint32_t count[2944];
-  unsigned long long stays;
-  uint32_t done, pad;
 };
 struct SampleArgs {
   const int32_t *top_k;  // optional [rows] each
@@ -285,7 +283,8 @@ struct SampleArgs {
   float *logprobs;       // optional
   // set at launch, from the workspace
   uint32_t *state;       // [rows]: 0, or the key of the maximum of a row that the first entries do not decide
-  DrawSums *sums;        // [rows]
+  uint32_t *done;        // [rows]: its workgroups that have left their sums
+  DrawSums *sums;        // [rows][slices]
   int slices;            // workgroups a row of the last launch
 };
 size_t draw_ws_bytes(int rows, int V);
