@@ -56,6 +56,16 @@ DEVI unsigned long long weight_of(double x) {
   return (unsigned long long)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & ((1ull << 52) - 1);
 }
 
+// a value that is the same in every lane, in scalar registers
+DEVI uint32_t scalar(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+DEVI float scalar(float x) { return __uint_as_float(scalar(__float_as_uint(x))); }
+DEVI double scalar(double x) {
+  return __hiloint2double((int)scalar((uint32_t)__double2hiint(x)), (int)scalar((uint32_t)__double2loint(x)));
+}
+DEVI unsigned long long scalar(unsigned long long x) {
+  return (unsigned long long)scalar((uint32_t)(x >> 32)) << 32 | scalar((uint32_t)x);
+}
+
 // A row's parameters; T = 0 is top_k = 1 at T = 1.
 struct DrawRow {
   float T, u, top_p, min_p;
@@ -67,11 +77,15 @@ struct DrawRow {
   double min_d;  // max - l up to this stays under min-p
 
   DEVI void read(const RowsArgs &a, const SampleArgs &p, int row) {
-    T = a.temps ? a.temps[row] : 1.f;
-    u = p.uniforms[row];
-    top_p = p.top_p ? p.top_p[row] : 1.f;
-    min_p = p.min_p ? p.min_p[row] : 0.f;
-    top_k = p.top_k ? p.top_k[row] : 0;
+    set(a, a.temps ? a.temps[row] : 1.f, p.uniforms[row], p.top_p ? p.top_p[row] : 1.f, p.min_p ? p.min_p[row] : 0.f,
+        p.top_k ? p.top_k[row] : 0);
+  }
+  DEVI void set(const RowsArgs &a, float t, float uniform, float tp, float mp, int k) {
+    T = t;
+    u = uniform;
+    top_p = tp;
+    min_p = mp;
+    top_k = k;
     ok = T >= 0.f && T < INFINITY && u >= 0.f && u < 1.f && top_p >= 0.f && top_p <= 1.f && min_p >= 0.f && min_p <= 1.f;
     if (T == 0.f) {
       top_k = 1;
@@ -83,9 +97,9 @@ struct DrawRow {
   }
   DEVI void set_max(float max) {
     m = max;
-    cd = 1.44269504088896340736 / (double)T;
-    cf = fminf((float)(cd * (double)(1 << (kBinsLog + kSplitLog))), 1e30f);
-    min_d = use_m ? -log((double)min_p) * (double)T : INFINITY;
+    cd = scalar(1.44269504088896340736 / (double)T);
+    cf = scalar(fminf((float)(cd * (double)(1 << (kBinsLog + kSplitLog))), 1e30f));
+    min_d = scalar(use_m ? -log((double)min_p) * (double)T : (double)INFINITY);
   }
   // of a value that is no NaN; logits of +inf have all the weight
   DEVI unsigned long long weight(float v) const {
@@ -118,7 +132,6 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
   const int row = blockIdx.x, tid = threadIdx.x;
   DrawRow d;
   d.read(a, p, row);
-  if (tid == 0) p.state[row] = 0;
   if (!d.ok) {
     if (tid == 0) {
       raise_error(a.err, DEV_BAD_PARAM);
@@ -203,10 +216,10 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
       return;
     }
   }
-  // for the next launch
+  // for the next launch, which takes the rows of the list in any order
   if (tid == 0) {
-    p.state[row] = order_key(d.m);
     p.done[row] = 0;
+    p.list[atomicAdd(p.listed, 1)] = {row, d.top_k, d.T, d.u, d.top_p, d.min_p, d.m};
   }
 }
 
@@ -236,36 +249,31 @@ static_assert(sizeof(WholeShared) <= 65536, "two workgroups a CU, static LDS");
 constexpr int kBinsPer = (kBins + kWholeThreads - 1) / kWholeThreads;  // bins a thread
 constexpr int kSeg = kListMax / kWholeWaves;                          // a wave's part of a list while it is collected
 
-// f(value, id) for the values of ids [v0, v1); the next 16-byte loads are on their way meanwhile.
+// f(16 bytes of values, first id) for the ids [v0, v1) of a row of at least a vector; -inf follows its last
+// value.  The next loads are on their way meanwhile: they go to clamped places without a branch, since
+// the compiler waits for all loads where one is on some path only (19 us instead of 9 for 38K values).
 template <typename LT, typename F>
 DEVI void each_of_row(const LT *lr, uint32_t V, uint32_t v0, uint32_t v1, F f) {
-  constexpr int N = RowVec<LT>::N, U = 2;
-  constexpr uint32_t step = kWholeThreads * N;
+  constexpr uint32_t N = RowVec<LT>::N, U = 2, step = kWholeThreads * N;
   u32x4 x[U], y[U];
   auto load = [&](u32x4 (&z)[U], uint32_t c0) {
-    if (c0 + U * step <= V) {  // uniform
 #pragma unroll
-      for (int q = 0; q < U; ++q) z[q] = row_load(lr + c0 + q * step + threadIdx.x * N);
-    } else {
-#pragma unroll
-      for (int q = 0; q < U; ++q) z[q] = row_load_end(lr, c0 + q * step + threadIdx.x * N, V);
-    }
+    for (uint32_t q = 0; q < U; ++q) z[q] = row_load(lr + min(c0 + q * step + threadIdx.x * N, V - N));
   };
   load(x, v0);
 #pragma unroll 1
   for (uint32_t c0 = v0; c0 < v1; c0 += U * step) {
-    if (c0 + U * step < v1) load(y, c0 + U * step);
+    load(y, c0 + U * step);
 #pragma unroll
-    for (int q = 0; q < U; ++q) {
+    for (uint32_t q = 0; q < U; ++q) {
       const uint32_t id = c0 + q * step + threadIdx.x * N;
-      if (id < v1) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) f(RowVec<LT>::get(x[q], e), id + e);
-      }
+      if (id + N <= v1) f(x[q], id);
     }
 #pragma unroll
-    for (int q = 0; q < U; ++q) x[q] = y[q];
+    for (uint32_t q = 0; q < U; ++q) x[q] = y[q];
   }
+  const uint32_t whole = v1 / N * N;  // (only the row's end is not whole vectors)
+  if (whole < v1 && threadIdx.x == 0) f(row_load_end(lr, whole, V), whole);
 }
 
 // The order in digits, each ascending: the bin and its part (of the distance to the
@@ -274,11 +282,8 @@ struct Digits {
   uint32_t y, k, id;
 };
 constexpr float kFar = (float)(kBins << kSplitLog);
-// the distance in parts of a bin; NaN and -inf are far.  INF: the maximum is +inf
-template <bool INF>
-DEVI float distance(const DrawRow &s, float v) {
-  return INF ? (v == INFINITY ? 0.f : kFar) : (s.m - v) * s.cf;
-}
+// the distance in parts of a bin; NaN and -inf are far
+DEVI float distance(const DrawRow &s, float v) { return (s.m - v) * s.cf; }
 DEVI bool near(const Digits &a, const Digits &b, int level) {
   const uint32_t my = level == 0 ? 0u : level == 1 ? ~2047u : ~0u;
   const uint32_t mk = level < 3 ? 0u : level == 3 ? ~0u << 21 : level == 4 ? ~0u << 10 : ~0u;
@@ -311,42 +316,60 @@ DEVI void set_digit(Digits &a, int level, uint32_t d) {
 // 2^-23 of itself, less than a part.
 struct Between {
   float lo, hi;
-  template <bool INF>
   DEVI static Between of(const DrawRow &s, uint32_t from, uint32_t to) {
-    if (INF) return {INFINITY, INFINITY};
     const double top = (double)s.m - ((double)from - 2.0) / (double)s.cf, end = (double)s.m - ((double)to + 2.0) / (double)s.cf;
-    return {(float)(end - fabs(end) * 0x1p-22), (float)(top + fabs(top) * 0x1p-22)};
+    return {scalar((float)(end - fabs(end) * 0x1p-22)), scalar((float)(top + fabs(top) * 0x1p-22))};
   }
-  DEVI bool has(float v) const { return v >= lo && v <= hi; }
+  DEVI static Between none() { return {INFINITY, INFINITY}; }  // (rows with a logit of +inf are done without)
+  DEVI bool some() const { return lo < INFINITY; }
+  // (no value is its own median of these if it is NaN)
+  DEVI bool has(float v) const { return __builtin_amdgcn_fmed3f(v, lo, hi) == v; }
 };
 // f(value, its digits) of the entries whose distance is in [from, to) parts
-template <typename LT, bool INF, typename F>
+template <typename LT, typename F>
 DEVI void each_between(const LT *lr, uint32_t V, const DrawRow &s, uint32_t from, uint32_t to, F f) {
-  const Between near_by = Between::of<INF>(s, from, to);
-  each_of_row(lr, V, 0, V, [&](float v, uint32_t id) {
-    if (near_by.has(v)) {
-      const float y = distance<INF>(s, v);
-      if (y >= (float)from && y < (float)to) f(v, Digits{(uint32_t)y, ~order_key(v), id});
+  const Between near_by = Between::of(s, from, to);
+  each_of_row(lr, V, 0, V, [&](const u32x4 &x, uint32_t id0) {
+#pragma unroll
+    for (int e = 0; e < RowVec<LT>::N; ++e) {
+      const float v = RowVec<LT>::get(x, e);
+      if (near_by.has(v)) {
+        const float y = distance(s, v);
+        if (y >= (float)from && y < (float)to) f(v, Digits{(uint32_t)y, ~order_key(v), id0 + e});
+      }
     }
   });
 }
-// Collects the values between the bounds of A in sh.list, and (TWO) of B in sh.draw, by waves: each has a
-// part of its own, so that no lane waits for a place.  false if one does not hold them.
-template <typename LT, bool TWO>
+// Collects the ids of the values between the bounds of A in sh.list, and of B in sh.draw, by waves: each has a
+// part of its own, so that no lane waits for a place.  false if one does not hold them.  A lane gathers
+// a vector's hits as bits, without a branch: a branch for every value took 24 us a row of 151936, three times as long.
+template <typename LT>
 DEVI bool collect(const LT *lr, uint32_t V, const Between &A, const Between &B, WholeShared &sh) {
+  constexpr int N = RowVec<LT>::N;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int na = 0, nb = 0;
-  each_of_row(lr, V, 0, V, [&](float v, uint32_t id) {
-    auto put = [&](bool on, unsigned long long *list, int &n) {
-      const unsigned long long mk = __ballot(on);
-      if (on) {
-        const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mk >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mk, 0));
-        if (at < kSeg) list[wave * kSeg + at] = (unsigned long long)__float_as_uint(v) << 32 | id;
+  each_of_row(lr, V, 0, V, [&](const u32x4 &x, uint32_t id0) {
+    uint32_t a = 0, b = 0;  // the last value in the lowest bit
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float v = RowVec<LT>::get(x, e);
+      a = a + a + (A.has(v) ? 1u : 0u);
+      b = b + b + (B.has(v) ? 1u : 0u);
+    }
+    auto put = [&](uint32_t bits, unsigned long long *list, int &n) {
+      while (true) {
+        const unsigned long long mk = __ballot(bits != 0);
+        if (!mk) break;
+        if (bits) {
+          const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mk >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mk, 0));
+          if (at < kSeg) list[wave * kSeg + at] = id0 + (N - 1) - (__ffs(bits) - 1);
+          bits &= bits - 1;
+        }
+        n += __popcll(mk);
       }
-      n += __popcll(mk);
     };
-    put(A.has(v), sh.list, na);
-    if (TWO) put(B.has(v), sh.draw, nb);
+    put(a, sh.list, na);
+    put(b, sh.draw, nb);
   });
   if (lane == 0) {
     sh.wave_n[0][wave] = na;
@@ -358,8 +381,9 @@ DEVI bool collect(const LT *lr, uint32_t V, const Between &A, const Between &B, 
   return ok;
 }
 // The entries of a collected list that `on` takes (by digits) and that have a weight, as keys in descending order; their number.
-template <bool INF, typename On>
-DEVI int pack_list(const DrawRow &s, unsigned long long *list, const int *wave_n, WholeShared &sh, int slot, On on) {
+template <typename LT, typename On>
+DEVI int pack_list(const LT *lr, uint32_t V, const DrawRow &s, unsigned long long *list, const int *wave_n, WholeShared &sh,
+                   int slot, On on) {
   constexpr int kTwo = kListMax / kWholeThreads;
   const int tid = threadIdx.x;
   unsigned long long k[kTwo];
@@ -368,9 +392,9 @@ DEVI int pack_list(const DrawRow &s, unsigned long long *list, const int *wave_n
     const int i = j * kWholeThreads + tid;
     k[j] = 0;
     if (i % kSeg < wave_n[i / kSeg]) {
-      const unsigned long long x = list[i];
-      const float v = __uint_as_float((uint32_t)(x >> 32)), y = distance<INF>(s, v);
-      if (y < kFar && on(Digits{(uint32_t)y, ~order_key(v), (uint32_t)x}) && s.weight(v)) k[j] = entry_key(v, (uint32_t)x);
+      const uint32_t id = (uint32_t)list[i];
+      const float v = id < V ? to_f32(lr[id]) : -INFINITY, y = distance(s, v);
+      if (y < kFar && on(Digits{(uint32_t)y, ~order_key(v), id}) && s.weight(v)) k[j] = entry_key(v, id);
     }
   }
   if (tid == 0) sh.n[slot] = 0;
@@ -415,7 +439,7 @@ DEVI Prefix pass_in_list(const DrawRow &s, const unsigned long long *list, int n
     }
   }
   __syncthreads();
-  const Prefix p = {sh.hit[0], sh.hit[1]};
+  const Prefix p = {scalar(sh.hit[0]), scalar(sh.hit[1])};
   __syncthreads();
   return p;
 }
@@ -442,31 +466,33 @@ DEVI Bin pass_in_bins(const unsigned long long *mass, const uint32_t *count, int
     }
   }
   __syncthreads();
-  const Bin r = {sh.hit_i, sh.hit[1], sh.hit[0]};
+  const Bin r = {(int)scalar((uint32_t)sh.hit_i), scalar(sh.hit[1]), scalar(sh.hit[0])};
   __syncthreads();
   return r;
 }
 
 // The shortest prefix of the whole row's order whose count (by_count) or sum is above `target`, which
 // is passed in `bin`: its entries, or, while they are too many for the list, those of a part of it.
-template <typename LT, bool INF>
+// The values of `also` come into sh.draw on the way; it is set to none if they were not.
+template <typename LT>
 DEVI Prefix find_in_row(const LT *lr, uint32_t V, const DrawRow &s, bool by_count, unsigned long long target, Bin bin,
-                        WholeShared &sh) {
+                        Between &also, WholeShared &sh) {
   const int tid = threadIdx.x;
   Digits at = {0, 0, 0};
   for (int level = 0;; ++level) {
     set_digit(at, level, bin.i);
     const uint32_t from = at.y, to = at.y + (level == 0 ? kSplit : 1);
-    if (collect<LT, false>(lr, V, Between::of<INF>(s, from, to), {}, sh)) {
-      const int n = pack_list<INF>(s, sh.list, sh.wave_n[0], sh, 0, [&](const Digits &d) { return near(d, at, level + 1); });
+    if (collect<LT>(lr, V, Between::of(s, from, to), also, sh)) {
+      const int n = pack_list(lr, V, s, sh.list, sh.wave_n[0], sh, 0, [&](const Digits &d) { return near(d, at, level + 1); });
       return pass_in_list(s, sh.list, n, by_count, target, bin.m0, bin.n0, sh);
     }
+    also = Between::none();
     if (level >= 2) {
       // (the bounds take neighbours too: the entries themselves may be few)
       __syncthreads();
       if (tid == 0) sh.n[0] = 0;
       __syncthreads();
-      each_between<LT, INF>(lr, V, s, from, to, [&](float v, const Digits &d) {
+      each_between<LT>(lr, V, s, from, to, [&](float v, const Digits &d) {
         if (near(d, at, level + 1) && s.weight(v)) {
           const int i = atomicAdd(&sh.n[0], 1);
           if (i < kListMax) sh.list[i] = entry_key(v, d.id);
@@ -485,7 +511,7 @@ DEVI Prefix find_in_row(const LT *lr, uint32_t V, const DrawRow &s, bool by_coun
       sh.part.count[i] = 0;
     }
     __syncthreads();
-    each_between<LT, INF>(lr, V, s, from, to, [&](float v, const Digits &d) {
+    each_between<LT>(lr, V, s, from, to, [&](float v, const Digits &d) {
       if (near(d, at, level + 1)) {
         const unsigned long long w = s.weight(v);
         if (w) {
@@ -506,45 +532,79 @@ DEVI Prefix find_in_row(const LT *lr, uint32_t V, const DrawRow &s, bool by_coun
   }
 }
 
-template <typename LT, bool INF>
-DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, int row, int slice, WholeShared &sh) {
+// A row whose maximum is +inf: its n logits of +inf have a weight of 1 each, in the order of their ids.
+template <typename LT>
+DEVI void draw_of_infinities(const LT *lr, const SampleArgs &p, const DrawRow &d, int V, int row, WholeShared &sh) {
+  const int tid = threadIdx.x, len = (V + kWholeThreads - 1) / kWholeThreads;
+  uint32_t mine = 0;
+  for (int i = tid * len; i < min((tid + 1) * len, V); ++i) mine += to_f32(lr[i]) == INFINITY;
+  uint32_t *red = (uint32_t *)sh.redu[0];
+  const uint32_t upto = block_scan<kWholeWaves>(mine, red);
+  if (tid == kWholeThreads - 1) sh.hit_i = (int)upto;
+  __syncthreads();
+  uint32_t n = sh.hit_i;
+  if (d.has_k) n = min(n, (uint32_t)d.top_k);
+  if (d.use_p) n = max(1u, min(n, (uint32_t)ceil((double)d.top_p * n)));
+  uint32_t at = min((uint32_t)floor((double)d.u * n), n - 1);  // the draw's place among them
+  if (at >= upto - mine && at < upto) {
+    at -= upto - mine;
+    for (int i = tid * len;; ++i)
+      if (to_f32(lr[i]) == INFINITY && at-- == 0) {
+        d.finish(p, row, i, d.logprob(INFINITY, (unsigned long long)n << kWeightBits));
+        break;
+      }
+  }
+}
+
+template <typename LT>
+DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, int row, int slice, int slices, DrawSums *g,
+                     WholeShared &sh) {
   constexpr int N = RowVec<LT>::N;
   const int tid = threadIdx.x;
   const LT *lr = (const LT *)a.logits + (size_t)row * a.ld;
+  if (d.m == INFINITY) {
+    if (slice == 0) draw_of_infinities(lr, p, d, a.V, row, sh);
+    return;
+  }
   for (int i = tid; i < kBins; i += kWholeThreads) {
     sh.mass[i] = 0;
     sh.count[i] = 0;
   }
   __syncthreads();
-  const uint32_t len = ((uint32_t)a.V / p.slices / N + 1) * N, v0 = slice * len, v1 = min((uint32_t)a.V, v0 + len);
-  auto add = [&](auto counted) {
-    each_of_row(lr, a.V, v0, v1, [&](float x, uint32_t) {
-      const float y = distance<INF>(d, x);
-      if (y < kFar) {
-        const int b = (int)y >> kSplitLog;
-        const unsigned long long w = INF ? 1ull << kWeightBits : weight_of(((double)d.m - (double)x) * d.cd);
-        if constexpr (decltype(counted)::value) {
-          if (w) {
-            atomicAdd(&sh.mass[b], w);
-            atomicAdd(&sh.count[b], 1u);
-          }
-        } else {
-          atomicAdd(&sh.mass[b], w);
+  const uint32_t len = ((uint32_t)a.V / slices / N + 1) * N, v0 = slice * len, v1 = min((uint32_t)a.V, v0 + len);
+  // f(bin, weight), four values at a time: their weights are formed side by side
+  auto each_weight = [&](auto f) {
+    each_of_row(lr, a.V, v0, v1, [&](const u32x4 &x, uint32_t) {
+#pragma unroll
+      for (int e = 0; e < N; e += 4) {
+        float y[4];
+        unsigned long long w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float v = RowVec<LT>::get(x, e + j);
+          y[j] = distance(d, v);
+          w[j] = weight_of(((double)d.m - (double)v) * d.cd);  // (any number where y is far)
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (y[j] < kFar) f((int)y[j] >> kSplitLog, w[j]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     });
   };
   if (v0 < v1) {
-    if (d.has_k) add(std::true_type{});
-    else add(std::false_type{});
+    each_weight([&](int b, unsigned long long w) { atomicAdd(&sh.mass[b], w); });
+    if (d.has_k)
+      each_weight([&](int b, unsigned long long w) {
+        if (w) atomicAdd(&sh.count[b], 1u);
+      });
   }
   __syncthreads();
-  if (p.slices > 1) {
+  if (slices > 1) {
     // To memory; the last workgroup of the row adds them all up.  Stores and loads are device-scope ones,
     // complete when the count of the storing thread's drains: 64 rows at once took 17 to 37 us by
     // 64-bit atomics into one place, and as long by plain stores between fences, which write back and
     // drop the whole cache of an XCD.
-    DrawSums *g = p.sums + (size_t)row * p.slices;
     for (int i = tid; i < kBins; i += kWholeThreads) {
       __hip_atomic_store(&g[slice].mass[i], sh.mass[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (d.has_k) __hip_atomic_store(&g[slice].count[i], sh.count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -552,19 +612,35 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
     __builtin_amdgcn_s_waitcnt(0);  // this thread's sums are there
     __syncthreads();
     if (tid == 0)
-      sh.last = __hip_atomic_fetch_add(&p.done[row], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)p.slices - 1;
+      sh.last = __hip_atomic_fetch_add(&p.done[row], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)slices - 1;
     __syncthreads();
     if (!sh.last) return;
-    for (int i = tid; i < kBins; i += kWholeThreads) {
-      unsigned long long m = 0;
-      uint32_t n = 0;
-#pragma unroll 4
-      for (int q = 0; q < p.slices; ++q) m += __hip_atomic_load(&g[q].mass[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (d.has_k)
-        for (int q = 0; q < p.slices; ++q) n += __hip_atomic_load(&g[q].count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      sh.mass[i] = m;
-      sh.count[i] = n;
+    unsigned long long m[kBinsPer] = {};
+    uint32_t n[kBinsPer] = {};
+    for (int q0 = 0; q0 < slices; q0 += 8) {  // (eight of every bin in flight: each waits a microsecond or two)
+      unsigned long long x[8][kBinsPer];
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+#pragma unroll
+        for (int j = 0; j < kBinsPer; ++j)
+          x[q][j] = __hip_atomic_load(&g[min(q0 + q, slices - 1)].mass[min(j * kWholeThreads + tid, kBins - 1)],
+                                      __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+#pragma unroll
+        for (int j = 0; j < kBinsPer; ++j) m[j] += q0 + q < slices ? x[q][j] : 0ull;
     }
+    if (d.has_k)
+      for (int q = 0; q < slices; ++q)
+#pragma unroll
+        for (int j = 0; j < kBinsPer; ++j)
+          n[j] += __hip_atomic_load(&g[q].count[min(j * kWholeThreads + tid, kBins - 1)], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int j = 0; j < kBinsPer; ++j)
+      if (j * kWholeThreads + tid < kBins) {
+        sh.mass[j * kWholeThreads + tid] = m[j];
+        sh.count[j * kWholeThreads + tid] = n[j];
+      }
     __syncthreads();
   }
   // what lies before each thread's bins, and in all of them
@@ -579,97 +655,106 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
     sh.hit[1] = em;
   }
   __syncthreads();
-  const unsigned long long entries = sh.hit[0];
-  unsigned long long total = sh.hit[1];
+  const unsigned long long entries = scalar(sh.hit[0]);
+  unsigned long long total = scalar(sh.hit[1]);
   __syncthreads();
   auto bin_of = [&](bool by_count, unsigned long long target) {
     return pass_in_bins(sh.mass, sh.count, kBins, by_count, target, em - pm, en - pn, sh);
   };
-  auto done = [&](const Prefix &f) {
-    if (tid == 0) d.finish(p, row, (int)entry_id(f.key), d.logprob(entry_value(f.key), total));
-  };
   auto drawn = [&](unsigned long long sum) { return min((unsigned long long)floor((double)d.u * (double)sum), sum - 1); };
-  if (d.has_k && (unsigned long long)d.top_k < entries) {
-    const unsigned long long target = d.top_k - 1;
-    total = find_in_row<LT, INF>(lr, a.V, d, true, target, bin_of(true, target), sh).mass;
-  }
-  if (d.use_p) {
-    const unsigned long long want = (unsigned long long)ceil((double)d.top_p * (double)total);
-    const unsigned long long target = want == 0 ? 0 : min(want, total) - 1;
-    const Bin bin = bin_of(false, target);
-    // The kept sum is target + 1 at least, and less than the weight of the bin's first part above it: where
-    // the draw falls into one bin in both cases, one pass collects both bins.
-    const unsigned long long most = min(total, target + 1 + d.weight_at(bin.i));
-    const Bin first = bin_of(false, drawn(target + 1)), last = bin_of(false, drawn(most));
-    if (!d.use_m && first.i == last.i) {
-      const uint32_t fa = (uint32_t)bin.i << kSplitLog, fb = (uint32_t)first.i << kSplitLog;
-      if (collect<LT, true>(lr, a.V, Between::of<INF>(d, fa, fa + kSplit), Between::of<INF>(d, fb, fb + kSplit), sh)) {
-        const int n = pack_list<INF>(d, sh.list, sh.wave_n[0], sh, 0, [&](const Digits &x) { return x.y >> kSplitLog == (uint32_t)bin.i; });
-        const int k = pack_list<INF>(d, sh.draw, sh.wave_n[1], sh, 1, [&](const Digits &x) { return x.y >> kSplitLog == (uint32_t)first.i; });
-        total = pass_in_list(d, sh.list, n, false, target, bin.m0, bin.n0, sh).mass;
-        done(pass_in_list(d, sh.draw, k, false, drawn(total), first.m0, first.n0, sh));
-        return;
+  // top-k, top-p, then (the shorter of it and min-p kept) the draw
+#pragma unroll 1
+  for (int step = d.has_k && (unsigned long long)d.top_k < entries ? 0 : d.use_p ? 1 : 2;; step = step == 0 && d.use_p ? 1 : 2) {
+    unsigned long long target = d.top_k - 1;
+    if (step == 1) {
+      const unsigned long long want = (unsigned long long)ceil((double)d.top_p * (double)total);
+      target = want == 0 ? 0 : min(want, total) - 1;
+    } else if (step == 2) {
+      if (d.use_m) {
+        // the sum that stays under min-p: whole bins, and of the bins around the border the entries that stay
+        const double border = d.min_d * (double)d.cf / kSplit;
+        const int b0 = (int)fmin(fmax(border - 1.0, 0.0), (double)kBins), b1 = min(b0 + 3, kBins);
+        unsigned long long mm = 0;
+        for (int b = tid; b < b0; b += kWholeThreads) mm += sh.mass[b];
+        if (b0 < kBins)
+          each_between<LT>(lr, a.V, d, b0 << kSplitLog, b1 << kSplitLog, [&](float v, const Digits &) {
+            if (d.stays(v)) mm += d.weight(v);
+          });
+        total = min(total, block_reduce_sum<kWholeWaves>(mm, sh.redu[0]));
+        __syncthreads();
       }
-      __syncthreads();
+      target = drawn(total);
     }
-    total = find_in_row<LT, INF>(lr, a.V, d, false, target, bin, sh).mass;
+    const Bin bin = bin_of(step == 0, target);
+    // The sum that top-p keeps is target + 1 at least, and less than the weight of the bin's first part above it:
+    // where the draw falls into one bin in both cases, one pass collects both bins.
+    Between also = Between::none();
+    Bin next = {};
+    if (step == 1 && !d.use_m) {
+      next = bin_of(false, drawn(target + 1));
+      const Bin last = bin_of(false, drawn(min(total, target + 1 + d.weight_at(bin.i))));
+      if (next.i == last.i) also = Between::of(d, (uint32_t)next.i << kSplitLog, (uint32_t)(next.i + 1) << kSplitLog);
+    }
+    Prefix f = find_in_row<LT>(lr, a.V, d, step == 0, target, bin, also, sh);
+    bool end = step == 2;
+    if (!end) total = f.mass;
+    if (also.some()) {
+      const int n = pack_list(lr, a.V, d, sh.draw, sh.wave_n[1], sh, 1, [&](const Digits &x) { return x.y >> kSplitLog == (uint32_t)next.i; });
+      f = pass_in_list(d, sh.draw, n, false, drawn(total), next.m0, next.n0, sh);
+      end = true;
+    }
+    if (end) {
+      if (tid == 0) d.finish(p, row, (int)entry_id(f.key), d.logprob(entry_value(f.key), total));
+      return;
+    }
   }
-  if (d.use_m) {
-    // the sum that stays under min-p: whole bins, and of the bins around the border the entries that stay
-    const double border = d.min_d * (double)d.cf / kSplit;
-    const int b0 = INF ? 0 : (int)fmin(fmax(border - 1.0, 0.0), (double)kBins), b1 = INF ? 1 : min(b0 + 3, kBins);
-    unsigned long long mm = 0;
-    for (int b = tid; b < b0; b += kWholeThreads) mm += sh.mass[b];
-    if (b0 < kBins)
-      each_between<LT, INF>(lr, a.V, d, b0 << kSplitLog, b1 << kSplitLog, [&](float v, const Digits &) {
-        if (d.stays(v)) mm += d.weight(v);
-      });
-    total = min(total, block_reduce_sum<kWholeWaves>(mm, sh.redu[0]));
-    __syncthreads();
-  }
-  const unsigned long long target = drawn(total);
-  done(find_in_row<LT, INF>(lr, a.V, d, false, target, bin_of(false, target), sh));
 }
 
+// The listed rows, each by as many workgroups as there are for it (few rows of a batch are flat), 16 at most.
 template <typename LT>
 __global__ __launch_bounds__(kWholeThreads) void draw_whole_kernel(RowsArgs a, SampleArgs p) {
   __shared__ WholeShared sh;
-  const int row = blockIdx.x / p.slices, slice = blockIdx.x % p.slices;
-  const uint32_t state = p.state[row];
-  if (state == 0) return;  // the first entries have decided
-  DrawRow d;
-  d.read(a, p, row);
-  d.set_max(order_key_value(state));
-  if (d.m == INFINITY) draw_whole<LT, true>(a, p, d, row, slice, sh);
-  else draw_whole<LT, false>(a, p, d, row, slice, sh);
+  const int listed = *p.listed;
+  if (listed == 0) return;  // the first entries have decided
+  const int slices = max(1, min(min(p.most_slices, (int)gridDim.x / listed), 16));
+  for (int i = blockIdx.x; i < listed * slices; i += gridDim.x) {
+    const DrawItem it = p.list[i / slices];
+    const int row = it.row;
+    DrawRow d;
+    d.set(a, it.T, it.u, it.top_p, it.min_p, it.top_k);
+    d.set_max(it.m);
+    draw_whole<LT>(a, p, d, row, i % slices, slices, p.sums + i / slices * slices, sh);
+    __syncthreads();
+  }
 }
 
-// Workgroups a row of the last launch: for few rows as many as cut a row of 128K ids to 8K each (64
-// rows of 128256 fp32 logits, the flat ones 120 us with one workgroup), for many enough to fill the chip.
-static int draw_slices(int rows, int V) { return std::max(1, std::min({16, 1024 / rows, V / 8192})); }
+// Workgroups of the last launch: one a CU (with two, some start only when others end), or 16 a row.
+static int draw_grid(int rows) { return (int)std::min(256L, 16L * rows); }
 
-// [error word and groups][state, workgroups done: per row][sums, where a row has several workgroups]
+// [error word and groups][listed][a row each: list, workgroups done][a workgroup each: sums]
 struct DrawLayout {
-  size_t state, done, sums, bytes;
+  size_t listed, list, done, sums, bytes;
 };
 static DrawLayout draw_layout(int rows, int V) {
   DrawLayout l;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  const int slices = draw_slices(rows, V);
-  l.state = up(rows_ws_bytes(rows, V));
-  l.done = l.state + (size_t)rows * 4;
+  l.listed = up(rows_ws_bytes(rows, V));
+  l.list = l.listed + 256;
+  l.done = l.list + (size_t)rows * sizeof(DrawItem);
   l.sums = up(l.done + (size_t)rows * 4);
-  l.bytes = l.sums + (slices > 1 ? (size_t)rows * slices * sizeof(DrawSums) : 0);
+  l.bytes = l.sums + draw_grid(rows) * sizeof(DrawSums);
   return l;
 }
 size_t draw_ws_bytes(int rows, int V) { return draw_layout(rows, V).bytes; }
 
 void launch_sample_logits(RowsArgs a, bool bf16, SampleArgs p, void *ws, hipStream_t st) {
   const DrawLayout l = draw_layout(a.rows, a.V);
-  p.state = (uint32_t *)((char *)ws + l.state);
-  p.done = (uint32_t *)((char *)ws + l.done);
-  p.sums = (DrawSums *)((char *)ws + l.sums);
-  p.slices = draw_slices(a.rows, a.V);
+  char *w = (char *)ws;
+  p.listed = a.zero = (int32_t *)(w + l.listed);
+  p.list = (DrawItem *)(w + l.list);
+  p.done = (uint32_t *)(w + l.done);
+  p.sums = (DrawSums *)(w + l.sums);
+  p.most_slices = a.V / 8192;
   a = launch_row_groups(a, bf16, ws, st);
   auto go = [&](auto t) {
     using LT = decltype(t);
@@ -677,7 +762,7 @@ void launch_sample_logits(RowsArgs a, bool bf16, SampleArgs p, void *ws, hipStre
       constexpr int NR = decltype(nr)::value;
       hipLaunchKernelGGL((draw_first_kernel<LT, NR>), dim3(a.rows), dim3(kSelThreads), 0, st, a, p);
     });
-    hipLaunchKernelGGL(draw_whole_kernel<LT>, dim3(a.rows * p.slices), dim3(kWholeThreads), 0, st, a, p);
+    hipLaunchKernelGGL(draw_whole_kernel<LT>, dim3(draw_grid(a.rows)), dim3(kWholeThreads), 0, st, a, p);
   };
   if (bf16) go(bf16_t{});
   else go(0.f);
