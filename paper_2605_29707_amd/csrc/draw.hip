@@ -77,15 +77,11 @@ struct DrawRow {
   double min_d;  // max - l up to this stays under min-p
 
   DEVI void read(const RowsArgs &a, const SampleArgs &p, int row) {
-    set(a, a.temps ? a.temps[row] : 1.f, p.uniforms[row], p.top_p ? p.top_p[row] : 1.f, p.min_p ? p.min_p[row] : 0.f,
-        p.top_k ? p.top_k[row] : 0);
-  }
-  DEVI void set(const RowsArgs &a, float t, float uniform, float tp, float mp, int k) {
-    T = t;
-    u = uniform;
-    top_p = tp;
-    min_p = mp;
-    top_k = k;
+    T = a.temps ? a.temps[row] : 1.f;
+    u = p.uniforms[row];
+    top_p = p.top_p ? p.top_p[row] : 1.f;
+    min_p = p.min_p ? p.min_p[row] : 0.f;
+    top_k = p.top_k ? p.top_k[row] : 0;
     ok = T >= 0.f && T < INFINITY && u >= 0.f && u < 1.f && top_p >= 0.f && top_p <= 1.f && min_p >= 0.f && min_p <= 1.f;
     if (T == 0.f) {
       top_k = 1;
@@ -132,6 +128,7 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
   const int row = blockIdx.x, tid = threadIdx.x;
   DrawRow d;
   d.read(a, p, row);
+  if (tid == 0) p.state[row] = 0;
   if (!d.ok) {
     if (tid == 0) {
       raise_error(a.err, DEV_BAD_PARAM);
@@ -216,10 +213,10 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
       return;
     }
   }
-  // for the next launch, which takes the rows of the list in any order
+  // for the next launch
   if (tid == 0) {
+    p.state[row] = order_key(d.m);
     p.done[row] = 0;
-    p.list[atomicAdd(p.listed, 1)] = {row, d.top_k, d.T, d.u, d.top_p, d.min_p, d.m};
   }
 }
 
@@ -710,39 +707,37 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
   }
 }
 
-// The listed rows, each by as many workgroups as there are for it (few rows of a batch are flat), 16 at most.
+// The rows that are left, a workgroup a slice of each.  (Slices that go by how many rows are left, from a
+// list of them, are no faster: their parameters come three dependent loads later.)
 template <typename LT>
 __global__ __launch_bounds__(kWholeThreads) void draw_whole_kernel(RowsArgs a, SampleArgs p) {
   __shared__ WholeShared sh;
-  const int listed = *p.listed;
-  if (listed == 0) return;  // the first entries have decided
-  const int slices = max(1, min(min(p.most_slices, (int)gridDim.x / listed), 16));
-  for (int i = blockIdx.x; i < listed * slices; i += gridDim.x) {
-    const DrawItem it = p.list[i / slices];
-    const int row = it.row;
-    DrawRow d;
-    d.set(a, it.T, it.u, it.top_p, it.min_p, it.top_k);
-    d.set_max(it.m);
-    draw_whole<LT>(a, p, d, row, i % slices, slices, p.sums + i / slices * slices, sh);
-    __syncthreads();
-  }
+  const int row = blockIdx.x / p.slices, slice = blockIdx.x % p.slices;
+  const uint32_t state = p.state[row];
+  if (state == 0) return;  // the first entries have decided
+  DrawRow d;
+  d.read(a, p, row);
+  d.set_max(order_key_value(state));
+  draw_whole<LT>(a, p, d, row, slice, p.slices, p.sums + (size_t)row * p.slices, sh);
 }
 
-// Workgroups of the last launch: one a CU (with two, some start only when others end), or 16 a row.
-static int draw_grid(int rows) { return (int)std::min(256L, 16L * rows); }
+// Workgroups a row of the last launch: for few rows as many as cut a row of 128K ids to 8K each (64
+// rows of 128256 fp32 logits, the flat ones 120 us with one workgroup), for many enough to fill the chip
+// (512 rows of 151936 bf16 logits 75 us with two, 92 with four).
+static int draw_slices(int rows, int V) { return std::max(1, std::min({16, 1024 / rows, V / 8192})); }
 
-// [error word and groups][listed][a row each: list, workgroups done][a workgroup each: sums]
+// [error word and groups][a row each: state, workgroups done][sums, where a row has several workgroups]
 struct DrawLayout {
-  size_t listed, list, done, sums, bytes;
+  size_t state, done, sums, bytes;
 };
 static DrawLayout draw_layout(int rows, int V) {
   DrawLayout l;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  l.listed = up(rows_ws_bytes(rows, V));
-  l.list = l.listed + 256;
-  l.done = l.list + (size_t)rows * sizeof(DrawItem);
+  const int slices = draw_slices(rows, V);
+  l.state = up(rows_ws_bytes(rows, V));
+  l.done = l.state + (size_t)rows * 4;
   l.sums = up(l.done + (size_t)rows * 4);
-  l.bytes = l.sums + draw_grid(rows) * sizeof(DrawSums);
+  l.bytes = l.sums + (slices > 1 ? (size_t)rows * slices * sizeof(DrawSums) : 0);
   return l;
 }
 size_t draw_ws_bytes(int rows, int V) { return draw_layout(rows, V).bytes; }
@@ -750,11 +745,10 @@ size_t draw_ws_bytes(int rows, int V) { return draw_layout(rows, V).bytes; }
 void launch_sample_logits(RowsArgs a, bool bf16, SampleArgs p, void *ws, hipStream_t st) {
   const DrawLayout l = draw_layout(a.rows, a.V);
   char *w = (char *)ws;
-  p.listed = a.zero = (int32_t *)(w + l.listed);
-  p.list = (DrawItem *)(w + l.list);
+  p.state = (uint32_t *)(w + l.state);
   p.done = (uint32_t *)(w + l.done);
   p.sums = (DrawSums *)(w + l.sums);
-  p.most_slices = a.V / 8192;
+  p.slices = draw_slices(a.rows, a.V);
   a = launch_row_groups(a, bf16, ws, st);
   auto go = [&](auto t) {
     using LT = decltype(t);
@@ -762,7 +756,7 @@ void launch_sample_logits(RowsArgs a, bool bf16, SampleArgs p, void *ws, hipStre
       constexpr int NR = decltype(nr)::value;
       hipLaunchKernelGGL((draw_first_kernel<LT, NR>), dim3(a.rows), dim3(kSelThreads), 0, st, a, p);
     });
-    hipLaunchKernelGGL(draw_whole_kernel<LT>, dim3(draw_grid(a.rows)), dim3(kWholeThreads), 0, st, a, p);
+    hipLaunchKernelGGL(draw_whole_kernel<LT>, dim3(a.rows * p.slices), dim3(kWholeThreads), 0, st, a, p);
   };
   if (bf16) go(bf16_t{});
   else go(0.f);

@@ -265,7 +265,6 @@ struct RowsArgs {
   int32_t *err;
   float2 *groups;      // [rows][G]: (max, sum of exp) of every 32 ids
   int G, nch;          // workgroups a row of the first launch
-  int32_t *zero = nullptr;  // optional: a word the first launch clears
 };
 size_t rows_ws_bytes(int rows, int V);
 RowsArgs launch_row_groups(RowsArgs a, bool bf16, void *ws, hipStream_t st);  // a with its workspace set
@@ -276,10 +275,6 @@ struct DrawSums {  // of one workgroup's part of a row: whole numbers, so their 
   unsigned long long mass[2944];
   uint32_t count[2944];
 };
-struct alignas(32) DrawItem {  // a row, its parameters and its maximum
-  int32_t row, top_k;
-  float T, u, top_p, min_p, m;
-};
 struct SampleArgs {
   const int32_t *top_k;  // optional [rows] each
   const float *top_p, *min_p;
@@ -287,11 +282,10 @@ struct SampleArgs {
   int32_t *tokens;
   float *logprobs;       // optional
   // set at launch, from the workspace
-  int32_t *listed;         // rows that their first entries do not decide: how many, and which
-  DrawItem *list;
-  uint32_t *done;          // [rows]: their workgroups that have left their sums
-  DrawSums *sums;          // of the last launch's workgroups
-  int most_slices;         // workgroups a row at most
+  uint32_t *state;         // [rows]: 0, or the key of the maximum of a row that its first entries do not decide
+  uint32_t *done;          // [rows]: its workgroups that have left their sums
+  DrawSums *sums;          // [rows][slices]
+  int slices;              // workgroups a row of the last launch
 };
 size_t draw_ws_bytes(int rows, int V);
 void launch_sample_logits(RowsArgs a, bool bf16, SampleArgs p, void *ws, hipStream_t st);

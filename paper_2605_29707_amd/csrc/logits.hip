@@ -21,10 +21,7 @@ template <typename LT>
 __global__ __launch_bounds__(kGrThreads) void row_groups_kernel(RowsArgs a) {
   constexpr int N = RowVec<LT>::N, NV = kGrChunk / kGrThreads / N, LPG = kGroup / N;
   const int row = blockIdx.x / a.nch, ch = blockIdx.x % a.nch, tid = threadIdx.x;
-  if (blockIdx.x == 0 && tid == 0) {
-    *a.err = 0;
-    if (a.zero) *a.zero = 0;
-  }
+  if (blockIdx.x == 0 && tid == 0) *a.err = 0;
   const uint32_t c0 = (uint32_t)ch * kGrChunk, V = a.V;
   const LT *lr = (const LT *)a.logits + (size_t)row * a.ld;
   u32x4 x[NV];
