@@ -140,18 +140,17 @@ def _check(status: int):
 
 
 def _ptr(t):
-    if t is None:
-        return None
-    return C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream):
     if stream is None:
         import torch
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+        # the handle alone: a Stream object costs 3 us, as much as a launch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
-        return C.c_void_p(stream)
-    return C.c_void_p(stream.cuda_stream)
+        return stream
+    return stream.cuda_stream
 
 
 def make_config(cfg) -> domino_config:
@@ -331,27 +330,27 @@ def domino_philox4x32_10(counters, key, out, stream=None):
 def _rows(logits):
     """(rows, vocab, row stride, domino_dtype) of a 2-D tensor of logits whose rows are dense."""
     import torch
-    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or \
-            (logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise DominoError(DOMINO_ERR_INVALID_ARG, "logits must be a 2-D fp32 or bf16 tensor with dense rows")
-    ld = logits.stride(0) if logits.shape[0] > 1 else max(logits.stride(0), logits.shape[1])
-    return logits.shape[0], logits.shape[1], ld, DOMINO_BF16 if logits.dtype == torch.bfloat16 else DOMINO_F32
+    dt = logits.dtype
+    if logits.dim() != 2 or dt not in (torch.float32, torch.bfloat16):
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "logits must be a 2-D fp32 or bf16 tensor")
+    (n, V), (ld, one) = logits.shape, logits.stride()
+    if V > 1 and one != 1:
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "logits must have dense rows")
+    return n, V, ld if n > 1 else max(ld, V), DOMINO_BF16 if dt is torch.bfloat16 else DOMINO_F32
 
 
-def _check_array(name, t, like, dtype, n):
-    """An optional per-row array: dense, of `dtype`, n elements, on the logits' device."""
-    if t is None:
-        return
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != like.device:
+def _check_array(name, t, device, dtype, n):
+    """An optional per-row array: dense, of `dtype`, n elements, on the logits' device (an index, -1 a CPU's)."""
+    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device):
         raise DominoError(DOMINO_ERR_INVALID_ARG,
-                          f"{name} must be a contiguous {dtype} tensor of {n} elements on {like.device}")
+                          f"{name} must be a contiguous {dtype} tensor of {n} elements on the logits' device")
 
 
-def _check_device(logits):
+def _check_device(device):
     """Work is launched on the current device: tensors of another one are refused."""
     import torch
-    if not logits.is_cuda or logits.device.index != torch.cuda.current_device():
-        raise DominoError(DOMINO_ERR_INVALID_ARG, f"logits must be on the current device, not on {logits.device}")
+    if device < 0 or device != torch.cuda.current_device():
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "logits must be on the current GPU")
 
 
 def domino_top_logits_workspace_bytes(rows, vocab, k) -> int:
@@ -362,11 +361,11 @@ def domino_top_logits(logits, top_ids, top_vals, workspace, rest=None, temperatu
     """logits [rows, vocab] with dense rows; top_ids int32 and top_vals fp32 [rows, k]; rest fp32 [rows]."""
     import torch
     n, V, ld, dt = _rows(logits)
-    k = top_ids.shape[-1]
-    _check_array("top_ids", top_ids, logits, torch.int32, n * k)
-    _check_array("top_vals", top_vals, logits, torch.float32, n * k)
-    _check_array("rest", rest, logits, torch.float32, n)
-    _check_device(logits)
+    k, dev = top_ids.shape[-1], logits.get_device()
+    _check_array("top_ids", top_ids, dev, torch.int32, n * k)
+    _check_array("top_vals", top_vals, dev, torch.float32, n * k)
+    _check_array("rest", rest, dev, torch.float32, n)
+    _check_device(dev)
     _check(load().domino_top_logits(n, V, k, _ptr(logits), dt, ld, float(temperature), _ptr(top_ids), _ptr(top_vals),
                                     _ptr(rest), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                     _stream(stream)))
@@ -381,18 +380,19 @@ def domino_distill_loss(logits, teacher_ids, teacher_vals, loss, workspace, teac
     """logits [rows, vocab] with dense rows; teacher_ids int32 and teacher_vals fp32 [rows, k]; grad as logits."""
     import torch
     n, V, ld, dt = _rows(logits)
-    k = teacher_ids.shape[-1]
-    _check_array("teacher_ids", teacher_ids, logits, torch.int32, n * k)
-    _check_array("teacher_vals", teacher_vals, logits, torch.float32, n * k)
-    for name, t, size in (("teacher_rest", teacher_rest, n), ("row_weights", row_weights, n), ("row_loss", row_loss, n),
-                          ("loss", loss, 1)):
-        _check_array(name, t, logits, torch.float32, size)
+    k, dev, f32 = teacher_ids.shape[-1], logits.get_device(), torch.float32
+    _check_array("teacher_ids", teacher_ids, dev, torch.int32, n * k)
+    _check_array("teacher_vals", teacher_vals, dev, f32, n * k)
+    _check_array("teacher_rest", teacher_rest, dev, f32, n)
+    _check_array("row_weights", row_weights, dev, f32, n)
+    _check_array("row_loss", row_loss, dev, f32, n)
+    _check_array("loss", loss, dev, f32, 1)
     ld_grad = 0
     if grad is not None:
         gn, gv, ld_grad, gdt = _rows(grad)
-        if (gn, gv, gdt, grad.device) != (n, V, dt, logits.device):
+        if (gn, gv, gdt, grad.get_device()) != (n, V, dt, dev):
             raise DominoError(DOMINO_ERR_INVALID_ARG, "grad must have the logits' shape, type and device")
-    _check_device(logits)
+    _check_device(dev)
     _check(load().domino_distill_loss(n, V, k, _ptr(logits), dt, ld, _ptr(teacher_ids), _ptr(teacher_vals),
                                       _ptr(teacher_rest), float(temperature), _ptr(row_weights), float(grad_scale),
                                       _ptr(loss), _ptr(row_loss), _ptr(grad), ld_grad, _ptr(workspace),
@@ -408,12 +408,15 @@ def domino_sample_logits(logits, uniforms, tokens, workspace, temperature=None, 
     """logits [rows, vocab] with dense rows; every other array [rows] (top_k and tokens int32, the rest fp32)."""
     import torch
     n, V, ld, dt = _rows(logits)
-    for name, t in (("uniforms", uniforms), ("temperature", temperature), ("top_p", top_p), ("min_p", min_p),
-                    ("logprobs", logprobs)):
-        _check_array(name, t, logits, torch.float32, n)
-    for name, t in (("tokens", tokens), ("top_k", top_k)):
-        _check_array(name, t, logits, torch.int32, n)
-    _check_device(logits)
+    dev, f32 = logits.get_device(), torch.float32
+    _check_array("uniforms", uniforms, dev, f32, n)
+    _check_array("temperature", temperature, dev, f32, n)
+    _check_array("top_p", top_p, dev, f32, n)
+    _check_array("min_p", min_p, dev, f32, n)
+    _check_array("logprobs", logprobs, dev, f32, n)
+    _check_array("tokens", tokens, dev, torch.int32, n)
+    _check_array("top_k", top_k, dev, torch.int32, n)
+    _check_device(dev)
     _check(load().domino_sample_logits(n, V, _ptr(logits), dt, ld, _ptr(temperature), _ptr(top_k), _ptr(top_p),
                                        _ptr(min_p), _ptr(uniforms), _ptr(tokens), _ptr(logprobs), _ptr(workspace),
                                        workspace.numel() * workspace.element_size(), _stream(stream)))

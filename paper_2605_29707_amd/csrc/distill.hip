@@ -29,6 +29,7 @@ namespace dk {
 constexpr int kDsThreads = 256;
 constexpr int kDsChunk = 4096;  // vocabulary ids a workgroup
 constexpr int kDsWaves = kDsThreads / 64;
+constexpr int kDsMaxK = 1024;   // entries at most
 
 template <typename LT>
 constexpr int kDsVecs = kDsChunk / kDsThreads / RowVec<LT>::N;
@@ -127,81 +128,132 @@ __global__ __launch_bounds__(kDsThreads) void distill_part_kernel(DistillArgs a,
   if (tid == 0) a.part[(size_t)row * a.nch + ch] = make_float2(bad ? NAN : m, s);
 }
 
-// (2) One row, in 64 bits: a few hundred values, and differences of logarithms.
+// maxima (of NF values) and sums (of ND) over the workgroup, one barrier each; every thread gets them
+template <int NF>
+DEVI void block_maxima(float (&v)[NF], float (*red)[kDsWaves]) {
+#pragma unroll
+  for (int i = 0; i < NF; ++i) v[i] = wave_max(v[i]);
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int i = 0; i < NF; ++i) red[i][threadIdx.x >> 6] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NF; ++i)
+#pragma unroll
+    for (int w = 0; w < kDsWaves; ++w) v[i] = fmaxf(v[i], red[i][w]);
+}
+template <int ND>
+DEVI void block_sums(double (&v)[ND], double (*red)[kDsWaves]) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < ND; ++i) v[i] += __shfl_xor(v[i], o, 64);
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int i = 0; i < ND; ++i) red[i][threadIdx.x >> 6] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < ND; ++i) {
+    v[i] = 0.0;
+#pragma unroll
+    for (int w = 0; w < kDsWaves; ++w) v[i] += red[i][w];
+  }
+}
+
+// (2) One row, in 64 bits: a few hundred values, and differences of logarithms.  Bound by its chain of
+// steps: its loads go out together, an entry's exponentials are formed once, and three barriers
+// part the maxima, the sums and the loss (7.2 us with a barrier for each of them).
 __global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs a) {
+  constexpr int kPer = kDsMaxK / kDsThreads;
   const int row = blockIdx.x, tid = threadIdx.x;
   __shared__ float redf[4][kDsWaves];
   __shared__ double red[4][kDsWaves];
   const float2 *part = a.part + (size_t)row * a.nch;
-  const int32_t *ids = a.ids + (size_t)row * a.k;
-  const float *tv = a.t_vals + (size_t)row * a.k;
-  float *z = a.z + (size_t)row * a.k;
-  const double inv_t = 1.0 / (double)a.T;
-  const double W = a.wsum[0];
-  const float w = ds_weight(a.weights ? a.weights[row] : 1.f);
-  // maxima: the other ids', the entries', the teacher's
-  float mr = -INFINITY, mz = -INFINITY, mt = -INFINITY;
-  float odd = 0.f;
-  for (int c = tid; c < a.nch; c += kDsThreads) {
-    const float x = part[c].x;
-    if (x != x) odd = 1.f;
-    mr = fmaxf(mr, x);
-  }
-  for (int i = tid; i < a.k; i += kDsThreads) {
-    if (ids[i] < 0 || ids[i] >= a.V) continue;
-    mz = fmaxf(mz, z[i]);
-    mt = fmaxf(mt, tv[i]);
-  }
-  mr = block_reduce_max<kDsWaves>(mr, redf[0]);
-  mz = block_reduce_max<kDsWaves>(mz, redf[1]);
-  mt = block_reduce_max<kDsWaves>(mt, redf[2]);
-  const bool bad = block_reduce_max<kDsWaves>(odd, redf[3]) != 0.f;
-  const float rt = a.t_rest ? order_val(a.t_rest[row]) : -INFINITY;
-  // sums relative to the maxima: R / exp(mr / T); Z / exp(m / T); the teacher's over the larger of its two parts
-  double R = 0.0, E = 0.0, P = 0.0;
-  const double tm = fmax((double)mt * inv_t, (double)rt);
-  const float m = fmaxf(mr, mz);
-  for (int c = tid; c < a.nch; c += kDsThreads) {
-    const float2 p = part[c];
-    if (p.x != -INFINITY) R += (double)p.y * exp(((double)p.x - mr) * inv_t);  // (NaN in a row of +inf)
-  }
-  for (int i = tid; i < a.k; i += kDsThreads) {
-    if (ids[i] < 0 || ids[i] >= a.V) continue;
-    if (z[i] != -INFINITY) E += exp(((double)z[i] - m) * inv_t);
-    const double t = (double)order_val(tv[i]) * inv_t;
-    if (t != -INFINITY) P += exp(t - tm);
-  }
-  R = block_reduce_sum<kDsWaves>(R, red[0]);
-  E = block_reduce_sum<kDsWaves>(E, red[1]);
-  P = block_reduce_sum<kDsWaves>(P, red[2]);
-  if (rt != -INFINITY) P += exp((double)rt - tm);
-  // logarithms relative to the maxima: beside values near the type's lowest log(V) would be lost
-  const double r_m = ((double)mr - m) * inv_t;
-  double Z = E;
-  if (R != 0.0) Z += R * exp(r_m);
-  const double log_Z = log(Z), log_P = log(P);      // Z = 0: no student logit above -inf
-  const bool none = tm == -INFINITY;                // the teacher says nothing of this row
-  const double scale = W > 0.0 && !none ? (double)a.T * (double)w / W * (double)a.grad_scale : 0.0;
-  double kl = 0.0;
-  for (int i = tid; i < a.k; i += kDsThreads) {
-    double g = 0.0;
-    if (ids[i] >= 0 && ids[i] < a.V) {
-      const double lp = ((double)order_val(tv[i]) * inv_t - tm) - log_P;
-      const double lq = z[i] == -INFINITY ? -INFINITY : ((double)z[i] - m) * inv_t - log_Z;
-      const double p = exp(lp);
-      if (!none && p != 0.0) kl += p * (lp - lq);
-      g = scale * (exp(lq) - p);
+  const size_t r0 = (size_t)row * a.k;
+  float *z = a.z + r0;
+  // entry i of thread i % 256: student's and teacher's logit, -inf where there is none
+  float zi[kPer], ti[kPer];
+  uint32_t used = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    zi[j] = ti[j] = -INFINITY;
+    const int i = j * kDsThreads + tid;
+    if (i < a.k) {
+      const int id = a.ids[r0 + i];
+      const float zv = z[i], tv = a.t_vals[r0 + i];
+      if (id >= 0 && id < a.V) {  // (another one's z is not set)
+        used |= 1u << j;
+        zi[j] = zv;
+        ti[j] = order_val(tv);
+      }
     }
-    z[i] = scale == 0.0 ? 0.f : bad ? NAN : (float)g;  // the entry's value is read, its gradient takes its place
   }
-  kl = block_reduce_sum<kDsWaves>(kl, red[3]);
+  const double W = a.wsum[0], odd_weights = a.wsum[1];
+  const float w = ds_weight(a.weights ? a.weights[row] : 1.f), rt = a.t_rest ? order_val(a.t_rest[row]) : -INFINITY;
+  // the first chunks' pairs, one a thread; the others below
+  const float2 p0 = tid < a.nch ? part[tid] : make_float2(-INFINITY, 0.f);
+  const double inv_t = 1.0 / (double)a.T;
+  // maxima: the other ids', the entries', the teacher's; whether an id was bad
+  float mx[4] = {p0.x, -INFINITY, -INFINITY, p0.x != p0.x ? 1.f : 0.f};
+  for (int c = kDsThreads + tid; c < a.nch; c += kDsThreads) {
+    const float x = part[c].x;
+    mx[3] = x != x ? 1.f : mx[3];
+    mx[0] = fmaxf(mx[0], x);
+  }
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    mx[1] = fmaxf(mx[1], zi[j]);
+    mx[2] = fmaxf(mx[2], ti[j]);
+  }
+  mx[0] = fmaxf(mx[0], -INFINITY);  // (a NaN is not a maximum)
+  block_maxima(mx, redf);
+  const float mr = mx[0], m = fmaxf(mx[0], mx[1]);
+  const bool bad = mx[3] != 0.f;
+  const double tm = fmax((double)mx[2] * inv_t, (double)rt);
+  const bool none = tm == -INFINITY;  // the teacher says nothing of this row
+  // sums relative to the maxima: R / exp(mr / T), the entries' part of Z / exp(m / T), P / exp(tm)
+  double e[kPer], pe[kPer], sum[3] = {0.0, 0.0, 0.0};
+  if (p0.x != -INFINITY) sum[0] = (double)p0.y * exp(((double)p0.x - mr) * inv_t);  // (NaN in a row of +inf)
+  for (int c = kDsThreads + tid; c < a.nch; c += kDsThreads) {
+    const float2 p = part[c];
+    if (p.x != -INFINITY) sum[0] += (double)p.y * exp(((double)p.x - mr) * inv_t);
+  }
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    e[j] = pe[j] = 0.0;
+    if (j * kDsThreads < a.k) {  // uniform
+      if (zi[j] != -INFINITY) e[j] = exp(((double)zi[j] - m) * inv_t);
+      if (ti[j] != -INFINITY) pe[j] = exp((double)ti[j] * inv_t - tm);
+      sum[1] += e[j];
+      sum[2] += pe[j];
+    }
+  }
+  block_sums(sum, red);
+  const double R = sum[0], P = sum[2] + (rt != -INFINITY ? exp((double)rt - tm) : 0.0);
+  // logarithms relative to the maxima: beside values near the type's lowest log(V) would be lost
+  const double r_m = ((double)mr - m) * inv_t, Zr = R != 0.0 ? R * exp(r_m) : 0.0, Z = sum[1] + Zr;
+  const double log_Z = log(Z), log_P = log(P);  // Z = 0: no student logit above -inf
+  const double scale = W > 0.0 && !none ? (double)a.T * (double)w / W * (double)a.grad_scale : 0.0;
+  double kl[1] = {0.0};
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    if (j * kDsThreads >= a.k) break;  // uniform
+    const double p = pe[j] / P, q = zi[j] == -INFINITY ? 0.0 : e[j] / Z;
+    const double lp = ((double)ti[j] * inv_t - tm) - log_P;
+    const double lq = zi[j] == -INFINITY ? -INFINITY : ((double)zi[j] - m) * inv_t - log_Z;
+    if ((used >> j & 1) && !none && p != 0.0) kl[0] += p * (lp - lq);
+    const int i = j * kDsThreads + tid;
+    if (i < a.k)  // the entry's value is read, its gradient takes its place
+      z[i] = scale == 0.0 ? 0.f : bad ? NAN : used >> j & 1 ? (float)(scale * (q - p)) : 0.f;
+  }
+  block_sums(kl, red + 3);
   if (tid == 0) {
     const double lpr = ((double)rt - tm) - log_P, lqr = R == 0.0 ? -INFINITY : r_m + (log(R) - log_Z);
     const double pr = none || rt == -INFINITY ? 0.0 : exp(lpr);
-    if (!none && pr != 0.0) kl += pr * (lpr - lqr);
-    const double loss = bad ? NAN : none ? 0.0 : (double)a.T * (double)a.T * kl;
+    if (!none && pr != 0.0) kl[0] += pr * (lpr - lqr);
+    const double loss = bad ? NAN : none ? 0.0 : (double)a.T * (double)a.T * kl[0];
     if (bad) raise_error(a.err, DEV_BAD_TOKEN);
-    if (row == 0 && a.wsum[1] != 0.0) raise_error(a.err, DEV_BAD_PARAM);
+    if (row == 0 && odd_weights != 0.0) raise_error(a.err, DEV_BAD_PARAM);
     a.row_loss[row] = (float)loss;
     a.share[row] = w > 0.f ? (double)w / W * loss : 0.0;
     // of any other id: exp((l - mr) / T) times this

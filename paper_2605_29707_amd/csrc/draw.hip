@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
   float rm = 0.f;
   double rs = 0.0;
   select_top<LT, NR>((const LT *)a.logits + (size_t)row * a.ld, a.groups + (size_t)row * a.G, a.V, a.G, C,
-                     row_scale(d.T), sh, rm, rs);
+                     row_scale(d.T), !d.has_k || d.top_k > C, sh, rm, rs);
   d.set_max(entry_value(sh.list[0]));
   if (d.m == -INFINITY) {  // nothing to draw from
     if (tid == 0) d.finish(p, row, -1, -INFINITY);

@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kSelThreads) void top_select_kernel(RowsArgs a, int
   float rm = 0.f;
   double rs = 0.0;
   select_top<LT, NR>((const LT *)a.logits + (size_t)row * a.ld, a.groups + (size_t)row * a.G, a.V, a.G, k, row_scale(a.T),
-                     sh, rm, rs);
+                     rest != nullptr, sh, rm, rs);
   for (int i = tid; i < k; i += kSelThreads) {
     const unsigned long long key = sh.list[i];
     ids[(size_t)row * k + i] = (int32_t)entry_id(key);

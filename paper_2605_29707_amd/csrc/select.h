@@ -120,7 +120,7 @@ struct Cut {
 // A cut that takes at least `want` items, and at most `cap` (want <= cap): by counts in 512
 // equal parts of [lo, hi], which holds the key of the want-th, and again of the part that holds
 // it while there are more than `cap` up to its end; among equal keys the same by ids.
-// each(f) calls f(key, id) for every item.
+// each(f) calls f(key, id) for every item.  sh.hist is clear, before and after.
 template <typename Each>
 DEVI Cut cut_at(uint32_t lo, uint32_t hi, int want, int cap, SelShared &sh, Each each) {
   const int tid = threadIdx.x;
@@ -130,14 +130,13 @@ DEVI Cut cut_at(uint32_t lo, uint32_t hi, int want, int cap, SelShared &sh, Each
   while (true) {
     const uint32_t range = hi - lo;
     const int shift = range < kSelThreads ? 0 : 32 - kSelLog - __builtin_clz(range);
-    sh.hist[tid] = 0;
-    __syncthreads();
     each([&](uint32_t k, uint32_t id) {
       const uint32_t x = by_id ? kIdMask - id : k;
       if (x >= lo && x <= hi && (!by_id || k == key)) atomicAdd(&sh.hist[kSelThreads - 1 - ((x - lo) >> shift)], 1u);
     });
     __syncthreads();
     const int c = sh.hist[tid];
+    sh.hist[tid] = 0;  // (for the next counts, after a barrier)
     const int n = above + block_scan<kSelWaves, uint32_t>(c, sh.wave[0]);
     if (n >= want && n - c < want) {  // one thread of all
       sh.hit[0] = kSelThreads - 1 - tid;
@@ -161,11 +160,11 @@ DEVI Cut cut_at(uint32_t lo, uint32_t hi, int want, int cap, SelShared &sh, Each
   }
 }
 
-// The first C entries of a row, sorted, in sh.list; of the others the largest value (rest_m)
-// and the sum of exp((l - rest_m) / T) (rest_s).  C <= min(V, kTopMax); a thread holds NR groups.
+// The first C entries of a row, sorted, in sh.list; where it is wanted, of the others the largest value
+// (rest_m) and the sum of exp((l - rest_m) / T) (rest_s).  C <= min(V, kTopMax); a thread holds NR groups.
 template <typename LT, int NR>
-DEVI void select_top(const LT *lr, const float2 *groups, int V, int G, int C, float c, SelShared &sh, float &rest_m,
-                     double &rest_s) {
+DEVI void select_top(const LT *lr, const float2 *groups, int V, int G, int C, float c, bool want_rest, SelShared &sh,
+                     float &rest_m, double &rest_s) {
   constexpr int N = RowVec<LT>::N, LPG = kGroup / N;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // the groups, group i * 512 + tid in register i (loads at clamped places, so that none waits for another)
@@ -204,6 +203,7 @@ DEVI void select_top(const LT *lr, const float2 *groups, int V, int G, int C, fl
     sh.wave[0][wave] = lo;
     sh.wave[1][wave] = hi;
   }
+  sh.hist[tid] = 0;
   if (tid == 0) sh.n = 0;
   __syncthreads();
 #pragma unroll
@@ -309,6 +309,7 @@ DEVI void select_top(const LT *lr, const float2 *groups, int V, int G, int C, fl
   }
   const int n = sh.n;
   sort_list<kSelWaves>(n, sh.list);
+  if (!want_rest) return;
   // The rest: the groups not read, the values not listed, the list behind C.
 #pragma unroll
   for (int i = 0; i < NR; ++i)
