@@ -240,6 +240,7 @@ struct WholeShared {
   };
   unsigned long long redu[2][kWholeWaves];
   unsigned long long hit[2];
+  uint32_t sort[kWholeThreads], red[kWholeWaves];  // of sort_list
   int hit_i, last, n[2], wave_n[2][kWholeWaves];
 };
 static_assert(sizeof(WholeShared) <= 65536, "two workgroups a CU, static LDS");
@@ -379,8 +380,8 @@ DEVI bool collect(const LT *lr, uint32_t V, const Between &A, const Between &B, 
 }
 // The entries of a collected list that `on` takes (by digits) and that have a weight, as keys in descending order; their number.
 template <typename LT, typename On>
-DEVI int pack_list(const LT *lr, uint32_t V, const DrawRow &s, unsigned long long *list, const int *wave_n, WholeShared &sh,
-                   int slot, On on) {
+DEVI int pack_list(const LT *lr, uint32_t V, const DrawRow &s, unsigned long long *list, const Between &of, const int *wave_n,
+                   WholeShared &sh, int slot, On on) {
   constexpr int kTwo = kListMax / kWholeThreads;
   const int tid = threadIdx.x;
   unsigned long long k[kTwo];
@@ -401,7 +402,7 @@ DEVI int pack_list(const LT *lr, uint32_t V, const DrawRow &s, unsigned long lon
     if (k[j]) list[atomicAdd(&sh.n[slot], 1)] = k[j];
   __syncthreads();
   const int n = sh.n[slot];
-  sort_list<kWholeWaves>(n, list);
+  sort_list<kWholeWaves>(n, list, order_key(of.lo), order_key(of.hi), sh.sort, sh.red);
   return n;
 }
 
@@ -479,8 +480,9 @@ DEVI Prefix find_in_row(const LT *lr, uint32_t V, const DrawRow &s, bool by_coun
   for (int level = 0;; ++level) {
     set_digit(at, level, bin.i);
     const uint32_t from = at.y, to = at.y + (level == 0 ? kSplit : 1);
-    if (collect<LT>(lr, V, Between::of(s, from, to), also, sh)) {
-      const int n = pack_list(lr, V, s, sh.list, sh.wave_n[0], sh, 0, [&](const Digits &d) { return near(d, at, level + 1); });
+    const Between of = Between::of(s, from, to);
+    if (collect<LT>(lr, V, of, also, sh)) {
+      const int n = pack_list(lr, V, s, sh.list, of, sh.wave_n[0], sh, 0, [&](const Digits &d) { return near(d, at, level + 1); });
       return pass_in_list(s, sh.list, n, by_count, target, bin.m0, bin.n0, sh);
     }
     also = Between::none();
@@ -498,7 +500,7 @@ DEVI Prefix find_in_row(const LT *lr, uint32_t V, const DrawRow &s, bool by_coun
       __syncthreads();
       const int n = sh.n[0];
       if (n <= kListMax) {  // (at the last level a part is one entry)
-        sort_list<kWholeWaves>(n, sh.list);
+        sort_list<kWholeWaves>(n, sh.list, order_key(of.lo), order_key(of.hi), sh.sort, sh.red);
         return pass_in_list(s, sh.list, n, by_count, target, bin.m0, bin.n0, sh);
       }
     }
@@ -696,7 +698,7 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
     bool end = step == 2;
     if (!end) total = f.mass;
     if (also.some()) {
-      const int n = pack_list(lr, a.V, d, sh.draw, sh.wave_n[1], sh, 1, [&](const Digits &x) { return x.y >> kSplitLog == (uint32_t)next.i; });
+      const int n = pack_list(lr, a.V, d, sh.draw, also, sh.wave_n[1], sh, 1, [&](const Digits &x) { return x.y >> kSplitLog == (uint32_t)next.i; });
       f = pass_in_list(d, sh.draw, n, false, drawn(total), next.m0, next.n0, sh);
       end = true;
     }

@@ -51,35 +51,73 @@ DEVI T block_scan(T v, T *red) {
   return base + v;
 }
 
-// list[0 .. n), n <= kListMax, in descending order (keys are distinct), by W waves.  Up to 512 (or two
-// a thread) a key counts those before it, by several threads where there are enough; more by a
-// bitonic network, whose short steps stay within a wave and need no barrier.
+// list[0 .. n), n <= kListMax, in descending order (keys are distinct, their upper halves in [lo, hi]), by
+// W waves.  Up to 128 a key counts those before it, by several threads where there are enough.  More
+// are dealt into as many equal parts of [lo, hi] as there are threads, and a key counts those before it in
+// its part (270 keys in 2.5K cycles; all against all, 11K beside another workgroup).  Where a part holds
+// many, as of equal values, a bitonic network, whose short steps stay within a wave and need no barrier.
+constexpr int kPartMax = 64;
 template <int W>
-DEVI void sort_list(int n, unsigned long long *list) {
-  constexpr int kThreads = 64 * W;
+DEVI void sort_list(int n, unsigned long long *list, uint32_t lo, uint32_t hi, uint32_t *hist, uint32_t *red) {
+  constexpr int kThreads = 64 * W, kEach = kListMax / kThreads, kLog = W == 16 ? 10 : 9;
+  static_assert(W == 8 || W == 16, "log2 of the threads");
   const int tid = threadIdx.x;
   if (tid == 0) list[n] = 0;  // (before every key; the place behind the longest list is there)
+  hist[tid] = 0;
   __syncthreads();
-  if (n <= min(512, 2 * kThreads)) {
+  if (n <= 128) {
     int lg = 0;
     while (lg < 4 && (n << (lg + 1)) <= kThreads) ++lg;
-    const int i = tid >> lg, parts = 1 << lg, j = i + kThreads;  // (j: only with one part)
-    const unsigned long long k = i < n ? list[i] : ~0ull, l = lg == 0 && j < n ? list[j] : ~0ull;
-    int r = 0, s = 0;
+    const int i = tid >> lg, parts = 1 << lg;
+    const unsigned long long k = i < n ? list[i] : ~0ull;
+    int r = 0;
 #pragma unroll 4
-    for (int q = (tid & ~63) >> lg < n ? 2 * (tid & (parts - 1)) : n; q < n; q += 2 * parts) {  // (a wave without keys: none)
-      const unsigned long long a = list[q], b = list[q + 1];
-      r += (a > k) + (b > k);
-      s += (a > l) + (b > l);
-    }
+    for (int q = (tid & ~63) >> lg < n ? 2 * (tid & (parts - 1)) : n; q < n; q += 2 * parts)  // (a wave without keys: none)
+      r += (list[q] > k) + (list[q + 1] > k);
     for (int o = 1; o < parts; o <<= 1) r += __shfl_xor(r, o, 64);
     __syncthreads();
     if (i < n && (tid & (parts - 1)) == 0) list[r] = k;
-    if (lg == 0 && j < n) list[s] = l;
     __syncthreads();
     return;
   }
-  int size = 512;
+  const uint32_t range = hi - lo;
+  const int shift = range < kThreads ? 0 : 32 - kLog - __builtin_clz(range);
+  unsigned long long k[kEach];
+  int part[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int i = j * kThreads + tid;
+    if (i < n) {
+      k[j] = list[i];
+      part[j] = kThreads - 1 - (int)(((uint32_t)(k[j] >> 32) - lo) >> shift);
+      atomicAdd(&hist[part[j]], 1u);
+    }
+  }
+  __syncthreads();
+  const uint32_t c = hist[tid], before = block_scan<W>(c, red) - c;
+  const bool many = __syncthreads_or(c > kPartMax);
+  if (!many) {
+    hist[tid] = before;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (j * kThreads + tid < n) list[atomicAdd(&hist[part[j]], 1u)] = k[j];  // (then hist has the parts' ends)
+    __syncthreads();
+    int r[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (j * kThreads + tid < n) {
+        r[j] = part[j] ? hist[part[j] - 1] : 0;
+        for (int q = r[j]; q < (int)hist[part[j]]; ++q) r[j] += list[q] > k[j];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (j * kThreads + tid < n) list[r[j]] = k[j];
+    __syncthreads();
+    return;
+  }
+  int size = 256;
   while (size < n) size <<= 1;
   for (int i = n + tid; i < size; i += kThreads) list[i] = 0;
   __syncthreads();
@@ -308,7 +346,7 @@ DEVI void select_top(const LT *lr, const float2 *groups, int V, int G, int C, fl
     if (sh.n <= kListMax) break;
   }
   const int n = sh.n;
-  sort_list<kSelWaves>(n, sh.list);
+  sort_list<kSelWaves>(n, sh.list, ec.key, hi, sh.hist, sh.wave[0]);
   if (!want_rest) return;
   // The rest: the groups not read, the values not listed, the list behind C.
 #pragma unroll
