@@ -160,16 +160,20 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
   }
   if (tid < 4) first[tid] = C;
   unsigned long long r = block_scan<kSelWaves>(sum, redu) - sum;
-  auto each = [&](auto f) {  // f(entry, its value, weight)
+  // the first entry that on(entry, its value, weight) takes, by one lane of each wave (entries are in the lanes' order)
+  auto first_of = [&](int slot, auto on) {
+    int i = C;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j)
-      if (j < per && tid * per + j < C) f(tid * per + j, v[j], w[j]);
+    for (int j = kPer - 1; j >= 0; --j)
+      if (j < per && tid * per + j < C && on(tid * per + j, v[j], w[j])) i = tid * per + j;
+    const unsigned long long mk = __ballot(i < C);
+    if (mk && (tid & 63) == __ffsll(mk) - 1) atomicMin(&first[slot], i);
   };
-  each([&](int i, float x, unsigned long long wi) {
-    run[i] = r += wi;
-    if (wi == 0ull) atomicMin(&first[0], i);       // ... has no weight
-    if (!d.stays(x)) atomicMin(&first[1], i);      // ... does not stay under min-p
-  });
+#pragma unroll
+  for (int j = 0; j < kPer; ++j)
+    if (j < per && tid * per + j < C) run[tid * per + j] = r += w[j];
+  first_of(0, [&](int, float, unsigned long long wi) { return wi == 0ull; });   // ... has no weight
+  first_of(1, [&](int, float x, unsigned long long) { return !d.stays(x); });   // ... does not stay under min-p
   __syncthreads();
   const unsigned long long sum_c = run[C - 1], kUnknown = ~0ull;
   const int weighty = first[0], n_m = first[1];    // C: all of them
@@ -183,9 +187,7 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
   if (d.use_p) {
     if (!d.has_k || d.top_k <= C || all) {
       const unsigned long long want = (unsigned long long)ceil((double)d.top_p * (double)whole);
-      each([&](int i, float, unsigned long long) {
-        if (run[i] >= want) atomicMin(&first[2], i);
-      });
+      first_of(2, [&](int i, float, unsigned long long) { return run[i] >= want; });
     } else {
       decided = false;  // the sum of the first top_k is not known
     }
@@ -200,9 +202,7 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
   }
   if (decided) {
     const unsigned long long target = (unsigned long long)floor((double)d.u * (double)total);
-    each([&](int i, float, unsigned long long) {
-      if (run[i] > target) atomicMin(&first[3], i);
-    });
+    first_of(3, [&](int i, float, unsigned long long) { return run[i] > target; });
     __syncthreads();
     const int i = first[3];
     if (i < C) {
