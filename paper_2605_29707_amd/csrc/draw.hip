@@ -180,7 +180,7 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
   const bool all = C == a.V || weighty < C;        // no weight lies behind the first C
   // the whole row's sum: of the first C exactly, of the rest from the groups' sums
   unsigned long long whole = sum_c;
-  if (!all && rs != 0.0) whole += (unsigned long long)(rs * exp2(((double)rm - (double)d.m) * d.cd) * kOne);
+  if (!all && rs != 0.0) whole += (unsigned long long)(rs * (rm == d.m ? 1.0 : exp2(((double)rm - (double)d.m) * d.cd)) * kOne);
   unsigned long long total = all ? sum_c : kUnknown;  // the kept prefix's sum
   bool decided = true;
   if (d.has_k && d.top_k <= C) whole = total = min(total, run[d.top_k - 1]);

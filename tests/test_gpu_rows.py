@@ -413,6 +413,28 @@ def test_sample_of_equal_logits_at_exact_borders():
     assert tok.tolist() == [0, 5000, 10000, 19999]
 
 
+@pytest.mark.parametrize("V,n_inf", [(500, 64), (500, 65), (3000, 2500), (151936, 70), (151936, 151936)])
+def test_sample_of_infinities(V, n_inf):
+    """Logits of +inf share all the weight, also where they are more than the first entries looked at.  Their running
+    sums are whole numbers, and u times one of them (24 bits times 18) is exact on both sides: so is the token, on
+    a border too."""
+    n = 9
+    x = _make("normal", n, V, "f32", seed=6)
+    rng = np.random.default_rng(V)
+    for r in range(n):
+        x[r, rng.permutation(V)[:n_inf]] = np.inf
+    u = (rng.integers(0, 60, n) + 0.5) / 60
+    for kw in (dict(), dict(top_k=min(V - 1, 1500)), dict(top_k=30), dict(top_p=0.6), dict(min_p=0.5),
+               dict(top_k=min(V - 1, 1500), top_p=0.3, min_p=0.1)):
+        par = {a: np.full(n, b, np.int64 if a == "top_k" else np.float32) for a, b in kw.items()}
+        par["T"] = np.linspace(0.5, 2, n).astype(np.float32)
+        tok, lp = _sample(_put(x, "f32"), u.astype(np.float32), **par)
+        par["temperature"] = par.pop("T")
+        want = ro.sample_logits(x, u.astype(np.float32), **par)
+        np.testing.assert_array_equal(tok, want["tokens"])
+        np.testing.assert_allclose(lp, want["logprobs"], rtol=2 * HALF["f32"])
+
+
 def test_sample_greedy_rows_and_per_row_filters():
     n, V = 64, 20011
     x = _make("zipf", n, V, "bf16", seed=5)
