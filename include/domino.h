@@ -409,7 +409,7 @@ size_t domino_top_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t k)
  * The first k entries of every row, and what the others weigh: of a teacher's
  * row (domino_target_verify's logits), what distillation keeps.
  *  k               in [1, min(vocab, 1024)]; vocab at most 327680
- *  temperature     T > 0 (finite); it only acts on rest
+ *  temperature     T in [1e-30, 1e30]; it only acts on rest
  *  top_ids         device int32 [rows][k], in order
  *  top_vals        device fp32 [rows][k]: their logits (not divided by T)
  *  rest            optional device fp32 [rows]: log of the sum over every other id
@@ -439,7 +439,7 @@ size_t domino_distill_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
  *  teacher_rest    optional device fp32 [rows]: rest_t, as domino_top_logits gives it
  *                  at the same T; NULL: -inf, the teacher is its entries alone
  *                  A row whose teacher has no weight at all has loss and gradient 0.
- *  temperature     T > 0 (finite)
+ *  temperature     T in [1e-30, 1e30]
  *  row_weights     optional device fp32 [rows]: w >= 0 and finite, NULL: 1.  A row of
  *                  weight 0 adds nothing to the loss and its gradient is 0, whatever it
  *                  holds; another value sets DOMINO_DEV_BAD_PARAM and counts as 0.
@@ -471,9 +471,10 @@ size_t domino_sample_logits_workspace_bytes(int32_t rows, int32_t vocab);
  * the first n = min(n_k, n_p, n_m) are kept, S the sum of their e; the token is the
  * first whose running sum exceeds u S, its log-probability log(e / S).  Logits of +inf
  * share all the weight.  e is held to 2^-45 (a lighter entry is never drawn) and summed as whole
- * numbers, so the token does not depend on the order of the sums.
+ * numbers, so the token does not depend on the order of the sums.  (Where a filter or the draw ends within a
+ * row's first 64 entries, what lies behind them counts by single-precision exponentials, within 4e-6 of it.)
  *  vocab           at most 327680
- *  temperature     optional device fp32 [rows]: T >= 0, finite; NULL: 1.  0: the first
+ *  temperature     optional device fp32 [rows]: T in [1e-30, 1e30], NULL: 1.  0: the first
  *                  entry of the order, whatever the filters
  *  top_k           optional device int32 [rows]
  *  top_p, min_p    optional device fp32 [rows], in [0, 1]

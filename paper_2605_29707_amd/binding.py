@@ -346,11 +346,13 @@ def _check_array(name, t, device, dtype, n):
                           f"{name} must be a contiguous {dtype} tensor of {n} elements on the logits' device")
 
 
-def _check_device(device):
+def _check_device(device, workspace):
     """Work is launched on the current device: tensors of another one are refused."""
     import torch
     if device < 0 or device != torch.cuda.current_device():
         raise DominoError(DOMINO_ERR_INVALID_ARG, "logits must be on the current GPU")
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "workspace must be a contiguous tensor on the logits' device")
 
 
 def domino_top_logits_workspace_bytes(rows, vocab, k) -> int:
@@ -365,7 +367,7 @@ def domino_top_logits(logits, top_ids, top_vals, workspace, rest=None, temperatu
     _check_array("top_ids", top_ids, dev, torch.int32, n * k)
     _check_array("top_vals", top_vals, dev, torch.float32, n * k)
     _check_array("rest", rest, dev, torch.float32, n)
-    _check_device(dev)
+    _check_device(dev, workspace)
     _check(load().domino_top_logits(n, V, k, _ptr(logits), dt, ld, float(temperature), _ptr(top_ids), _ptr(top_vals),
                                     _ptr(rest), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                     _stream(stream)))
@@ -392,7 +394,7 @@ def domino_distill_loss(logits, teacher_ids, teacher_vals, loss, workspace, teac
         gn, gv, ld_grad, gdt = _rows(grad)
         if (gn, gv, gdt, grad.get_device()) != (n, V, dt, dev):
             raise DominoError(DOMINO_ERR_INVALID_ARG, "grad must have the logits' shape, type and device")
-    _check_device(dev)
+    _check_device(dev, workspace)
     _check(load().domino_distill_loss(n, V, k, _ptr(logits), dt, ld, _ptr(teacher_ids), _ptr(teacher_vals),
                                       _ptr(teacher_rest), float(temperature), _ptr(row_weights), float(grad_scale),
                                       _ptr(loss), _ptr(row_loss), _ptr(grad), ld_grad, _ptr(workspace),
@@ -416,7 +418,7 @@ def domino_sample_logits(logits, uniforms, tokens, workspace, temperature=None, 
     _check_array("logprobs", logprobs, dev, f32, n)
     _check_array("tokens", tokens, dev, torch.int32, n)
     _check_array("top_k", top_k, dev, torch.int32, n)
-    _check_device(dev)
+    _check_device(dev, workspace)
     _check(load().domino_sample_logits(n, V, _ptr(logits), dt, ld, _ptr(temperature), _ptr(top_k), _ptr(top_p),
                                        _ptr(min_p), _ptr(uniforms), _ptr(tokens), _ptr(logprobs), _ptr(workspace),
                                        workspace.numel() * workspace.element_size(), _stream(stream)))

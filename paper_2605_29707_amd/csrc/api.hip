@@ -1311,7 +1311,9 @@ domino_status check_workspace(const void *ws, size_t have, size_t need) {
   if (have < need) return fail(DOMINO_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", have, need);
   return DOMINO_OK;
 }
-bool temperature_ok(float t) { return t > 0.f && std::isfinite(t) && 1.0f / t <= 1e30f; }
+domino_status check_temperature(float t) {
+  return row_temperature_ok(t) ? DOMINO_OK : fail(DOMINO_ERR_INVALID_ARG, "temperature must be in [1e-30, 1e30]");
+}
 }  // namespace
 
 size_t domino_top_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t k) {
@@ -1324,7 +1326,7 @@ domino_status domino_top_logits(int32_t rows, int32_t vocab, int32_t k, const vo
                                 void *workspace, size_t workspace_bytes, void *stream) {
   if (domino_status s = check_rows(rows, vocab, logits, logits_dtype, ld); s != DOMINO_OK) return s;
   if (k < 1 || k > 1024 || k > vocab) return fail(DOMINO_ERR_INVALID_ARG, "k must be in [1, 1024] and at most vocab");
-  if (!temperature_ok(temperature)) return fail(DOMINO_ERR_INVALID_ARG, "temperature must be positive and finite");
+  if (domino_status s = check_temperature(temperature); s != DOMINO_OK) return s;
   if (!top_ids || !top_vals) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
   if (!rows_supported(rows, vocab))
     return fail(DOMINO_ERR_UNSUPPORTED, "vocab must be at most %d and rows at most %ld", kRowsMaxVocab, kMaxBlocks / 64);
@@ -1385,7 +1387,7 @@ domino_status domino_distill_loss(int32_t rows, int32_t vocab, int32_t k, const 
                                   void *workspace, size_t workspace_bytes, void *stream) {
   if (domino_status s = check_rows(rows, vocab, logits, logits_dtype, ld); s != DOMINO_OK) return s;
   if (k < 1 || k > 1024 || k > vocab) return fail(DOMINO_ERR_INVALID_ARG, "k must be in [1, 1024] and at most vocab");
-  if (!temperature_ok(temperature)) return fail(DOMINO_ERR_INVALID_ARG, "temperature must be positive and finite");
+  if (domino_status s = check_temperature(temperature); s != DOMINO_OK) return s;
   if (!std::isfinite(grad_scale)) return fail(DOMINO_ERR_INVALID_ARG, "grad_scale must be finite");
   if (!teacher_ids || !teacher_vals || !loss) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
   if (grad && ((uintptr_t)grad % (logits_dtype == DOMINO_BF16 ? 2 : 4) || ld_grad < vocab))

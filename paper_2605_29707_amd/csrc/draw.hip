@@ -82,7 +82,7 @@ struct DrawRow {
     top_p = p.top_p ? p.top_p[row] : 1.f;
     min_p = p.min_p ? p.min_p[row] : 0.f;
     top_k = p.top_k ? p.top_k[row] : 0;
-    ok = T >= 0.f && T < INFINITY && u >= 0.f && u < 1.f && top_p >= 0.f && top_p <= 1.f && min_p >= 0.f && min_p <= 1.f;
+    ok = (T == 0.f || row_temperature_ok(T)) && u >= 0.f && u < 1.f && top_p >= 0.f && top_p <= 1.f && min_p >= 0.f && min_p <= 1.f;
     if (T == 0.f) {
       top_k = 1;
       T = 1.f;
@@ -94,7 +94,7 @@ struct DrawRow {
   DEVI void set_max(float max) {
     m = max;
     cd = scalar(1.44269504088896340736 / (double)T);
-    cf = scalar(fminf((float)(cd * (double)(1 << (kBinsLog + kSplitLog))), 1e30f));
+    cf = scalar((float)(cd * (double)(1 << (kBinsLog + kSplitLog))));
     min_d = scalar(use_m ? -log((double)min_p) * (double)T : (double)INFINITY);
   }
   // of a value that is no NaN; logits of +inf have all the weight

@@ -254,7 +254,11 @@ void launch_verify_sample(int bs, int B, int V, const int32_t *node_token, const
 void launch_philox_words(const uint32_t *ctr, uint64_t key, uint32_t *out, int n, hipStream_t st);
 
 // ---- rows of logits: their groups and top entries (logits.hip)
-constexpr int kRowsMaxVocab = 327680;  // ten groups of 32 ids in the registers of each of 1024 threads
+constexpr int kRowsMaxVocab = 327680;  // 20 groups of 32 ids in the registers of each of 512 threads
+// A difference of logits over T in single precision: its factor is finite, also in units of the sampler's
+// bins (2^17 log2(e) / T), and a difference that overflows (above 2^128) has no weight left (exp(-2^28)).
+constexpr float kRowsMinT = 1e-30f, kRowsMaxT = 1e30f;
+__host__ __device__ inline bool row_temperature_ok(float T) { return T >= kRowsMinT && T <= kRowsMaxT; }
 struct RowsArgs {
   int rows, V;
   const void *logits;  // rows ld elements apart

@@ -461,6 +461,35 @@ def test_sample_parameters_out_of_range():
     assert np.all(tok[1:] == -1) and np.isnan(lp[1:]).all() and np.isfinite(lp[0])
 
 
+def test_sample_temperatures_at_the_ends_of_their_range():
+    """1e-30 over logits 1e-32 apart: a hundred entries an e-fold.  1e30: what is not -inf or the type's lowest
+    is equal.  Past them: refused."""
+    n, V = 6, 4096
+    u = np.linspace(0.05, 0.9, n)
+    x = np.tile((-1e-32 * np.arange(V)).astype(np.float32), (n, 1))
+    for kw in (dict(), dict(top_p=0.8), dict(min_p=0.3), dict(top_k=200)):
+        _check_sample(x, u, T=np.full(n, 1e-30), **kw)
+    y = _make("normal", n, V, "f32", seed=2)
+    y[:, ::3], y[:, 1::3] = -np.inf, LOWEST["f32"]
+    for kw in (dict(), dict(top_p=0.8), dict(top_k=1200)):
+        want = _check_sample(y, u, T=np.full(n, 1e30), **kw)
+        assert np.all(want["tokens"] % 3 == 2)
+    T = np.array([0.9e-30, 1.1e30, 1.0, 1e-38, 3e38, 1e-45], np.float32)
+    tok, _ = _sample(_put(y, "f32"), u.astype(np.float32), T, error=bd.DEV_BAD_PARAM)
+    assert (tok >= 0).tolist() == [False, False, True, False, False, False]
+
+
+@pytest.mark.parametrize("kind,V,dtype", [("normal", 151936, "f32"), ("falling", 151936, "bf16"), ("close", 262144, "f32")])
+def test_sample_few_flat_rows(kind, V, dtype):
+    """Rows that several workgroups share, their filters' borders far behind the first entries and, in rows in
+    falling order, a border's entries side by side."""
+    n = 4
+    x = _make(kind, n, V, dtype, seed=11)
+    rng = np.random.default_rng(V)
+    for kw in (dict(), dict(top_p=0.9), dict(top_k=30000, top_p=0.5, min_p=0.01), dict(top_k=100000), dict(min_p=0.3)):
+        _check_sample(x, rng.random(n), T=np.linspace(2, 4, n), dtype=dtype, **kw)
+
+
 # --------------------------------------------------------------------------
 # streams, graphs, and all of them together
 # --------------------------------------------------------------------------
@@ -482,6 +511,38 @@ def test_two_streams_at_once():
     for i in (0, 1):
         alone = _sample(lgs[i], u.cpu().numpy(), top_p=0.9)[0]
         np.testing.assert_array_equal(toks[i].cpu().numpy(), alone)
+
+
+def test_rows_past_32_bit_offsets():
+    """The second row begins 2^31 + 3 values after the first, for reading and for the gradient."""
+    V, k, ld = 20000, 16, 2**31 + 3
+    x = _make("zipf", 2, V, "bf16", seed=1)
+    big, gbig = (torch.empty(ld + V, dtype=torch.bfloat16, device=DEV).as_strided((2, V), (ld, 1)) for _ in range(2))
+    big.copy_(torch.from_numpy(x))
+    near = _put(x, "bf16")
+    ids, vals, rest = _top(big, k)
+    for a, b in zip((ids, vals, rest), _top(near, k)):
+        np.testing.assert_array_equal(a, b)
+    u = np.array([0.3, 0.99], np.float32)
+    for T in (0.7, 4.0):
+        for a, b in zip(_sample(big, u, np.full(2, T), top_p=0.95), _sample(near, u, np.full(2, T), top_p=0.95)):
+            np.testing.assert_array_equal(a, b)
+    want = _distill(near, ids, vals, rest, 2.0)
+    loss, ws = torch.empty(1, device=DEV), torch.empty(bd.domino_distill_workspace_bytes(2, V, k), dtype=torch.uint8, device=DEV)
+    bd.domino_distill_loss(big, _t(ids, torch.int32), _t(vals), loss, ws, teacher_rest=_t(rest), temperature=2.0, grad=gbig)
+    torch.cuda.synchronize()
+    assert float(loss[0]) == want[0]
+    np.testing.assert_array_equal(gbig.float().cpu().numpy(), want[2])
+
+
+def test_a_workspace_elsewhere_is_refused():
+    lg = _put(_make("normal", 2, 100, "f32"), "f32")
+    tok = torch.empty(2, dtype=torch.int32, device=DEV)
+    nb = bd.domino_sample_logits_workspace_bytes(2, 100)
+    for ws in (torch.empty(nb, dtype=torch.uint8), torch.empty(2 * nb, dtype=torch.uint8, device=DEV)[::2]):
+        with pytest.raises(bd.DominoError) as e:
+            bd.domino_sample_logits(lg, torch.zeros(2, device=DEV), tok, ws)
+        assert e.value.status == bd.DOMINO_ERR_INVALID_ARG
 
 
 def test_captured_calls_replay_on_new_inputs():

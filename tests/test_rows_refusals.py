@@ -26,7 +26,7 @@ DISTILL = dict(rows=3, vocab=100, k=5, logits=P, dtype=0, ld=100, ids=P, vals=P,
 ROWS = [(dict(rows=0), INV), (dict(rows=-1), INV), (dict(vocab=0), INV), (dict(dtype=2), INV), (dict(logits=None), INV),
         (dict(ld=99), INV), (dict(logits=C.c_void_p(4097)), INV), (dict(ws=None), WS), (dict(nbytes=8), WS),
         (dict(ws=C.c_void_p(4100)), WS)]
-BAD_T = [(dict(T=t), INV) for t in (0.0, -1.0, float("nan"), float("inf"), 1e-38)]
+BAD_T = [(dict(T=t), INV) for t in (0.0, -1.0, float("nan"), float("inf"), 1e-38, 0.9e-30, 1.1e30)]
 
 
 @pytest.mark.parametrize("kw,status", ROWS + BAD_T + [
