@@ -1,10 +1,11 @@
 // The top entries of rows of logits: one pass over a row for the maximum and the sum of exp of
 // its groups of 32 ids, then a workgroup a row that selects from those (select.h).
 //   groups  bound by the logits' bytes: 16-byte loads, a group in the registers of 4 (bf16)
-//           or 8 (fp32) lanes
+//           or 8 (fp32) lanes (960 rows of 151936 bf16 logits 63.6 us, 4.6 TB/s)
 //   top     the first C groups' values in registers, those that can be among the first C entries
 //           sorted in LDS; the sum of the rest from the other groups' sums and the registers, never as
-//           a total less the entries
+//           a total less the entries.  At few rows bound by the chain of its steps (one row of 128 groups
+//           6.8 us, 16 of 4748 12), at many by their instructions (960 rows, 256 entries 42 us)
 #include <type_traits>
 
 #include "common.h"
