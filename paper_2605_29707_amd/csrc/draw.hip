@@ -14,7 +14,7 @@
 //   whole   the other rows (flat ones, whose kept entries or draw lie behind the first 64), several
 //           workgroups a row: sums of e by bins of log2 e, in LDS, then added in memory; the last
 //           workgroup to finish a row finds the bin where a running sum passes its target, and the entry
-//           among the bin's, sorted, or first by parts of the bin while they are too many.  Bound by the
+//           among the bin's, sorted, or first by parts of their range while they are too many.  Bound by the
 //           polynomials and LDS atomics of the sums, then by one CU's pass over a row for each border (64 of
 //           512 rows of 151936 bf16 logits flat: 75 us, 21 of them for the sums, 22 a pass).
 #include <algorithm>
@@ -31,7 +31,7 @@ static_assert(kRowsMaxVocab <= 1 << 19, "sums of weights must fit 63 bits");
 constexpr int kBinsLog = 6;                           // bins of 1/64 in log2 of the weight
 constexpr int kBins = (kWeightBits + 2) << kBinsLog;  // a weight past them rounds to 0
 static_assert(sizeof(DrawSums::mass) == kBins * 8, "the bins in memory");
-constexpr int kSplitLog = 11;                         // parts a bin is split into, level by level
+constexpr int kSplitLog = 11;                         // parts of a bin
 constexpr int kSplit = 1 << kSplitLog;
 constexpr int kFirst = 64;                            // entries looked at first where top_k is off
 constexpr int kWholeThreads = 1024;
@@ -107,6 +107,8 @@ struct DrawRow {
   }
   // above every weight of a bin
   DEVI unsigned long long weight_at(int bin) const { return weight_of((double)bin / (1 << kBinsLog)) + (1ull << (kWeightBits - 20)); }
+  // whether a bin of this sum may hold few enough entries for a list
+  DEVI bool few(unsigned long long mass, int bin) const { return mass <= weight_at(bin) * (kListMax * 15 / 16); }
   DEVI bool stays(float v) const { return v == m || (double)m - (double)v <= min_d; }
   DEVI float logprob(float v, unsigned long long total) const {
     return (float)((v == m ? 0.0 : ((double)v - (double)m) / (double)T) - log((double)total / kOne));
@@ -247,77 +249,49 @@ struct WholeShared {
 };
 static_assert(sizeof(WholeShared) <= 65536, "two workgroups a CU, static LDS");
 constexpr int kBinsPer = (kBins + kWholeThreads - 1) / kWholeThreads;  // bins a thread
-constexpr int kSeg = kListMax / kWholeWaves;                          // a wave's part of a list while it is collected
+constexpr int kSeg = 2 * kListMax / kWholeWaves;                      // a wave's part of a list while it is ids
 
 // f(16 bytes of values, first id) for the ids [v0, v1) of a row of at least a vector; -inf follows its last
-// value.  The next loads are on their way meanwhile: they go to clamped places without a branch, since
-// the compiler waits for all loads where one is on some path only (19 us instead of 9 for 38K values).
-template <typename LT, typename F>
+// value.  The next U loads are on their way meanwhile: they go to clamped places without a branch, since
+// the compiler waits for all loads where one is on some path only (19 us instead of 9 for 38K values).  The row's end is
+// in the loop, and its rarer users have U = 1: this code is long, and comes from memory at its first run.
+template <int U, typename LT, typename F>
 DEVI void each_of_row(const LT *lr, uint32_t V, uint32_t v0, uint32_t v1, F f) {
-  constexpr uint32_t N = RowVec<LT>::N, U = 2, step = kWholeThreads * N;
+  constexpr uint32_t N = RowVec<LT>::N, step = kWholeThreads * N;
   u32x4 x[U], y[U];
   auto load = [&](u32x4 (&z)[U], uint32_t c0) {
 #pragma unroll
-    for (uint32_t q = 0; q < U; ++q) z[q] = row_load(lr + min(c0 + q * step + threadIdx.x * N, V - N));
+    for (int q = 0; q < U; ++q) z[q] = row_load(lr + min(c0 + q * step + threadIdx.x * N, V - N));
   };
   load(x, v0);
 #pragma unroll 1
   for (uint32_t c0 = v0; c0 < v1; c0 += U * step) {
     load(y, c0 + U * step);
 #pragma unroll
-    for (uint32_t q = 0; q < U; ++q) {
+    for (int q = 0; q < U; ++q) {
       const uint32_t id = c0 + q * step + threadIdx.x * N;
-      if (id + N <= v1) f(x[q], id);
+      if (id < v1) f(id + N <= V ? x[q] : row_move_end<LT>(x[q], id + N - V), id);
     }
 #pragma unroll
-    for (uint32_t q = 0; q < U; ++q) x[q] = y[q];
+    for (int q = 0; q < U; ++q) x[q] = y[q];
   }
-  const uint32_t whole = v1 / N * N;  // (only the row's end is not whole vectors)
-  if (whole < v1 && threadIdx.x == 0) f(row_load_end(lr, whole, V), whole);
 }
 
-// The order in digits, each ascending: the bin and its part (of the distance to the
-// maximum), the value's key, the id; `level` says which digit, `near` whether those before it agree.
-struct Digits {
-  uint32_t y, k, id;
-};
+// the distance to the maximum in parts of a bin; NaN and -inf are far
 constexpr float kFar = (float)(kBins << kSplitLog);
-// the distance in parts of a bin; NaN and -inf are far
 DEVI float distance(const DrawRow &s, float v) { return (s.m - v) * s.cf; }
-DEVI bool near(const Digits &a, const Digits &b, int level) {
-  const uint32_t my = level == 0 ? 0u : level == 1 ? ~2047u : ~0u;
-  const uint32_t mk = level < 3 ? 0u : level == 3 ? ~0u << 21 : level == 4 ? ~0u << 10 : ~0u;
-  const uint32_t mi = level < 6 ? 0u : level == 6 ? ~2047u : ~0u;
-  return (((a.y ^ b.y) & my) | ((a.k ^ b.k) & mk) | ((a.id ^ b.id) & mi)) == 0;
-}
-DEVI uint32_t digit_of(const Digits &a, int level) {
-  switch (level) {
-    case 1: return a.y & 2047;
-    case 2: return a.k >> 21;
-    case 3: return a.k >> 10 & 2047;
-    case 4: return a.k & 1023;
-    case 5: return a.id >> 11;
-    default: return a.id & 2047;
-  }
-}
-DEVI void set_digit(Digits &a, int level, uint32_t d) {
-  switch (level) {
-    case 0: a.y = d << 11; break;
-    case 1: a.y |= d; break;
-    case 2: a.k = d << 21; break;
-    case 3: a.k |= d << 10; break;
-    case 4: a.k |= d; break;
-    case 5: a.id = d << 11; break;
-    default: a.id |= d; break;
-  }
+DEVI bool in_bin(const DrawRow &s, float v, int bin) {
+  const float y = distance(s, v);
+  return y < kFar && (int)y >> kSplitLog == bin;
 }
 
-// Bounds of the values whose distance is in [from, to) parts, a little wider: the distance is off by
-// 2^-23 of itself, less than a part.
+// Bounds of the values of the bins [from, to), a little wider: the distance is off by 2^-23 of itself, less
+// than a part.
 struct Between {
   float lo, hi;
-  DEVI static Between of(const DrawRow &s, uint32_t from, uint32_t to) {
-    const double top = (double)s.m - ((double)from - 2.0) / (double)s.cf, end = (double)s.m - ((double)to + 2.0) / (double)s.cf;
+  DEVI static Between bins(const DrawRow &s, int from, int to) {
+    const double part = 1.0 / (double)s.cf;
+    const double top = (double)s.m - ((double)(from << kSplitLog) - 2.0) * part, end = (double)s.m - ((double)(to << kSplitLog) + 2.0) * part;
     return {scalar((float)(end - fabs(end) * 0x1p-22)), scalar((float)(top + fabs(top) * 0x1p-22))};
   }
   DEVI static Between none() { return {INFINITY, INFINITY}; }  // (rows with a logit of +inf are done without)
@@ -325,44 +299,43 @@ struct Between {
   // (no value is its own median of these if it is NaN)
   DEVI bool has(float v) const { return __builtin_amdgcn_fmed3f(v, lo, hi) == v; }
 };
-// f(value, its digits) of the entries whose distance is in [from, to) parts
-template <typename LT, typename F>
-DEVI void each_between(const LT *lr, uint32_t V, const DrawRow &s, uint32_t from, uint32_t to, F f) {
-  const Between near_by = Between::of(s, from, to);
-  each_of_row(lr, V, 0, V, [&](const u32x4 &x, uint32_t id0) {
+// which of a vector's values are between the bounds, the last one in the lowest bit; without a branch: one for every
+// value took 24 us a row of 151936, three times as long
+template <typename LT>
+DEVI uint32_t hits(const u32x4 &x, const Between &of) {
+  uint32_t b = 0;
 #pragma unroll
-    for (int e = 0; e < RowVec<LT>::N; ++e) {
-      const float v = RowVec<LT>::get(x, e);
-      if (near_by.has(v)) {
-        const float y = distance(s, v);
-        if (y >= (float)from && y < (float)to) f(v, Digits{(uint32_t)y, ~order_key(v), id0 + e});
-      }
+  for (int e = 0; e < RowVec<LT>::N; ++e) b = b + b + (of.has(RowVec<LT>::get(x, e)) ? 1u : 0u);
+  return b;
+}
+// f(value, id) of the values between the bounds
+template <typename LT, typename F>
+DEVI void each_between(const LT *lr, uint32_t V, const Between &of, F f) {
+  constexpr int N = RowVec<LT>::N;
+  each_of_row<1>(lr, V, 0, V, [&](const u32x4 &x, uint32_t id0) {
+    for (uint32_t b = hits<LT>(x, of); b; b &= b - 1) {
+      const int e = N - 1 - (__ffs(b) - 1), i = e * 4 / N;
+      const uint32_t w = i < 2 ? (i == 0 ? x[0] : x[1]) : (i == 2 ? x[2] : x[3]);
+      f(RowVec<LT>::get(u32x4{w, w, w, w}, 0 + (N == 8 && (e & 1))), id0 + e);
     }
   });
 }
 // Collects the ids of the values between the bounds of A in sh.list, and of B in sh.draw, by waves: each has a
-// part of its own, so that no lane waits for a place.  false if one does not hold them.  A lane gathers
-// a vector's hits as bits, without a branch: a branch for every value took 24 us a row of 151936, three times as long.
+// part of its own, so that no lane waits for a place.  Bit 0, bit 1: A's, B's are all there.
 template <typename LT>
-DEVI bool collect(const LT *lr, uint32_t V, const Between &A, const Between &B, WholeShared &sh) {
+DEVI int collect(const LT *lr, uint32_t V, const Between &A, const Between &B, WholeShared &sh) {
   constexpr int N = RowVec<LT>::N;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int na = 0, nb = 0;
-  each_of_row(lr, V, 0, V, [&](const u32x4 &x, uint32_t id0) {
-    uint32_t a = 0, b = 0;  // the last value in the lowest bit
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float v = RowVec<LT>::get(x, e);
-      a = a + a + (A.has(v) ? 1u : 0u);
-      b = b + b + (B.has(v) ? 1u : 0u);
-    }
+  each_of_row<2>(lr, V, 0, V, [&](const u32x4 &x, uint32_t id0) {
+    const uint32_t a = hits<LT>(x, A), b = hits<LT>(x, B);
     auto put = [&](uint32_t bits, unsigned long long *list, int &n) {
       while (true) {
         const unsigned long long mk = __ballot(bits != 0);
         if (!mk) break;
         if (bits) {
           const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mk >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mk, 0));
-          if (at < kSeg) list[wave * kSeg + at] = id0 + (N - 1) - (__ffs(bits) - 1);
+          if (at < kSeg) ((uint32_t *)list)[wave * kSeg + at] = id0 + (N - 1) - (__ffs(bits) - 1);
           bits &= bits - 1;
         }
         n += __popcll(mk);
@@ -376,35 +349,41 @@ DEVI bool collect(const LT *lr, uint32_t V, const Between &A, const Between &B, 
     sh.wave_n[1][wave] = nb;
   }
   __syncthreads();
-  bool ok = true;
-  for (int w = 0; w < kWholeWaves; ++w) ok = ok && sh.wave_n[0][w] <= kSeg && sh.wave_n[1][w] <= kSeg;
-  return ok;
-}
-// The entries of a collected list that `on` takes (by digits) and that have a weight, as keys in descending order; their number.
-template <typename LT, typename On>
-DEVI int pack_list(const LT *lr, uint32_t V, const DrawRow &s, unsigned long long *list, const Between &of, const int *wave_n,
-                   WholeShared &sh, int slot, On on) {
-  constexpr int kTwo = kListMax / kWholeThreads;
-  const int tid = threadIdx.x;
-  unsigned long long k[kTwo];
-#pragma unroll
-  for (int j = 0; j < kTwo; ++j) {
-    const int i = j * kWholeThreads + tid;
-    k[j] = 0;
-    if (i % kSeg < wave_n[i / kSeg]) {
-      const uint32_t id = (uint32_t)list[i];
-      const float v = id < V ? to_f32(lr[id]) : -INFINITY, y = distance(s, v);
-      if (y < kFar && on(Digits{(uint32_t)y, ~order_key(v), id}) && s.weight(v)) k[j] = entry_key(v, id);
+  int most[2] = {0, 0}, all[2] = {0, 0};
+  for (int w = 0; w < kWholeWaves; ++w)
+    for (int i = 0; i < 2; ++i) {
+      most[i] = max(most[i], sh.wave_n[i][w]);
+      all[i] += sh.wave_n[i][w];
     }
+  return (most[0] <= kSeg && all[0] <= kListMax ? 1 : 0) | (most[1] <= kSeg && all[1] <= kListMax ? 2 : 0);
+}
+// The entries of a collected list that are of `bin` and have a weight, as keys in descending order; their number.
+template <typename LT>
+DEVI int pack_list(const LT *lr, uint32_t V, const DrawRow &s, unsigned long long *list, int bin, const Between &of,
+                   const int *wave_n, WholeShared &sh, int slot) {
+  constexpr int kPer = 2 * kListMax / kWholeThreads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, have = wave_n[wave];  // (its own part)
+  unsigned long long k[kPer];
+  uint32_t id[kPer];
+  float v[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    id[j] = ((const uint32_t *)list)[wave * kSeg + j * 64 + lane];
+    v[j] = to_f32(lr[min(id[j], V - 1)]);  // (at any place of the row where there is none)
+  }
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    k[j] = 0;
+    if (j * 64 + lane < have && id[j] < V && in_bin(s, v[j], bin) && s.weight(v[j])) k[j] = entry_key(v[j], id[j]);
   }
   if (tid == 0) sh.n[slot] = 0;
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kTwo; ++j)
+  for (int j = 0; j < kPer; ++j)
     if (k[j]) list[atomicAdd(&sh.n[slot], 1)] = k[j];
   __syncthreads();
   const int n = sh.n[slot];
-  sort_list<kWholeWaves>(n, list, order_key(of.lo), order_key(of.hi), sh.sort, sh.red);
+  sort_list<kWholeWaves, LT>(n, list, order_key(of.lo), order_key(of.hi), sh.sort, sh.red);
   return n;
 }
 
@@ -449,11 +428,12 @@ struct Bin {
   int i;
   unsigned long long m0, n0;
 };
+template <int PER>
 DEVI Bin pass_in_bins(const unsigned long long *mass, const uint32_t *count, int bins, bool by_count, unsigned long long target,
                       unsigned long long em, unsigned long long en, WholeShared &sh) {
 #pragma unroll
-  for (int j = 0; j < kBinsPer; ++j) {
-    const int b = threadIdx.x * kBinsPer + j;
+  for (int j = 0; j < PER; ++j) {
+    const int b = threadIdx.x * PER + j;
     if (b < bins) {
       const unsigned long long mb = mass[b], a0 = by_count ? en : em, a1 = a0 + (by_count ? count[b] : mb);
       if (a0 <= target && target < a1) {  // one bin of all
@@ -471,90 +451,126 @@ DEVI Bin pass_in_bins(const unsigned long long *mass, const uint32_t *count, int
   return r;
 }
 
-// The shortest prefix of the whole row's order whose count (by_count) or sum is above `target`, which
-// is passed in `bin`: its entries, or, while they are too many for the list, those of a part of it.
-// The values of `also` come into sh.draw on the way; it is set to none if they were not.
+// The ids of the values with a key, counted by 256s in sh.part.count; their number.
+constexpr int kIdsLog = 8;
+static_assert(kRowsMaxVocab <= kSplit << kIdsLog, "a row's ids in the parts");
+template <typename LT>
+DEVI uint32_t count_equal(const LT *lr, uint32_t V, uint32_t key, WholeShared &sh) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  for (int i = tid; i < kSplit; i += kWholeThreads) sh.part.count[i] = 0;
+  __syncthreads();
+  const float v = order_key_value(key);
+  each_between<LT>(lr, V, Between{v, v}, [&](float, uint32_t id) { atomicAdd(&sh.part.count[id >> kIdsLog], 1u); });
+  __syncthreads();
+  const uint32_t n = sh.part.count[2 * tid] + sh.part.count[2 * tid + 1];
+  return block_reduce_sum<kWholeWaves>(n, sh.red);
+}
+static_assert(kSplit == 2 * kWholeThreads, "two parts a thread");
+// The at-th id of those, of as many and more.
+template <typename LT>
+DEVI uint32_t equal_at(const LT *lr, uint32_t V, uint32_t key, uint32_t at, WholeShared &sh) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  const uint32_t c0 = sh.part.count[2 * tid], c1 = sh.part.count[2 * tid + 1];
+  const uint32_t before = block_scan<kWholeWaves>(c0 + c1, sh.red) - c0 - c1;
+  if (before <= at && at < before + c0 + c1) {
+    sh.hit_i = 2 * tid + (at >= before + c0);
+    sh.hit[0] = at - before - (at >= before + c0 ? c0 : 0);
+  }
+  __syncthreads();
+  const uint32_t id = ((uint32_t)sh.hit_i << kIdsLog) + tid;
+  const bool on = tid < 1 << kIdsLog && id < V && order_key(to_f32(lr[min(id, V - 1)])) == key;
+  const uint32_t place = (uint32_t)sh.hit[0], upto = block_scan<kWholeWaves>(on ? 1u : 0u, sh.sort);
+  if (on && upto == place + 1) sh.hit[1] = id;
+  __syncthreads();
+  const uint32_t r = scalar((uint32_t)sh.hit[1]);
+  __syncthreads();
+  return r;
+}
+
+// The shortest prefix of the whole row's order whose count (by_count) or sum is above `target`, which is passed in
+// `bin`: among its entries, sorted, where they are not too many; or of a part of their keys' range, cut in 2048 parts
+// again and again, or of equal values by their place among the ids (bf16 logits above 16 are 1/8 apart: a flat row of
+// 151936 has thousands of each).  The values of `also` come into sh.draw on the way; it is set to none if they did not.
 template <typename LT>
 DEVI Prefix find_in_row(const LT *lr, uint32_t V, const DrawRow &s, bool by_count, unsigned long long target, Bin bin,
                         Between &also, WholeShared &sh) {
-  const int tid = threadIdx.x;
-  Digits at = {0, 0, 0};
-  for (int level = 0;; ++level) {
-    set_digit(at, level, bin.i);
-    const uint32_t from = at.y, to = at.y + (level == 0 ? kSplit : 1);
-    const Between of = Between::of(s, from, to);
-    if (collect<LT>(lr, V, of, also, sh)) {
-      const int n = pack_list(lr, V, s, sh.list, of, sh.wave_n[0], sh, 0, [&](const Digits &d) { return near(d, at, level + 1); });
+  const int tid = threadIdx.x, b = bin.i;
+  const Between of = Between::bins(s, b, b + 1);
+  int got = 0;
+  if (s.few(sh.mass[b], b)) {
+    got = collect<LT>(lr, V, of, also, sh);
+    if (!(got & 2)) also = Between::none();
+    if (got & 1) {
+      const int n = pack_list(lr, V, s, sh.list, b, of, sh.wave_n[0], sh, 0);
       return pass_in_list(s, sh.list, n, by_count, target, bin.m0, bin.n0, sh);
     }
-    also = Between::none();
-    if (level >= 2) {
-      // (the bounds take neighbours too: the entries themselves may be few)
-      __syncthreads();
-      if (tid == 0) sh.n[0] = 0;
-      __syncthreads();
-      each_between<LT>(lr, V, s, from, to, [&](float v, const Digits &d) {
-        if (near(d, at, level + 1) && s.weight(v)) {
-          const int i = atomicAdd(&sh.n[0], 1);
-          if (i < kListMax) sh.list[i] = entry_key(v, d.id);
-        }
-      });
-      __syncthreads();
-      const int n = sh.n[0];
-      if (n <= kListMax) {  // (at the last level a part is one entry)
-        sort_list<kWholeWaves>(n, sh.list, order_key(of.lo), order_key(of.hi), sh.sort, sh.red);
-        return pass_in_list(s, sh.list, n, by_count, target, bin.m0, bin.n0, sh);
-      }
-    }
+  }
+  also = Between::none();
+  uint32_t lo = order_key(of.lo), hi = order_key(of.hi);
+  // f(value, id) of the bin's entries with a key in [lo, hi]
+  auto each = [&](auto f) {
+    each_between<LT>(lr, V, of, [&](float v, uint32_t id) {
+      const uint32_t key = order_key(v);
+      if (in_bin(s, v, b) && key >= lo && key <= hi) f(v, id);
+    });
+  };
+  while (true) {
+    const uint32_t range = hi - lo;
+    const int shift = range < kSplit ? 0 : 32 - kSplitLog - __builtin_clz(range);
     __syncthreads();
     for (int i = tid; i < kSplit; i += kWholeThreads) {
       sh.part.mass[i] = 0;
       sh.part.count[i] = 0;
     }
+    if (tid == 0) sh.n[0] = 0;
     __syncthreads();
-    each_between<LT>(lr, V, s, from, to, [&](float v, const Digits &d) {
-      if (near(d, at, level + 1)) {
-        const unsigned long long w = s.weight(v);
-        if (w) {
-          atomicAdd(&sh.part.mass[digit_of(d, level + 1)], w);
-          atomicAdd(&sh.part.count[digit_of(d, level + 1)], 1u);
-        }
+    each([&](float v, uint32_t) {
+      const unsigned long long w = s.weight(v);
+      if (w) {
+        const uint32_t i = kSplit - 1 - ((order_key(v) - lo) >> shift);
+        atomicAdd(&sh.part.mass[i], w);
+        atomicAdd(&sh.part.count[i], 1u);
       }
     });
     __syncthreads();
-    unsigned long long pm = 0, pn = 0;
-    for (int b = tid * kBinsPer; b < min((tid + 1) * kBinsPer, kSplit); ++b) {
-      pm += sh.part.mass[b];
-      pn += sh.part.count[b];
-    }
+    const unsigned long long pm = sh.part.mass[2 * tid] + sh.part.mass[2 * tid + 1];
+    const uint32_t pn = sh.part.count[2 * tid] + sh.part.count[2 * tid + 1];
     const unsigned long long em = bin.m0 + block_scan<kWholeWaves>(pm, sh.redu[0]) - pm;
-    const unsigned long long en = bin.n0 + block_scan<kWholeWaves>(pn, sh.redu[1]) - pn;
-    bin = pass_in_bins(sh.part.mass, sh.part.count, kSplit, by_count, target, em, en, sh);
+    const unsigned long long en = bin.n0 + block_scan<kWholeWaves, unsigned long long>(pn, sh.redu[1]) - pn;
+    bin = pass_in_bins<2>(sh.part.mass, sh.part.count, kSplit, by_count, target, em, en, sh);
+    const int n = (int)scalar(sh.part.count[bin.i]);
+    lo += (uint32_t)(kSplit - 1 - bin.i) << shift;
+    hi = min(hi, lo + ((1u << shift) - 1u));
+    __syncthreads();
+    if (n <= kListMax) {
+      each([&](float v, uint32_t id) {
+        if (s.weight(v)) sh.list[min(atomicAdd(&sh.n[0], 1), kListMax - 1)] = entry_key(v, id);  // (n of them)
+      });
+      __syncthreads();
+      sort_list<kWholeWaves, LT>(n, sh.list, lo, hi, sh.sort, sh.red);
+      return pass_in_list(s, sh.list, n, by_count, target, bin.m0, bin.n0, sh);
+    }
+    if (shift == 0) break;
   }
+  // one value: the place among its ids
+  const float v = order_key_value(lo);
+  const unsigned long long w = s.weight(v), at = by_count ? target - bin.n0 : (target - bin.m0) / w;
+  count_equal<LT>(lr, V, lo, sh);
+  return {bin.m0 + (at + 1) * w, entry_key(v, equal_at<LT>(lr, V, lo, (uint32_t)at, sh))};
 }
 
 // A row whose maximum is +inf: its n logits of +inf have a weight of 1 each, in the order of their ids.
 template <typename LT>
 DEVI void draw_of_infinities(const LT *lr, const SampleArgs &p, const DrawRow &d, int V, int row, WholeShared &sh) {
-  const int tid = threadIdx.x, len = (V + kWholeThreads - 1) / kWholeThreads;
-  uint32_t mine = 0;
-  for (int i = tid * len; i < min((tid + 1) * len, V); ++i) mine += to_f32(lr[i]) == INFINITY;
-  uint32_t *red = (uint32_t *)sh.redu[0];
-  const uint32_t upto = block_scan<kWholeWaves>(mine, red);
-  if (tid == kWholeThreads - 1) sh.hit_i = (int)upto;
-  __syncthreads();
-  uint32_t n = sh.hit_i;
+  const uint32_t key = order_key(INFINITY);
+  uint32_t n = count_equal<LT>(lr, V, key, sh);
   if (d.has_k) n = min(n, (uint32_t)d.top_k);
   if (d.use_p) n = max(1u, min(n, (uint32_t)ceil((double)d.top_p * n)));
-  uint32_t at = min((uint32_t)floor((double)d.u * n), n - 1);  // the draw's place among them
-  if (at >= upto - mine && at < upto) {
-    at -= upto - mine;
-    for (int i = tid * len;; ++i)
-      if (to_f32(lr[i]) == INFINITY && at-- == 0) {
-        d.finish(p, row, i, d.logprob(INFINITY, (unsigned long long)n << kWeightBits));
-        break;
-      }
-  }
+  const uint32_t at = min((uint32_t)floor((double)d.u * n), n - 1);  // the draw's place among them
+  const uint32_t id = equal_at<LT>(lr, V, key, at, sh);
+  if (threadIdx.x == 0) d.finish(p, row, (int)id, d.logprob(INFINITY, (unsigned long long)n << kWeightBits));
 }
 
 template <typename LT>
@@ -575,7 +591,7 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
   const uint32_t len = ((uint32_t)a.V / slices / N + 1) * N, v0 = slice * len, v1 = min((uint32_t)a.V, v0 + len);
   // f(bin, weight), four values at a time: their weights are formed side by side
   auto each_weight = [&](auto f) {
-    each_of_row(lr, a.V, v0, v1, [&](const u32x4 &x, uint32_t) {
+    each_of_row<2>(lr, a.V, v0, v1, [&](const u32x4 &x, uint32_t) {
 #pragma unroll
       for (int e = 0; e < N; e += 4) {
         float y[4];
@@ -660,7 +676,7 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
   unsigned long long total = scalar(sh.hit[1]);
   __syncthreads();
   auto bin_of = [&](bool by_count, unsigned long long target) {
-    return pass_in_bins(sh.mass, sh.count, kBins, by_count, target, em - pm, en - pn, sh);
+    return pass_in_bins<kBinsPer>(sh.mass, sh.count, kBins, by_count, target, em - pm, en - pn, sh);
   };
   auto drawn = [&](unsigned long long sum) { return min((unsigned long long)floor((double)d.u * (double)sum), sum - 1); };
   // top-k, top-p, then (the shorter of it and min-p kept) the draw
@@ -678,8 +694,9 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
         unsigned long long mm = 0;
         for (int b = tid; b < b0; b += kWholeThreads) mm += sh.mass[b];
         if (b0 < kBins)
-          each_between<LT>(lr, a.V, d, b0 << kSplitLog, b1 << kSplitLog, [&](float v, const Digits &) {
-            if (d.stays(v)) mm += d.weight(v);
+          each_between<LT>(lr, a.V, Between::bins(d, b0, b1), [&](float v, uint32_t) {
+            const float y = distance(d, v);
+            if (y < kFar && (int)y >> kSplitLog >= b0 && (int)y >> kSplitLog < b1 && d.stays(v)) mm += d.weight(v);
           });
         total = min(total, block_reduce_sum<kWholeWaves>(mm, sh.redu[0]));
         __syncthreads();
@@ -694,13 +711,13 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
     if (step == 1 && !d.use_m) {
       next = bin_of(false, drawn(target + 1));
       const Bin last = bin_of(false, drawn(min(total, target + 1 + d.weight_at(bin.i))));
-      if (next.i == last.i) also = Between::of(d, (uint32_t)next.i << kSplitLog, (uint32_t)(next.i + 1) << kSplitLog);
+      if (next.i == last.i && d.few(sh.mass[next.i], next.i)) also = Between::bins(d, next.i, next.i + 1);
     }
     Prefix f = find_in_row<LT>(lr, a.V, d, step == 0, target, bin, also, sh);
     bool end = step == 2;
     if (!end) total = f.mass;
     if (also.some()) {
-      const int n = pack_list(lr, a.V, d, sh.draw, also, sh.wave_n[1], sh, 1, [&](const Digits &x) { return x.y >> kSplitLog == (uint32_t)next.i; });
+      const int n = pack_list(lr, a.V, d, sh.draw, next.i, also, sh.wave_n[1], sh, 1);
       f = pass_in_list(d, sh.draw, n, false, drawn(total), next.m0, next.n0, sh);
       end = true;
     }

@@ -47,6 +47,19 @@ template <typename LT>
 DEVI void row_store(LT *p, const u32x4 &x) {
   __builtin_memcpy(p, &x, 16);
 }
+// The row's last 16 bytes as the vector that begins `by` values later, -inf past the row's end.
+template <typename LT>
+DEVI u32x4 row_move_end(u32x4 x, uint32_t by) {
+  constexpr int N = RowVec<LT>::N;
+  constexpr uint32_t kLow = RowVec<LT>::kLow;
+  if (by & (N / 2)) x = u32x4{x[2], x[3], kLow, kLow};
+  if (by & (N / 4)) x = u32x4{x[1], x[2], x[3], kLow};
+  if (N == 8 && (by & 1)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_alignbit(e < 3 ? x[e + 1] : kLow, x[e], 16);
+  }
+  return x;
+}
 // The vector at v0 < V of a row of V values, -inf past its end.  Where it crosses the end the row's
 // last 16 bytes are loaded and moved down, in a few instructions: this code is in many loops.
 template <typename LT>
@@ -58,13 +71,7 @@ DEVI u32x4 row_load_end(const LT *row, uint32_t v0, uint32_t V) {
   if (v0 >= V) return x;
   const uint32_t by = v0 + N - V;  // values past the end
   if (V >= N) {
-    x = row_load(row + (V - N));
-    if (by & (N / 2)) x = u32x4{x[2], x[3], kLow, kLow};
-    if (by & (N / 4)) x = u32x4{x[1], x[2], x[3], kLow};
-    if (N == 8 && (by & 1)) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_alignbit(e < 3 ? x[e + 1] : kLow, x[e], 16);
-    }
+    x = row_move_end<LT>(row_load(row + (V - N)), by);
   } else {  // (v0 = 0, fewer values than a vector has)
 #pragma unroll 1
     for (uint32_t i = V; i-- > 0;) {

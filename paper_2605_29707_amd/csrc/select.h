@@ -55,10 +55,11 @@ DEVI T block_scan(T v, T *red) {
 // list[0 .. n), n <= kListMax, in descending order (keys are distinct, their upper halves in [lo, hi]), by
 // W waves.  Up to 128 a key counts those before it, by several threads where there are enough.  More
 // are dealt into as many equal parts of [lo, hi] as there are threads, and a key counts those before it in
-// its part (270 keys in 2.5K cycles; all against all, 11K beside another workgroup).  Where a part holds
-// many, as of equal values, a bitonic network, whose short steps stay within a wave and need no barrier.
+// its part (270 keys in 2.5K cycles; all against all, 11K beside another workgroup).  The ids follow in the
+// parts, and bf16 values leave out the bits they do not have, so that equal values fall into many.  Where a part
+// holds many all the same, a bitonic network, whose short steps stay within a wave and need no barrier (2048 keys: 20 us).
 constexpr int kPartMax = 64;
-template <int W>
+template <int W, typename LT>
 DEVI void sort_list(int n, unsigned long long *list, uint32_t lo, uint32_t hi, uint32_t *hist, uint32_t *red) {
   constexpr int kThreads = 64 * W, kEach = kListMax / kThreads, kLog = W == 16 ? 10 : 9;
   static_assert(W == 8 || W == 16, "log2 of the threads");
@@ -81,8 +82,11 @@ DEVI void sort_list(int n, unsigned long long *list, uint32_t lo, uint32_t hi, u
     __syncthreads();
     return;
   }
-  const uint32_t range = hi - lo;
-  const int shift = range < kThreads ? 0 : 32 - kLog - __builtin_clz(range);
+  constexpr int kDrop = RowVec<LT>::N == 8 ? 16 : 0;
+  constexpr uint32_t kIds = (1u << 19) - 1;
+  static_assert(kRowsMaxVocab <= (int)kIds, "ids in 19 bits");
+  const unsigned long long range = (unsigned long long)((hi >> kDrop) - (lo >> kDrop)) << 19 | kIds;
+  const int shift = 64 - kLog - __builtin_clzll(range);
   unsigned long long k[kEach];
   int part[kEach];
 #pragma unroll
@@ -90,7 +94,8 @@ DEVI void sort_list(int n, unsigned long long *list, uint32_t lo, uint32_t hi, u
     const int i = j * kThreads + tid;
     if (i < n) {
       k[j] = list[i];
-      part[j] = kThreads - 1 - (int)(((uint32_t)(k[j] >> 32) - lo) >> shift);
+      const unsigned long long at = (unsigned long long)(((uint32_t)(k[j] >> 32) >> kDrop) - (lo >> kDrop)) << 19 | ((uint32_t)k[j] & kIds);
+      part[j] = kThreads - 1 - (int)(at >> shift);
       atomicAdd(&hist[part[j]], 1u);
     }
   }
@@ -347,7 +352,7 @@ DEVI void select_top(const LT *lr, const float2 *groups, int V, int G, int C, fl
     if (sh.n <= kListMax) break;
   }
   const int n = sh.n;
-  sort_list<kSelWaves>(n, sh.list, ec.key, hi, sh.hist, sh.wave[0]);
+  sort_list<kSelWaves, LT>(n, sh.list, ec.key, hi, sh.hist, sh.wave[0]);
   if (!want_rest) return;
   // The rest: the groups not read, the values not listed, the list behind C.
 #pragma unroll

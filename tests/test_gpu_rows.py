@@ -46,6 +46,8 @@ def _make(kind, rows, V, dtype, seed=0):
         x = -np.sort(-x, axis=1)
     elif kind == "equal":
         x = np.full((rows, V), 1.5)
+    elif kind == "coarse":   # bf16 values 1/8 apart: thousands of each
+        x = 24 + 1.2 * x
     elif kind == "close":    # values that differ in their last bits alone, of both signs
         x = rng.integers(-3000, 3000, size=(rows, V)) * 1e-9
     elif kind in ("masked", "lowest"):   # few ids stay, none in the last row
@@ -479,7 +481,8 @@ def test_sample_temperatures_at_the_ends_of_their_range():
     assert (tok >= 0).tolist() == [False, False, True, False, False, False]
 
 
-@pytest.mark.parametrize("kind,V,dtype", [("normal", 151936, "f32"), ("falling", 151936, "bf16"), ("close", 262144, "f32")])
+@pytest.mark.parametrize("kind,V,dtype", [("normal", 151936, "f32"), ("falling", 151936, "bf16"), ("close", 262144, "f32"),
+                                          ("coarse", 151936, "bf16")])
 def test_sample_few_flat_rows(kind, V, dtype):
     """Rows that several workgroups share, their filters' borders far behind the first entries and, in rows in
     falling order, a border's entries side by side."""
