@@ -285,12 +285,12 @@ DEVI bool in_bin(const DrawRow &s, float v, int bin) {
   return y < kFar && (int)y >> kSplitLog == bin;
 }
 
-// Bounds of the values of the bins [from, to), a little wider: the distance is off by 2^-23 of itself, less
-// than a part.
+// Bounds of the values of the bins [from, to), a little wider: the distance is off by 2^-23 of itself, and its factor
+// by 2^-24, together less than two parts.
 struct Between {
   float lo, hi;
   DEVI static Between bins(const DrawRow &s, int from, int to) {
-    const double part = 1.0 / (double)s.cf;
+    const double part = (double)s.T * (0.6931471805599453 / (1 << (kBinsLog + kSplitLog)));
     const double top = (double)s.m - ((double)(from << kSplitLog) - 2.0) * part, end = (double)s.m - ((double)(to << kSplitLog) + 2.0) * part;
     return {scalar((float)(end - fabs(end) * 0x1p-22)), scalar((float)(top + fabs(top) * 0x1p-22))};
   }
@@ -703,15 +703,17 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
       }
       target = drawn(total);
     }
-    const Bin bin = bin_of(step == 0, target);
+    Bin bin = {}, next = {};
     // The sum that top-p keeps is target + 1 at least, and less than the weight of the bin's first part above it:
     // where the draw falls into one bin in both cases, one pass collects both bins.
     Between also = Between::none();
-    Bin next = {};
-    if (step == 1 && !d.use_m) {
-      next = bin_of(false, drawn(target + 1));
-      const Bin last = bin_of(false, drawn(min(total, target + 1 + d.weight_at(bin.i))));
-      if (next.i == last.i && d.few(sh.mass[next.i], next.i)) also = Between::bins(d, next.i, next.i + 1);
+    const int both = step == 1 && !d.use_m ? 3 : 1;
+#pragma unroll 1
+    for (int t = 0; t < both; ++t) {  // (a loop: three copies of the search come from memory three times)
+      const Bin r = bin_of(step == 0, t == 0 ? target : drawn(t == 1 ? target + 1 : min(total, target + 1 + d.weight_at(bin.i))));
+      if (t == 0) bin = r;
+      else if (t == 1) next = r;
+      else if (next.i == r.i && d.few(sh.mass[r.i], r.i)) also = Between::bins(d, r.i, r.i + 1);
     }
     Prefix f = find_in_row<LT>(lr, a.V, d, step == 0, target, bin, also, sh);
     bool end = step == 2;
