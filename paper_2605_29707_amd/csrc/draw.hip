@@ -328,7 +328,6 @@ DEVI int collect(const LT *lr, uint32_t V, const Between &A, const Between &B, W
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int na = 0, nb = 0;
   each_of_row<2>(lr, V, 0, V, [&](const u32x4 &x, uint32_t id0) {
-    const uint32_t a = hits<LT>(x, A), b = hits<LT>(x, B);
     auto put = [&](uint32_t bits, unsigned long long *list, int &n) {
       while (true) {
         const unsigned long long mk = __ballot(bits != 0);
@@ -341,8 +340,8 @@ DEVI int collect(const LT *lr, uint32_t V, const Between &A, const Between &B, W
         n += __popcll(mk);
       }
     };
-    put(a, sh.list, na);
-    put(b, sh.draw, nb);
+    put(hits<LT>(x, A), sh.list, na);
+    if (B.some()) put(hits<LT>(x, B), sh.draw, nb);  // (uniform; the loop is bound by its instructions)
   });
   if (lane == 0) {
     sh.wave_n[0][wave] = na;
