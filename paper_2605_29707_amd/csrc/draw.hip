@@ -16,7 +16,8 @@
 //           workgroup to finish a row finds the bin where a running sum passes its target, and the entry
 //           among the bin's, sorted, or first by parts of their range while they are too many.  Bound by the
 //           polynomials and LDS atomics of the sums, then by one CU's pass over a row for each border (64 of
-//           512 rows of 151936 bf16 logits flat: 75 us, 21 of them for the sums, 22 a pass).
+//           512 rows of 151936 bf16 logits flat: 67 us, 21 of them for the sums, 6 to join them, 14 a pass
+//           and 6 for the list it leaves).
 #include <algorithm>
 #include <type_traits>
 
@@ -491,7 +492,8 @@ DEVI uint32_t equal_at(const LT *lr, uint32_t V, uint32_t key, uint32_t at, Whol
 // The shortest prefix of the whole row's order whose count (by_count) or sum is above `target`, which is passed in
 // `bin`: among its entries, sorted, where they are not too many; or of a part of their keys' range, cut in 2048 parts
 // again and again, or of equal values by their place among the ids (bf16 logits above 16 are 1/8 apart: a flat row of
-// 151936 has thousands of each).  The values of `also` come into sh.draw on the way; it is set to none if they did not.
+// 151936 has thousands of each; 64 such rows without filters 210 us in all, 700 with a level for every 11 bits of
+// the order).  The values of `also` come into sh.draw on the way; it is set to none if they did not.
 template <typename LT>
 DEVI Prefix find_in_row(const LT *lr, uint32_t V, const DrawRow &s, bool by_count, unsigned long long target, Bin bin,
                         Between &also, WholeShared &sh) {
@@ -744,8 +746,8 @@ __global__ __launch_bounds__(kWholeThreads) void draw_whole_kernel(RowsArgs a, S
 }
 
 // Workgroups a row of the last launch: for few rows as many as cut a row of 128K ids to 8K each (64
-// rows of 128256 fp32 logits, the flat ones 120 us with one workgroup), for many enough to fill the chip
-// (512 rows of 151936 bf16 logits 75 us with two, 92 with four).
+// rows of 128256 fp32 logits, the flat ones: 46 us, 66 with one), for many enough to fill the chip
+// (512 rows of 151936 bf16 logits, 64 of them flat: 78 us with one, 67 with two, 99 with four).
 static int draw_slices(int rows, int V) { return std::max(1, std::min({16, 1024 / rows, V / 8192})); }
 
 // [error word and groups][a row each: state, workgroups done][sums, where a row has several workgroups]
