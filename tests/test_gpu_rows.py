@@ -121,6 +121,7 @@ def _check_rest(got, want):
     ("zipf", 5, 50257, 64, "bf16", 0, 0, 1.0), ("zipf", 3, 50257, 1000, "f32", 5, 2, 0.7),
     ("zipf", 2, 151936, 256, "bf16", 0, 0, 1.0), ("zipf", 2, 327680, 1024, "f32", 0, 0, 1.0),
     ("ties", 3, 151936, 512, "bf16", 0, 0, 1.0), ("ties", 2, 40000, 33, "f32", 0, 0, 1.0),
+    ("ties", 3, 5000, 1024, "f32", 0, 0, 1.0), ("ties", 3, 2000, 700, "bf16", 0, 1, 1.0), ("coarse", 2, 151936, 900, "bf16", 0, 0, 2.0),
     ("falling", 2, 50257, 300, "f32", 0, 0, 1.0), ("falling", 2, 151936, 1024, "f32", 0, 0, 1.0),
     ("falling", 2, 20000, 1024, "bf16", 0, 0, 1.0), ("equal", 2, 327680, 1024, "bf16", 0, 0, 1.0),
     ("equal", 2, 5000, 100, "f32", 0, 0, 1.0), ("close", 2, 30000, 700, "f32", 0, 0, 1.0),
@@ -482,7 +483,7 @@ def test_sample_temperatures_at_the_ends_of_their_range():
 
 
 @pytest.mark.parametrize("kind,V,dtype", [("normal", 151936, "f32"), ("falling", 151936, "bf16"), ("close", 262144, "f32"),
-                                          ("coarse", 151936, "bf16")])
+                                          ("coarse", 151936, "bf16"), ("ties", 262144, "f32"), ("ties", 9001, "f32")])
 def test_sample_few_flat_rows(kind, V, dtype):
     """Rows that several workgroups share, their filters' borders far behind the first entries and, in rows in
     falling order, a border's entries side by side."""
