@@ -255,19 +255,21 @@ __global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs a) 
     if (i < a.k)  // the entry's value is read, its gradient takes its place
       z[i] = scale == 0.0 ? 0.f : bad ? NAN : used >> j & 1 ? (float)(scale * (q - p)) : 0.f;
   }
-  block_sums(kl, red + 3);
-  if (tid == 0) {
+  if (tid == 64) {  // the bucket of the other ids, beside the entries' of the first wave
     const double lpr = ((double)rt - tm) - log_P, lqr = R == 0.0 ? -INFINITY : r_m + (log(R) - log_Z);
     const double pr = none || rt == -INFINITY ? 0.0 : exp(lpr);
     if (!none && pr != 0.0) kl[0] += pr * (lpr - lqr);
+    // the gradient of any other id: exp((l - mr) / T) times this
+    const double coef = scale == 0.0 ? 0.0 : bad ? NAN : R == 0.0 ? 0.0 : scale * (exp(lqr) - pr) / R;
+    a.stat[row] = make_float2(mr == -INFINITY ? 0.f : mr, (float)coef);
+  }
+  block_sums(kl, red + 3);
+  if (tid == 0) {
     const double loss = bad ? NAN : none ? 0.0 : (double)a.T * (double)a.T * kl[0];
     if (bad) raise_error(a.err, DEV_BAD_TOKEN);
     if (row == 0 && odd_weights != 0.0) raise_error(a.err, DEV_BAD_PARAM);
     a.row_loss[row] = (float)loss;
     a.share[row] = w > 0.f ? (double)w / W * loss : 0.0;
-    // of any other id: exp((l - mr) / T) times this
-    const double coef = scale == 0.0 ? 0.0 : bad ? NAN : R == 0.0 ? 0.0 : scale * (exp(lqr) - pr) / R;
-    a.stat[row] = make_float2(mr == -INFINITY ? 0.f : mr, (float)coef);
   }
 }
 
