@@ -470,9 +470,10 @@ size_t domino_sample_logits_workspace_bytes(int32_t rows, int32_t vocab);
  *   n_m = the number of entries with e >= min_p (0: every entry);
  * the first n = min(n_k, n_p, n_m) are kept, S the sum of their e; the token is the
  * first whose running sum exceeds u S, its log-probability log(e / S).  Logits of +inf
- * share all the weight.  e is held to 2^-45 (a lighter entry is never drawn) and summed as whole
- * numbers, so the token does not depend on the order of the sums.  (Where a filter or the draw ends within a
- * row's first 64 entries, what lies behind them counts by single-precision exponentials, within 4e-6 of it.)
+ * share all the weight.  e is computed to 2^-38.8 of itself and rounded to a whole number of 2^-44 (one below
+ * 2^-45 is never drawn), and these are what is summed, so the token depends neither on the order of the
+ * sums nor on where in the row it lies.  (Without filters, the log-probability of one of a row's first 64 entries has
+ * an S in which the others count by single-precision exponentials, within 2^-16 of their sum.)
  *  vocab           at most 327680
  *  temperature     optional device fp32 [rows]: T in [1e-30, 1e30], NULL: 1.  0: the first
  *                  entry of the order, whatever the filters

@@ -9,8 +9,9 @@
 // Launches:
 //   groups  as for the top entries (logits.hip)
 //   first   a workgroup a row: the first C entries (select.h), C = top_k where that is at most 1024,
-//           or 64; the filters and the draw in their running sums.  Nearly all rows of a model
-//           end here.  Bound by the chain of its steps (one row of 151936 11 us, 512 19).
+//           or 64; the filters and the draw in their running sums.  A row ends here if they all fall among
+//           those, clear of what the sum of the others may be off by, since that is of single-precision
+//           exponentials.  Bound by the chain of its steps (one row of 151936 11 us, 512 19).
 //   whole   the other rows (flat ones, whose kept entries or draw lie behind the first 64), several
 //           workgroups a row: sums of e by bins of log2 e, in LDS, then added in memory; the last
 //           workgroup to finish a row finds the bin where a running sum passes its target, and the entry
@@ -38,6 +39,11 @@ constexpr int kFirst = 64;                            // entries looked at first
 constexpr int kWholeThreads = 1024;
 constexpr int kWholeWaves = kWholeThreads / 64;
 constexpr double kOne = (double)(1ull << kWeightBits);
+// What a row's sum behind its first entries may be off by where it comes from single-precision exponentials, of itself.
+// In units of 2^-24: an exponent is off by 2.3 of itself (the factor, the difference, the product), and the
+// weighted mean of the exponents is log2 V < 18.4 at most, so 29 of the sum; two exponentials 4; sums of 10 in a group, of
+// 20 groups and of 132 values in a thread 162.  Together 195, below 256.
+constexpr double kRestOff = 0x1p-16;
 
 // round(2^44 2^-x) for 0 <= x < 2^10.  2^f on [-1/2, 1/2] as 1 + f q(f), q interpolating (2^f - 1) / f at the
 // zeros of the Chebyshev polynomial of degree 8: 2^-38.8 of the value off at most, and exactly 1 at 0.
@@ -128,7 +134,7 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
   __shared__ SelShared sh;
   __shared__ unsigned long long run[kTopMax];  // running sums of the first C
   __shared__ unsigned long long redu[kSelWaves];
-  __shared__ int first[4];
+  __shared__ int first[6];
   constexpr int kPer = kTopMax / kSelThreads;
   const int row = blockIdx.x, tid = threadIdx.x;
   DrawRow d;
@@ -163,7 +169,7 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
     w[j] = on ? d.weight(v[j]) : 0ull;
     sum += w[j];
   }
-  if (tid < 4) first[tid] = C;
+  if (tid < 6) first[tid] = C;
   unsigned long long r = block_scan<kSelWaves>(sum, redu) - sum;
   // the first entry that on(entry, its value, weight) takes, by one lane of each wave (entries are in the lanes' order)
   auto first_of = [&](int slot, auto on) {
@@ -183,34 +189,60 @@ __global__ __launch_bounds__(kSelThreads) void draw_first_kernel(RowsArgs a, Sam
   const unsigned long long sum_c = run[C - 1], kUnknown = ~0ull;
   const int weighty = first[0], n_m = first[1];    // C: all of them
   const bool all = C == a.V || weighty < C;        // no weight lies behind the first C
-  // the whole row's sum: of the first C exactly, of the rest from the groups' sums
-  unsigned long long whole = sum_c;
-  if (!all && rs != 0.0) whole += (unsigned long long)(rs * (rm == d.m ? 1.0 : exp2(((double)rm - (double)d.m) * d.cd)) * kOne);
-  unsigned long long total = all ? sum_c : kUnknown;  // the kept prefix's sum
+  // The whole row's sum, of the first C as the next launch has it, of the rest from the groups' sums: that launch's
+  // is within `off` of it, half a unit an entry for the rounding of its weights.  A border or a draw that falls among
+  // the first C decides here where it is the same entry for the least and the most that the sum can be.
+  unsigned long long whole = sum_c, off = 0;
+  if (!all && rs != 0.0) {
+    const double rest = rs * (rm == d.m ? 1.0 : exp2(((double)rm - (double)d.m) * d.cd)) * kOne;
+    whole += (unsigned long long)rest;
+    off = (unsigned long long)(rest * kRestOff) + (unsigned)a.V;
+  }
+  unsigned long long least = all ? sum_c : kUnknown, most = least;  // the kept prefix's sum
   bool decided = true;
-  if (d.has_k && d.top_k <= C) whole = total = min(total, run[d.top_k - 1]);
+  if (d.has_k && d.top_k <= C) {
+    whole = least = most = min(least, run[d.top_k - 1]);
+    off = 0;
+  }
   if (d.use_p) {
     if (!d.has_k || d.top_k <= C || all) {
-      const unsigned long long want = (unsigned long long)ceil((double)d.top_p * (double)whole);
-      first_of(2, [&](int i, float, unsigned long long) { return run[i] >= want; });
+      auto border = [&](int slot, unsigned long long sum) {
+        const unsigned long long want = (unsigned long long)ceil((double)d.top_p * (double)sum);
+        first_of(slot, [&](int i, float, unsigned long long) { return run[i] >= want; });
+      };
+      border(2, whole - off);
+      if (off) border(4, whole + off);
     } else {
       decided = false;  // the sum of the first top_k is not known
     }
     __syncthreads();
-    if (first[2] < C) total = min(total, run[first[2]]);
+    const int p0 = first[2], p1 = off ? first[4] : p0;
+    if (p0 < C) least = min(least, run[p0]);
+    if (p1 < C) most = min(most, run[p1]);
   }
-  if (d.use_m && n_m < C) total = min(total, run[n_m - 1]);
+  if (d.use_m && n_m < C) {
+    least = min(least, run[n_m - 1]);
+    most = min(most, run[n_m - 1]);
+  }
+  if (least != most) decided = false;
   // no filter ends within the first C: without any, the draw may still fall there
+  unsigned long long total = least;
   if (total == kUnknown) {
     total = whole;
+    least = whole - off;
+    most = whole + off;
     if (d.use_p || d.use_m || d.has_k) decided = false;
   }
   if (decided) {
-    const unsigned long long target = (unsigned long long)floor((double)d.u * (double)total);
-    first_of(3, [&](int i, float, unsigned long long) { return run[i] > target; });
+    auto drawn = [&](int slot, unsigned long long sum) {
+      const unsigned long long target = (unsigned long long)floor((double)d.u * (double)sum);
+      first_of(slot, [&](int i, float, unsigned long long) { return run[i] > target; });
+    };
+    drawn(3, least);
+    if (least != most) drawn(5, most);
     __syncthreads();
     const int i = first[3];
-    if (i < C) {
+    if (i < C && (least == most || i == first[5])) {
       if (tid == 0) {
         const unsigned long long key = sh.list[i];
         d.finish(p, row, (int)entry_id(key), d.logprob(entry_value(key), total));
