@@ -29,6 +29,10 @@ DEVI bf16_t f32_to_bf16(float f) {
 // workgroup hands to another within a launch: the store is complete at the
 // device coherence point once the storing thread's vector-memory count drains,
 // and the load does not hit a stale line in a CU or XCD cache.
+// That holds on this target; others count stores apart, or cache them elsewhere.
+#if defined(__HIP_DEVICE_COMPILE__) && !defined(__gfx950__)
+#error "written for gfx950: hand-overs between workgroups count on its caches and its counter of stores"
+#endif
 DEVI float ld_coherent(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 DEVI void st_coherent(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 

@@ -654,16 +654,20 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
     // To memory; the last workgroup of the row adds them all up.  Stores and loads are device-scope ones,
     // complete when the count of the storing thread's drains: 64 rows at once took 17 to 37 us by
     // 64-bit atomics into one place, and as long by plain stores between fences, which write back and
-    // drop the whole cache of an XCD.
+    // drop the whole cache of an XCD.  Relaxed accesses say nothing of the order of sums and count: it comes from this
+    // chip's counter of stores, the barrier, and fences for the compiler alone, which emit no instruction.
     for (int i = tid; i < kBins; i += kWholeThreads) {
       __hip_atomic_store(&g[slice].mass[i], sh.mass[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (d.has_k) __hip_atomic_store(&g[slice].count[i], sh.count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0);  // this thread's sums are there
+    asm volatile("" ::: "memory");
     __syncthreads();
     if (tid == 0)
       sh.last = __hip_atomic_fetch_add(&p.done[row], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)slices - 1;
     __syncthreads();
+    asm volatile("" ::: "memory");
     if (!sh.last) return;
     unsigned long long m[kBinsPer] = {};
     uint32_t n[kBinsPer] = {};
