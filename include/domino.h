@@ -413,7 +413,8 @@ size_t domino_top_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t k)
  *  top_ids         device int32 [rows][k], in order
  *  top_vals        device fp32 [rows][k]: their logits (not divided by T)
  *  rest            optional device fp32 [rows]: log of the sum over every other id
- *                  of exp(logit / T); -inf where there is none above -inf
+ *                  of exp(logit / T); -inf where there is none above -inf, +inf where
+ *                  one is +inf
  */
 domino_status domino_top_logits(int32_t rows, int32_t vocab, int32_t k, const void *logits, domino_dtype logits_dtype,
                                 int64_t ld, float temperature, int32_t *top_ids, float *top_vals, float *rest,
@@ -438,7 +439,9 @@ size_t domino_distill_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
  *  teacher_vals    device fp32 [rows][k]: t (NaN counts as -inf)
  *  teacher_rest    optional device fp32 [rows]: rest_t, as domino_top_logits gives it
  *                  at the same T; NULL: -inf, the teacher is its entries alone
- *                  A row whose teacher has no weight at all has loss and gradient 0.
+ *                  A row whose teacher has no weight at all has loss and gradient 0.  In another
+ *                  one a logit, a teacher_vals or a teacher_rest of +inf (which domino_top_logits
+ *                  gives where more than k logits are +inf) makes the loss and the gradient NaN.
  *  temperature     T in [1e-30, 1e30]
  *  row_weights     optional device fp32 [rows]: w >= 0 and finite, NULL: 1.  A row of
  *                  weight 0 adds nothing to the loss and its gradient is 0, whatever it

@@ -54,7 +54,9 @@ def distill_row(row, ids, vals, rest, T):
     t = np.append(t, rest)
     if t.max() == -np.inf:
         return 0.0, grad
-    t = t if np.isinf(t.max()) else t - t.max()
+    if t.max() == np.inf or row.max() == np.inf:  # no distribution
+        return np.nan, np.full(V, np.nan)
+    t = t - t.max()
     log_p = t - _lse(t)
     p = np.exp(log_p)
     # (relative to the maximum: log(V) is lost beside values near the type's lowest)
@@ -69,7 +71,7 @@ def distill_row(row, ids, vals, rest, T):
     loss = T * T * np.sum(p[some] * (log_p[some] - log_q[some]))
     grad[ids] = T * (q[:-1] - p[:-1])
     if lr > -np.inf:
-        zo = z[others] if np.isinf(lr) else z[others] - z[others].max()
+        zo = z[others] - z[others].max()
         grad[others] = T * np.exp(zo - _lse(zo)) * (q[-1] - p[-1])
     return loss, grad
 

@@ -220,6 +220,7 @@ __global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs a) 
   const bool bad = mx[3] != 0.f;
   const double tm = fmax((double)mx[2] * inv_t, (double)rt);
   const bool none = tm == -INFINITY;  // the teacher says nothing of this row
+  const bool lost = bad || m == INFINITY || tm == INFINITY;  // its loss and gradient are NaN
   // sums relative to the maxima: R / exp(mr / T), the entries' part of Z / exp(m / T), P / exp(tm)
   double e[kPer], pe[kPer], sum[3] = {0.0, 0.0, 0.0};
   if (p0.x != -INFINITY) sum[0] = (double)p0.y * exp(((double)p0.x - mr) * inv_t);  // (NaN in a row of +inf)
@@ -253,19 +254,19 @@ __global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs a) 
     if ((used >> j & 1) && !none && p != 0.0) kl[0] += p * (lp - lq);
     const int i = j * kDsThreads + tid;
     if (i < a.k)  // the entry's value is read, its gradient takes its place
-      z[i] = scale == 0.0 ? 0.f : bad ? NAN : used >> j & 1 ? (float)(scale * (q - p)) : 0.f;
+      z[i] = scale == 0.0 ? 0.f : lost ? NAN : used >> j & 1 ? (float)(scale * (q - p)) : 0.f;
   }
   if (tid == 64) {  // the bucket of the other ids, beside the entries' of the first wave
     const double lpr = ((double)rt - tm) - log_P, lqr = R == 0.0 ? -INFINITY : r_m + (log(R) - log_Z);
     const double pr = none || rt == -INFINITY ? 0.0 : exp(lpr);
     if (!none && pr != 0.0) kl[0] += pr * (lpr - lqr);
     // the gradient of any other id: exp((l - mr) / T) times this
-    const double coef = scale == 0.0 ? 0.0 : bad ? NAN : R == 0.0 ? 0.0 : scale * (exp(lqr) - pr) / R;
+    const double coef = scale == 0.0 ? 0.0 : lost ? NAN : R == 0.0 ? 0.0 : scale * (exp(lqr) - pr) / R;
     a.stat[row] = make_float2(mr == -INFINITY ? 0.f : mr, (float)coef);
   }
   block_sums(kl, red + 3);
   if (tid == 0) {
-    const double loss = bad ? NAN : none ? 0.0 : (double)a.T * (double)a.T * kl[0];
+    const double loss = bad ? NAN : none ? 0.0 : lost ? NAN : (double)a.T * (double)a.T * kl[0];
     if (bad) raise_error(a.err, DEV_BAD_TOKEN);
     if (row == 0 && odd_weights != 0.0) raise_error(a.err, DEV_BAD_PARAM);
     a.row_loss[row] = (float)loss;

@@ -103,3 +103,17 @@ def test_sample_edges():
     assert ro.sample_row(np.full(4, -np.inf))[0] == -1
     assert ro.sample_row(np.array([0.0, np.inf, 1.0, np.inf]), u=0.75)[:2] == (3, -np.log(2))
     assert [ro.sample_row(np.zeros(4), top_p=0.5, u=u)[0] for u in (0.0, 0.49, 0.5, 0.99)] == [0, 0, 1, 1]
+
+
+def test_distill_of_infinities():
+    """+inf in the student's row, the teacher's entries or its rest: NaN, unless the teacher says nothing."""
+    x, inf = np.array([[0.0, 1.0, -1.0, 0.5]]), np.inf
+    for y, vals, rest in ((np.array([[0.0, inf, -1.0, 0.5]]), [[1.0, 0.0]], None),
+                          (np.array([[0.0, -inf, -inf, inf]]), [[1.0, 0.0]], None),
+                          (x, [[1.0, inf]], None), (x, [[1.0, 0.0]], [inf])):
+        got = ro.distill_loss(y, [[0, 3]], vals, rest)
+        assert np.isnan(got["loss"]) and np.isnan(got["grad"]).all()
+        got = ro.distill_loss(y, [[0, 3]], vals, rest, weights=[0.0])
+        assert got["loss"] == 0 and not got["grad"].any()
+    got = ro.distill_loss(np.array([[0.0, inf]]), [[-1]], [[1.0]])
+    assert got["loss"] == 0 and not got["grad"].any()
