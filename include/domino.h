@@ -442,7 +442,9 @@ size_t domino_distill_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
  *                  A row whose teacher has no weight at all has loss and gradient 0.  In another
  *                  one a logit, a teacher_vals or a teacher_rest of +inf (which domino_top_logits
  *                  gives where more than k logits are +inf) makes the loss and the gradient NaN.
- *  temperature     T in [1e-30, 1e30]
+ *  temperature     T in [1e-30, 1e4].  (Teacher and student differ by 1 / T, and the loss is T^2
+ *                  times what is left of that: the sum over the other ids is held to 2^-17 of
+ *                  itself, which is T 2^-17 of the difference.)
  *  row_weights     optional device fp32 [rows]: w >= 0 and finite, NULL: 1.  A row of
  *                  weight 0 adds nothing to the loss and its gradient is 0, whatever it
  *                  holds; another value sets DOMINO_DEV_BAD_PARAM and counts as 0.

@@ -47,16 +47,18 @@ def distill_row(row, ids, vals, rest, T):
     V = row.size
     grad = np.zeros(V)
     used = ids >= 0
-    ids, t = ids[used], np.where(np.isnan(vals[used]), -np.inf, vals[used]) / T
+    ids, t = ids[used], np.where(np.isnan(vals[used]), -np.inf, vals[used])
     rest = -np.inf if np.isnan(rest) else rest
     if np.any(ids >= V) or len(set(ids.tolist())) < ids.size:
         return np.nan, np.full(V, np.nan)
-    t = np.append(t, rest)
-    if t.max() == -np.inf:
+    top = max(t, default=-np.inf)
+    if max(top, rest) == -np.inf:
         return 0.0, grad
-    if t.max() == np.inf or row.max() == np.inf:  # no distribution
+    if max(top, rest) == np.inf or row.max() == np.inf:  # no distribution
         return np.nan, np.full(V, np.nan)
-    t = t - t.max()
+    # relative to the larger of the first entry and the rest; differences first, t / T alone may be 1e38
+    # (the rest's is of one product and one sum: 0 where it rounds past the other)
+    t = np.append((t - top) / T, min(rest - top / T, 0.0)) if top / T >= rest else np.append(np.minimum(t / T - rest, 0.0), 0.0)
     log_p = t - _lse(t)
     p = np.exp(log_p)
     # (relative to the maximum: log(V) is lost beside values near the type's lowest)

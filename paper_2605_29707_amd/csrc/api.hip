@@ -1387,7 +1387,9 @@ domino_status domino_distill_loss(int32_t rows, int32_t vocab, int32_t k, const 
                                   void *workspace, size_t workspace_bytes, void *stream) {
   if (domino_status s = check_rows(rows, vocab, logits, logits_dtype, ld); s != DOMINO_OK) return s;
   if (k < 1 || k > 1024 || k > vocab) return fail(DOMINO_ERR_INVALID_ARG, "k must be in [1, 1024] and at most vocab");
-  if (domino_status s = check_temperature(temperature); s != DOMINO_OK) return s;
+  // (beyond: T^2 times a difference of logarithms has no digits left)
+  if (!(temperature >= kRowsMinT && temperature <= kDistillMaxT))
+    return fail(DOMINO_ERR_INVALID_ARG, "temperature must be in [1e-30, 1e4]");
   if (!std::isfinite(grad_scale)) return fail(DOMINO_ERR_INVALID_ARG, "grad_scale must be finite");
   if (!teacher_ids || !teacher_vals || !loss) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
   if (grad && ((uintptr_t)grad % (logits_dtype == DOMINO_BF16 ? 2 : 4) || ld_grad < vocab))

@@ -218,10 +218,16 @@ __global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs a) 
   block_maxima(mx, redf);
   const float mr = mx[0], m = fmaxf(mx[0], mx[1]);
   const bool bad = mx[3] != 0.f;
-  const double tm = fmax((double)mx[2] * inv_t, (double)rt);
+  // The teacher's logits over T relative to the largest of them and the rest: differences first, since t / T alone may
+  // be 1e38, where one step is more than the differences.  (Products and sums contract: without the minimum
+  // what rounds to 0 could be a step above it.)
+  const double te = (double)mx[2] * inv_t, tm = fmax(te, (double)rt);
+  const bool by_rest = rt > te;
+  auto teacher = [&](float t) { return by_rest ? fmin((double)t * inv_t - rt, 0.0) : ((double)t - mx[2]) * inv_t; };
+  const double tr = by_rest ? 0.0 : fmin(rt - te, 0.0);
   const bool none = tm == -INFINITY;  // the teacher says nothing of this row
   const bool lost = bad || m == INFINITY || tm == INFINITY;  // its loss and gradient are NaN
-  // sums relative to the maxima: R / exp(mr / T), the entries' part of Z / exp(m / T), P / exp(tm)
+  // sums relative to the maxima: R / exp(mr / T), the entries' part of Z / exp(m / T), the teacher's P
   double e[kPer], pe[kPer], sum[3] = {0.0, 0.0, 0.0};
   if (p0.x != -INFINITY) sum[0] = (double)p0.y * exp(((double)p0.x - mr) * inv_t);  // (NaN in a row of +inf)
   for (int c = kDsThreads + tid; c < a.nch; c += kDsThreads) {
@@ -233,13 +239,13 @@ __global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs a) 
     e[j] = pe[j] = 0.0;
     if (j * kDsThreads < a.k) {  // uniform
       if (zi[j] != -INFINITY) e[j] = exp(((double)zi[j] - m) * inv_t);
-      if (ti[j] != -INFINITY) pe[j] = exp((double)ti[j] * inv_t - tm);
+      if (ti[j] != -INFINITY) pe[j] = exp(teacher(ti[j]));
       sum[1] += e[j];
       sum[2] += pe[j];
     }
   }
   block_sums(sum, red);
-  const double R = sum[0], P = sum[2] + (rt != -INFINITY ? exp((double)rt - tm) : 0.0);
+  const double R = sum[0], P = sum[2] + (rt != -INFINITY ? exp(tr) : 0.0);
   // logarithms relative to the maxima: beside values near the type's lowest log(V) would be lost
   const double r_m = ((double)mr - m) * inv_t, Zr = R != 0.0 ? R * exp(r_m) : 0.0, Z = sum[1] + Zr;
   const double log_Z = log(Z), log_P = log(P);  // Z = 0: no student logit above -inf
@@ -249,7 +255,7 @@ __global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs a) 
   for (int j = 0; j < kPer; ++j) {
     if (j * kDsThreads >= a.k) break;  // uniform
     const double p = pe[j] / P, q = zi[j] == -INFINITY ? 0.0 : e[j] / Z;
-    const double lp = ((double)ti[j] * inv_t - tm) - log_P;
+    const double lp = teacher(ti[j]) - log_P;
     const double lq = zi[j] == -INFINITY ? -INFINITY : ((double)zi[j] - m) * inv_t - log_Z;
     if ((used >> j & 1) && !none && p != 0.0) kl[0] += p * (lp - lq);
     const int i = j * kDsThreads + tid;
@@ -257,7 +263,7 @@ __global__ __launch_bounds__(kDsThreads) void distill_row_kernel(DistillArgs a) 
       z[i] = scale == 0.0 ? 0.f : lost ? NAN : used >> j & 1 ? (float)(scale * (q - p)) : 0.f;
   }
   if (tid == 64) {  // the bucket of the other ids, beside the entries' of the first wave
-    const double lpr = ((double)rt - tm) - log_P, lqr = R == 0.0 ? -INFINITY : r_m + (log(R) - log_Z);
+    const double lpr = tr - log_P, lqr = R == 0.0 ? -INFINITY : r_m + (log(R) - log_Z);
     const double pr = none || rt == -INFINITY ? 0.0 : exp(lpr);
     if (!none && pr != 0.0) kl[0] += pr * (lpr - lqr);
     // the gradient of any other id: exp((l - mr) / T) times this

@@ -295,6 +295,7 @@ size_t draw_ws_bytes(int rows, int V);
 void launch_sample_logits(RowsArgs a, bool bf16, SampleArgs p, void *ws, hipStream_t st);
 
 // ---- distillation from a teacher's top entries (distill.hip)
+constexpr float kDistillMaxT = 1e4f;
 struct DistillArgs {
   int rows, V, k, nch;
   const void *logits;
