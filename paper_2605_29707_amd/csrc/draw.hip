@@ -280,7 +280,7 @@ struct WholeShared {
   uint32_t sort[kWholeThreads], red[kWholeWaves];  // of sort_list
   int hit_i, last, n[2], wave_n[2][kWholeWaves];
 };
-static_assert(sizeof(WholeShared) <= 65536, "two workgroups a CU, static LDS");
+static_assert(sizeof(WholeShared) <= 65536, "static LDS");
 constexpr int kBinsPer = (kBins + kWholeThreads - 1) / kWholeThreads;  // bins a thread
 constexpr int kSeg = 2 * kListMax / kWholeWaves;                      // a wave's part of a list while it is ids
 
@@ -768,7 +768,8 @@ DEVI void draw_whole(const RowsArgs &a, const SampleArgs &p, const DrawRow &d, i
 }
 
 // The rows that are left, a workgroup a slice of each.  (Slices that go by how many rows are left, from a
-// list of them, are no faster: their parameters come three dependent loads later.)
+// list of them, are no faster: their parameters come three dependent loads later.)  Its 128 registers, all that
+// 16 waves can have, keep it to one workgroup a CU, and it spills 37 of them (35 with fp32 logits).
 template <typename LT>
 __global__ __launch_bounds__(kWholeThreads) void draw_whole_kernel(RowsArgs a, SampleArgs p) {
   __shared__ WholeShared sh;
@@ -783,7 +784,9 @@ __global__ __launch_bounds__(kWholeThreads) void draw_whole_kernel(RowsArgs a, S
 
 // Workgroups a row of the last launch: for few rows as many as cut a row of 128K ids to 8K each (64
 // rows of 128256 fp32 logits, the flat ones: 46 us, 66 with one), for many enough to fill the chip
-// (512 rows of 151936 bf16 logits, 64 of them flat: 78 us with one, 67 with two, 99 with four).
+// (512 rows of 151936 bf16 logits, 64 of them flat: 78 us with one, 67 with two, 99 with four.  What four
+// cost is not the work of a slice; most likely it is the many workgroups without a row left, each of which takes
+// a CU to itself.  Not traced.)
 static int draw_slices(int rows, int V) { return std::max(1, std::min({16, 1024 / rows, V / 8192})); }
 
 // [error word and groups][a row each: state, workgroups done][sums, where a row has several workgroups]
