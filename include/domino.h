@@ -62,7 +62,8 @@ enum {
   DOMINO_DEV_BAD_CTX_LEN = 2,     /* ctx_lens[b] outside [n_new, max_ctx] (clamped) */
   DOMINO_DEV_BAD_TREE = 4,        /* a node_parent entry that is not an earlier node (ignored) */
   DOMINO_DEV_BARRIER_TIMEOUT = 8, /* a bounded cross-workgroup wait of the rollout exceeded its spin bound */
-  DOMINO_DEV_BAD_PARAM = 16       /* a row's temperature, top_p, min_p, uniform or weight out of its range */
+  DOMINO_DEV_BAD_PARAM = 16,      /* a row's temperature, top_p, min_p, uniform or weight out of its range */
+  DOMINO_DEV_BAD_PAGE = 32        /* a page table entry of a slot in use that is none of the cache's pages */
 };
 
 /*
@@ -493,6 +494,151 @@ domino_status domino_sample_logits(int32_t rows, int32_t vocab, const void *logi
                                    const float *temperature, const int32_t *top_k, const float *top_p,
                                    const float *min_p, const float *uniforms, int32_t *tokens, float *logprobs,
                                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A key/value cache of pages, for serving many sequences beside each other: slot s of
+ * sequence b (its s-th row) is row s % page_size of page page_table[b][s / page_size], in
+ * every layer.  Strides are in elements and shared by k and v, so that a page may be
+ * stored slot by slot ([page_size][n_kv_heads][head_dim], as the dense caches above) or
+ * head by head; the head_dim elements of a row are dense.  Rows start at multiples of 16 bytes
+ * (strides, k and v).  No two rows overlap.
+ *  k, v            device, storage type; K is post k-norm and RoPE
+ *  weights         device fp32 [n_layers][n_pages][n_kv_heads][page_size], the attention
+ *                  weight that every slot has received, or NULL (domino_paged_evict needs it)
+ *  page_table      device int32 [batch][max_pages]; only entries of slots in use are read
+ *  page_size       a power of two up to 65536; max_pages * page_size below 2^30
+ *  head_dim        64 or 128
+ * For the calls below
+ *  seq_starts      device int32 [batch + 1]: rows [seq_starts[b], seq_starts[b + 1]) of the
+ *                  packed new tokens are sequence b's (none: the sequence waits).  Rows behind the
+ *                  last sequence are left as they are
+ *  kv_lens         device int32 [batch]: slots in use, the new tokens' own included (they are
+ *                  the last ones).  A sequence whose starts and lengths disagree, or pass the
+ *                  limits that the call was given, is left out: DOMINO_DEV_BAD_CTX_LEN
+ *  a table entry of a slot in use that is not in [0, n_pages) sets DOMINO_DEV_BAD_PAGE: nothing is
+ *                  written to such a slot, and what is read from it is undefined
+ *  sequences may share pages that a call only reads; a page that a call writes (weights
+ *                  included) belongs to one sequence
+ *  workspace       device, aligned to 16 bytes; its first word is an error word that calls
+ *                  set and do not clear (one look at it covers a step's calls over all layers):
+ *                  zero it before the first call (domino_workspace_clear_error)
+ */
+typedef struct {
+  void *k, *v;
+  float *weights;
+  const int32_t *page_table;
+  int64_t layer_stride, page_stride, slot_stride, head_stride;
+  int32_t n_layers, n_pages, page_size, n_kv_heads, head_dim, batch, max_pages;
+  domino_dtype dtype;
+} domino_paged_cache;
+
+#define DOMINO_PAGED_WORKSPACE_BYTES 16u /* of calls without a query of their own */
+
+/* How rotary positions are stretched beyond the length that a model was trained on. */
+typedef enum {
+  DOMINO_ROPE_NONE = 0,
+  DOMINO_ROPE_LINEAR = 1, /* every frequency divided by factor (position interpolation) */
+  DOMINO_ROPE_NTK = 2,    /* theta multiplied by factor^(d / (d - 2)), d = rotary_dim */
+  DOMINO_ROPE_YARN = 3    /* YaRN (Peng et al. 2023): with r the turns a frequency makes in original_ctx positions, divided
+                             by factor where r <= beta_slow, kept where r >= beta_fast, linear in r between;
+                             rotated elements times 0.1 ln(factor) + 1 */
+} domino_rope_scaling;
+
+/*
+ * The angles a position of the rotary_dim / 2 rotated pairs, theta^(-2i / rotary_dim) for
+ * pair i, scaled.  Runs on the host.
+ *  rotary_dim      even, in [2, 128] (4 or more for DOMINO_ROPE_NTK); theta > 1
+ *  factor          >= 1 (unused by DOMINO_ROPE_NONE); original_ctx >= 1 and
+ *                  beta_fast > beta_slow > 0 for DOMINO_ROPE_YARN, else unused
+ *  frequencies     host fp64 [rotary_dim / 2]; rope_scale host fp32 [1]
+ */
+domino_status domino_rope_frequencies(int32_t rotary_dim, double theta, domino_rope_scaling scaling, double factor,
+                                      int32_t original_ctx, double beta_fast, double beta_slow, double *frequencies,
+                                      float *rope_scale);
+
+/*
+ * New tokens' queries and keys with their rotary positions, and keys and values stored
+ * into the pages.  A q or k head x becomes, each step optional, x * rsqrt(mean(x^2) + rms_eps) * gain and then, for the
+ * pairs (x_i, x_(i + rotary_dim / 2)), or (x_2i, x_(2i + 1)) where interleaved, rope_scale times
+ * (x cos a - y sin a, y cos a + x sin a) with a = position * frequencies[i]; elements from rotary_dim on
+ * are not rotated (nor scaled).  fp32 arithmetic, angles in fp64, one rounding.
+ *  layer           of the cache
+ *  q, k, v         device [tokens][n_q_heads or n_kv_heads][head_dim] in the storage type, tokens
+ *                  *_stride elements apart (parts of one projection's rows, say); 16-byte rows
+ *  q_out           device, as q; q itself, or apart from q, k and v
+ *  positions       optional device int32 [tokens]; NULL: the token's slot.  (After an eviction slots
+ *                  are no positions any more.)
+ *  frequencies     device fp64 [rotary_dim / 2]; rotary_dim 0: no rotation (NULL), else a multiple of 16 up to head_dim
+ *  q_norm, k_norm  optional device [head_dim] gains in the storage type
+ * The slots' weights become 0 where the cache has weights.
+ */
+domino_status domino_paged_append(const domino_paged_cache *cache, int32_t layer, int32_t tokens, int32_t n_q_heads,
+                                  const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                                  int64_t v_stride, void *q_out, int64_t q_out_stride, const int32_t *seq_starts,
+                                  const int32_t *kv_lens, const int32_t *positions, const double *frequencies,
+                                  int32_t rotary_dim, int32_t interleaved, float rope_scale, const void *q_norm,
+                                  const void *k_norm, float rms_eps, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace domino_paged_attention needs (0 for arguments that it refuses). */
+size_t domino_paged_attention_workspace_bytes(const domino_paged_cache *cache, int32_t tokens, int32_t n_q_heads,
+                                              int32_t max_new, int32_t max_len, int32_t accumulate);
+
+/*
+ * Attention of the new tokens (in the pages already) over their sequences' slots: the
+ * softmax(scale q k) v of grouped-query heads, from one token a sequence (decoding) to chunks of a
+ * prompt, or the drafted nodes of domino_build_tree.
+ * Every row sees the slots before the new ones; of the new ones token i sees 0 .. i, or with
+ * a mask those with mask[t][j] != 0 (t its packed row, j the other's place among the
+ * sequence's new tokens; the diagonal counts for nothing by itself).  A row that sees no slot with a score above -inf
+ * has output 0 and lse -inf.
+ *  max_new, max_len  at least every sequence's new tokens and slots; they choose the launch
+ *  q, out          device [tokens][n_q_heads][head_dim], storage type, tokens *_stride apart, 16-byte rows; not the same memory.
+ *                  n_q_heads a multiple of n_kv_heads
+ *  scale           positive and finite
+ *  mask            optional device uint8 [tokens] rows mask_ld apart, mask_ld >= max_new
+ *                  (ancestor_mask of trees of one size: mask_ld = n_nodes = max_new)
+ *  lse             optional device fp32 [tokens][n_q_heads]: log of the sum of exp of a row's scores
+ *  accumulate      not 0: cache->weights[slot] += the sum, over the sequence's new tokens and the query heads
+ *                  of the kv head, of their attention weight
+ * Deterministic: no floating-point atomics.
+ */
+domino_status domino_paged_attention(const domino_paged_cache *cache, int32_t layer, int32_t tokens, int32_t n_q_heads,
+                                     int32_t max_new, int32_t max_len, const void *q, int64_t q_stride, void *out,
+                                     int64_t out_stride, const int32_t *seq_starts, const int32_t *kv_lens, float scale,
+                                     const uint8_t *mask, int64_t mask_ld, float *lse, int32_t accumulate, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace domino_paged_evict needs (0 for arguments that it refuses). */
+size_t domino_paged_evict_workspace_bytes(const domino_paged_cache *cache, int32_t max_len, int32_t budget);
+
+/*
+ * Sequences of more than `budget` slots are cut to it, each layer and kv head by its own
+ * weights: the first `sink` slots stay, the last `recent`, and of those between them the ones with the greatest weight
+ * (value desc, slot asc; NaN lowest, the zeros of both signs equal).  What stays keeps its order: the i-th kept slot's
+ * rows and weight become slot i's.
+ *  kv_lens         device int32 [batch] in [0, max_len]; new_lens device int32 [batch], not kv_lens: min(kv_lens, budget)
+ *  budget          >= sink + recent; sink, recent >= 0
+ *  new_table       NULL: in place, pages behind the budget are free afterwards (their contents are undefined).  Else device
+ *                  int32 [batch][new_pages], new_pages * page_size >= budget: the kept rows (of every
+ *                  sequence, also those within the budget) go to these pages, none of which is in use, and the old ones are left as they are
+ *  kept            optional device int32 [n_layers][batch][n_kv_heads][budget]: the slots that stay, -1 padded
+ */
+domino_status domino_paged_evict(const domino_paged_cache *cache, const int32_t *kv_lens, int32_t *new_lens, int32_t max_len,
+                                 int32_t budget, int32_t sink, int32_t recent, const int32_t *new_table, int32_t new_pages,
+                                 int32_t *kept, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * domino_target_commit on pages: the drafted nodes' rows are in slots ctx_lens[b] + node; node 0 and the
+ * accepted path (accepted_nodes[b][0 .. accept_len[b]-1]) become slots ctx_lens[b] .. ctx_lens[b] + accept_len[b] of every
+ * layer, with their weights; new_ctx_lens[b] = ctx_lens[b] + 1 + accept_len[b].  The node at depth d has an id in
+ * [d, n_nodes), else DOMINO_DEV_BAD_TREE; a sequence with that, lengths out of range or a bad page is left
+ * unchanged (new_ctx_lens[b] = ctx_lens[b]).
+ *  max_depth       the row stride of accepted_nodes, in [1, 63]; n_nodes in [1, 1024]
+ *  ctx_lens        device int32 [batch]: slots before node 0's; new_ctx_lens device int32 [batch], not ctx_lens
+ */
+domino_status domino_paged_commit(const domino_paged_cache *cache, int32_t n_nodes, int32_t max_depth,
+                                  const int32_t *ctx_lens, const int32_t *accept_len, const int32_t *accepted_nodes,
+                                  int32_t *new_ctx_lens, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Philox-4x32-10 (Salmon et al., SC 2011) of n explicit counters: counters
  * device uint32 [n][4], key = (key lo, key hi) 32-bit words, out device uint32

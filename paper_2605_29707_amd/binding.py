@@ -22,7 +22,10 @@ DOMINO_ERR_HIP = -4
 DOMINO_ERR_DEVICE = -5
 DOMINO_F32, DOMINO_BF16 = 0, 1
 
-DEV_BAD_TOKEN, DEV_BAD_CTX_LEN, DEV_BAD_TREE, DEV_BARRIER_TIMEOUT, DEV_BAD_PARAM = 1, 2, 4, 8, 16
+DEV_BAD_TOKEN, DEV_BAD_CTX_LEN, DEV_BAD_TREE, DEV_BARRIER_TIMEOUT, DEV_BAD_PARAM, DEV_BAD_PAGE = 1, 2, 4, 8, 16, 32
+
+DOMINO_ROPE_NONE, DOMINO_ROPE_LINEAR, DOMINO_ROPE_NTK, DOMINO_ROPE_YARN = 0, 1, 2, 3
+DOMINO_PAGED_WORKSPACE_BYTES = 16
 
 KERNEL_CLASSES = ["embed", "norm", "qkv", "rope", "attn", "wo", "gateup", "down", "lmhead", "w1h",
                   "headloop", "ctxproj", "trainloss"]
@@ -49,6 +52,13 @@ class domino_weights(C.Structure):
 
 class domino_debug(C.Structure):
     _fields_ = [(n, _VP) for n in ("hidden", "base_logits", "final_logits", "states")]
+
+
+class domino_paged_cache(C.Structure):
+    _fields_ = [(n, _VP) for n in ("k", "v", "weights", "page_table")] + [
+        (n, C.c_int64) for n in ("layer_stride", "page_stride", "slot_stride", "head_stride")] + [
+        (n, C.c_int32) for n in ("n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim", "batch", "max_pages")] + [
+        ("dtype", C.c_int)]
 
 
 class DominoError(RuntimeError):
@@ -101,6 +111,16 @@ def load() -> C.CDLL:
                                       C.c_int64, P, sz, P]),
         "domino_sample_logits_workspace_bytes": (sz, [i32, i32]),
         "domino_sample_logits": (i32, [i32, i32, P, C.c_int, C.c_int64, P, P, P, P, P, P, P, P, sz, P]),
+        "domino_rope_frequencies": (i32, [i32, C.c_double, C.c_int, C.c_double, i32, C.c_double, C.c_double, P,
+                                          C.POINTER(C.c_float)]),
+        "domino_paged_append": (i32, [P, i32, i32, i32, P, C.c_int64, P, C.c_int64, P, C.c_int64, P, C.c_int64, P, P, P, P,
+                                      i32, i32, C.c_float, P, P, C.c_float, P, sz, P]),
+        "domino_paged_attention_workspace_bytes": (sz, [P, i32, i32, i32, i32, i32]),
+        "domino_paged_attention": (i32, [P, i32, i32, i32, i32, i32, P, C.c_int64, P, C.c_int64, P, P, C.c_float, P,
+                                         C.c_int64, P, i32, P, sz, P]),
+        "domino_paged_evict_workspace_bytes": (sz, [P, i32, i32]),
+        "domino_paged_evict": (i32, [P, P, P, i32, i32, i32, i32, P, i32, P, P, sz, P]),
+        "domino_paged_commit": (i32, [P, i32, i32, P, P, P, P, P, sz, P]),
         "domino_train_workspace_bytes": (sz, [P, i32, i32, i32]),
         "domino_target_create": (i32, [C.POINTER(domino_config), C.POINTER(domino_weights), C.POINTER(P)]),
         "domino_target_workspace_bytes": (sz, [P, i32, i32, i32]),
@@ -127,7 +147,9 @@ def exported_symbols():
             "domino_distill_workspace_bytes", "domino_distill_loss", "domino_sample_logits_workspace_bytes",
             "domino_sample_logits", "domino_train_workspace_bytes", "domino_train_forward",
             "domino_target_create", "domino_target_workspace_bytes", "domino_target_verify", "domino_target_commit",
-            "domino_debug_set_poll_limit", "domino_debug_last_paths", "domino_verify_accept_noalloc"]
+            "domino_debug_set_poll_limit", "domino_debug_last_paths", "domino_verify_accept_noalloc",
+            "domino_rope_frequencies", "domino_paged_append", "domino_paged_attention_workspace_bytes",
+            "domino_paged_attention", "domino_paged_evict_workspace_bytes", "domino_paged_evict", "domino_paged_commit"]
 
 
 def last_error() -> str:
@@ -422,6 +444,170 @@ def domino_sample_logits(logits, uniforms, tokens, workspace, temperature=None, 
     _check(load().domino_sample_logits(n, V, _ptr(logits), dt, ld, _ptr(temperature), _ptr(top_k), _ptr(top_p),
                                        _ptr(min_p), _ptr(uniforms), _ptr(tokens), _ptr(logprobs), _ptr(workspace),
                                        workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+class PagedCache:
+    """A domino_paged_cache over tensors, which it keeps alive: k, v [layers, pages, page_size, n_kv, head_dim] (a single
+    layer's may leave the first out) of equal strides, rows dense, so that pages stored head by head are passed as
+    transposed views; page_table int32 [batch, max_pages]; weights fp32 [layers, pages, n_kv, page_size]."""
+
+    def __init__(self, k, v, page_table, weights=None):
+        import torch
+        bad = lambda msg: DominoError(DOMINO_ERR_INVALID_ARG, msg)  # noqa: E731
+        if k.dim() == 4 and v.dim() == 4:
+            k, v = k[None], v[None]
+        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.float32, torch.bfloat16):
+            raise bad("k and v must be fp32 or bf16 tensors [layers, pages, page_size, n_kv, head_dim] of one shape and type")
+        if 0 in k.shape:
+            raise bad("k and v must not be empty")
+        dh = k.shape[4]
+        strides = [st if n > 1 else dh for n, st in zip(k.shape[:4], k.stride())]
+        if strides != [st if n > 1 else dh for n, st in zip(v.shape[:4], v.stride())] or 1 not in (k.stride(4), dh) \
+                or 1 not in (v.stride(4), dh):
+            raise bad("k and v must have equal strides and dense rows")
+        dev = k.get_device()
+        if v.get_device() != dev:
+            raise bad("k and v must be on one device")
+        if page_table.dim() != 2 or page_table.numel() == 0:
+            raise bad("page_table must be [batch, max_pages]")
+        _check_array("page_table", page_table, dev, torch.int32, page_table.numel())
+        layers, pages, size, nkv = k.shape[:4]
+        _check_array("weights", weights, dev, torch.float32, layers * pages * nkv * size)
+        if weights is not None and tuple(weights.shape[-3:]) != (pages, nkv, size):
+            raise bad("weights must be [layers, pages, n_kv, page_size]")
+        self.k, self.v, self.page_table, self.weights, self.device, self.dtype = k, v, page_table, weights, dev, k.dtype
+        self.n_layers, self.page_size, self.n_kv, self.head_dim, self.batch = layers, size, nkv, dh, page_table.shape[0]
+        self.struct = domino_paged_cache(
+            k=_ptr(k), v=_ptr(v), weights=_ptr(weights), page_table=_ptr(page_table), layer_stride=strides[0],
+            page_stride=strides[1], slot_stride=strides[2], head_stride=strides[3], n_layers=layers, n_pages=pages,
+            page_size=size, n_kv_heads=nkv, head_dim=dh, batch=page_table.shape[0], max_pages=page_table.shape[1],
+            dtype=DOMINO_BF16 if k.dtype is torch.bfloat16 else DOMINO_F32)
+        self.ref = C.byref(self.struct)
+
+
+def _heads(cache: PagedCache, name, t, tokens=None, heads=None):
+    """(tokens, heads, token stride) of a [tokens, heads, head_dim] tensor whose tokens' heads are dense."""
+    if t.dim() != 3 or t.shape[2] != cache.head_dim or t.dtype != cache.dtype or t.get_device() != cache.device \
+            or (tokens is not None and t.shape[0] != tokens) or (heads is not None and t.shape[1] != heads):
+        raise DominoError(DOMINO_ERR_INVALID_ARG,
+                          f"{name} must be [tokens, heads, head_dim] of the cache's type, on its device")
+    (n, h, dh), (ld, lh, one) = t.shape, t.stride()
+    if one != 1 or (h > 1 and lh != dh):
+        raise DominoError(DOMINO_ERR_INVALID_ARG, f"{name} must have dense heads")
+    return n, h, ld if n > 1 else h * dh
+
+
+def domino_rope_frequencies(rotary_dim, theta, scaling=DOMINO_ROPE_NONE, factor=1.0, original_ctx=0, beta_fast=32.0,
+                            beta_slow=1.0):
+    """(fp64 numpy array [rotary_dim / 2], rope_scale)."""
+    f, scale = np.empty(max(int(rotary_dim), 0) // 2, dtype=np.float64), C.c_float(0)
+    _check(load().domino_rope_frequencies(int(rotary_dim), float(theta), int(scaling), float(factor), int(original_ctx),
+                                          float(beta_fast), float(beta_slow), f.ctypes.data, C.byref(scale)))
+    return f, float(scale.value)
+
+
+def domino_paged_append(cache: PagedCache, q, k, v, q_out, seq_starts, kv_lens, workspace, layer=0, positions=None,
+                        frequencies=None, rope_scale=1.0, interleaved=False, q_norm=None, k_norm=None, rms_eps=1e-6,
+                        stream=None):
+    """q, q_out [tokens, n_q, head_dim], k, v [tokens, n_kv, head_dim]; frequencies fp64 on the device, two elements of a
+    head for each."""
+    import torch
+    dev, i32 = cache.device, torch.int32
+    n, nq, lq = _heads(cache, "q", q)
+    _, _, lk = _heads(cache, "k", k, n, cache.n_kv)
+    _, _, lv = _heads(cache, "v", v, n, cache.n_kv)
+    _, _, lo = _heads(cache, "q_out", q_out, n, nq)
+    _check_array("seq_starts", seq_starts, dev, i32, cache.batch + 1)
+    _check_array("kv_lens", kv_lens, dev, i32, cache.batch)
+    _check_array("positions", positions, dev, i32, n)
+    if frequencies is not None:
+        _check_array("frequencies", frequencies, dev, torch.float64, frequencies.numel())
+    _check_array("q_norm", q_norm, dev, cache.dtype, cache.head_dim)
+    _check_array("k_norm", k_norm, dev, cache.dtype, cache.head_dim)
+    _check_device(dev, workspace)
+    _check(load().domino_paged_append(
+        cache.ref, int(layer), n, nq, _ptr(q), lq, _ptr(k), lk, _ptr(v), lv, _ptr(q_out), lo, _ptr(seq_starts),
+        _ptr(kv_lens), _ptr(positions), _ptr(frequencies), 0 if frequencies is None else 2 * frequencies.numel(),
+        int(bool(interleaved)), float(rope_scale), _ptr(q_norm), _ptr(k_norm), float(rms_eps), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def domino_paged_attention_workspace_bytes(cache: PagedCache, tokens, n_q_heads, max_new, max_len, accumulate=False) -> int:
+    n = load().domino_paged_attention_workspace_bytes(cache.ref, int(tokens), int(n_q_heads), int(max_new), int(max_len),
+                                                      int(bool(accumulate)))
+    if n == 0:
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "domino_paged_attention_workspace_bytes returned 0: " + last_error())
+    return int(n)
+
+
+def domino_paged_attention(cache: PagedCache, q, out, seq_starts, kv_lens, max_new, max_len, workspace, layer=0, scale=None,
+                           mask=None, lse=None, accumulate=False, stream=None):
+    """q, out [tokens, n_q, head_dim]; scale None: head_dim ** -0.5; mask uint8 or bool with dense rows, [tokens, >= max_new]
+    or [batch, n, n] of sequences that all have n new tokens; lse fp32 [tokens, n_q]."""
+    import torch
+    dev, i32 = cache.device, torch.int32
+    n, nq, lq = _heads(cache, "q", q)
+    _, _, lo = _heads(cache, "out", out, n, nq)
+    _check_array("seq_starts", seq_starts, dev, i32, cache.batch + 1)
+    _check_array("kv_lens", kv_lens, dev, i32, cache.batch)
+    _check_array("lse", lse, dev, torch.float32, n * nq)
+    mask_ld = 0
+    if mask is not None:
+        if mask.dim() == 3 and mask.is_contiguous():
+            mask = mask.view(-1, mask.shape[2])
+        if mask.dim() != 2 or mask.shape[0] != n or mask.dtype not in (torch.uint8, torch.bool) \
+                or mask.get_device() != dev or (mask.shape[1] > 1 and mask.stride(1) != 1) or mask.shape[1] < int(max_new):
+            raise DominoError(DOMINO_ERR_INVALID_ARG,
+                              "mask must be uint8 or bool rows of at least max_new, one for each token, on the cache's device")
+        mask_ld = mask.stride(0) if n > 1 else mask.shape[1]
+    _check_device(dev, workspace)
+    _check(load().domino_paged_attention(
+        cache.ref, int(layer), n, nq, int(max_new), int(max_len), _ptr(q), lq, _ptr(out), lo, _ptr(seq_starts),
+        _ptr(kv_lens), float(cache.head_dim ** -0.5 if scale is None else scale), _ptr(mask), mask_ld, _ptr(lse),
+        int(bool(accumulate)), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def domino_paged_evict_workspace_bytes(cache: PagedCache, max_len, budget) -> int:
+    n = load().domino_paged_evict_workspace_bytes(cache.ref, int(max_len), int(budget))
+    if n == 0:
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "domino_paged_evict_workspace_bytes returned 0: " + last_error())
+    return int(n)
+
+
+def domino_paged_evict(cache: PagedCache, kv_lens, new_lens, max_len, budget, workspace, sink=0, recent=0, new_table=None,
+                       kept=None, stream=None):
+    """new_table int32 [batch, pages]; kept int32 [layers, batch, n_kv, budget]."""
+    import torch
+    dev, i32 = cache.device, torch.int32
+    _check_array("kv_lens", kv_lens, dev, i32, cache.batch)
+    _check_array("new_lens", new_lens, dev, i32, cache.batch)
+    _check_array("kept", kept, dev, i32, cache.n_layers * cache.batch * cache.n_kv * int(budget))
+    if new_table is not None:
+        if new_table.dim() != 2:
+            raise DominoError(DOMINO_ERR_INVALID_ARG, "new_table must be [batch, pages]")
+        _check_array("new_table", new_table, dev, i32, cache.batch * new_table.shape[1])
+    _check_device(dev, workspace)
+    _check(load().domino_paged_evict(
+        cache.ref, _ptr(kv_lens), _ptr(new_lens), int(max_len), int(budget), int(sink), int(recent), _ptr(new_table),
+        0 if new_table is None else new_table.shape[1], _ptr(kept), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def domino_paged_commit(cache: PagedCache, n_nodes, ctx_lens, accept_len, accepted_nodes, new_ctx_lens, workspace,
+                        stream=None):
+    import torch
+    dev, i32 = cache.device, torch.int32
+    if accepted_nodes.dim() != 2:
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "accepted_nodes must be [batch, max_depth]")
+    depth = accepted_nodes.shape[1]
+    _check_array("ctx_lens", ctx_lens, dev, i32, cache.batch)
+    _check_array("accept_len", accept_len, dev, i32, cache.batch)
+    _check_array("accepted_nodes", accepted_nodes, dev, i32, cache.batch * depth)
+    _check_array("new_ctx_lens", new_ctx_lens, dev, i32, cache.batch)
+    _check_device(dev, workspace)
+    _check(load().domino_paged_commit(
+        cache.ref, int(n_nodes), depth, _ptr(ctx_lens), _ptr(accept_len), _ptr(accepted_nodes), _ptr(new_ctx_lens),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def domino_build_tree(topk_ids, anchor, ctx_lens, node_token, node_parent, node_depth, node_pos,

@@ -1430,6 +1430,286 @@ domino_status domino_distill_loss(int32_t rows, int32_t vocab, int32_t k, const 
   return DOMINO_OK;
 }
 
+// ---- paged cache
+namespace {
+domino_status check_paged(const domino_paged_cache *c) {
+  if (!c) return fail(DOMINO_ERR_INVALID_ARG, "cache is NULL");
+  if (c->dtype != DOMINO_F32 && c->dtype != DOMINO_BF16) return fail(DOMINO_ERR_INVALID_ARG, "bad cache dtype");
+  if (!c->k || !c->v || !c->page_table) return fail(DOMINO_ERR_INVALID_ARG, "a pointer of the cache is NULL");
+  if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->batch < 1 || c->max_pages < 1)
+    return fail(DOMINO_ERR_INVALID_ARG, "n_layers, n_pages, n_kv_heads, batch and max_pages must be >= 1");
+  if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
+    return fail(DOMINO_ERR_UNSUPPORTED, "page_size must be a power of two up to 65536");
+  if ((int64_t)c->max_pages * c->page_size >= (1 << 30))
+    return fail(DOMINO_ERR_UNSUPPORTED, "max_pages * page_size must be below 2^30");
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(DOMINO_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  const int64_t vec = c->dtype == DOMINO_BF16 ? 8 : 4;
+  const struct { int64_t stride; int32_t n; } dims[] = {
+      {c->layer_stride, c->n_layers}, {c->page_stride, c->n_pages}, {c->slot_stride, c->page_size}, {c->head_stride, c->n_kv_heads}};
+  for (const auto &d : dims)
+    if (d.n > 1 && (d.stride < c->head_dim || d.stride % vec))
+      return fail(DOMINO_ERR_INVALID_ARG, "a stride of the cache is below head_dim or no multiple of 16 bytes");
+  if ((uintptr_t)c->k % 16 || (uintptr_t)c->v % 16 || (uintptr_t)c->weights % 4 || (uintptr_t)c->page_table % 4)
+    return fail(DOMINO_ERR_INVALID_ARG, "a pointer of the cache is not aligned");
+  return DOMINO_OK;
+}
+PagedView paged_view(const domino_paged_cache *c) {
+  PagedView v;
+  v.k = (char *)c->k;
+  v.v = (char *)c->v;
+  v.weights = c->weights;
+  v.table = c->page_table;
+  v.layer_stride = c->layer_stride;
+  v.page_stride = c->page_stride;
+  v.slot_stride = c->slot_stride;
+  v.head_stride = c->head_stride;
+  v.n_layers = c->n_layers;
+  v.n_pages = c->n_pages;
+  v.page_shift = __builtin_ctz(c->page_size);
+  v.n_kv = c->n_kv_heads;
+  v.dh = c->head_dim;
+  v.batch = c->batch;
+  v.max_pages = c->max_pages;
+  v.bf16 = c->dtype == DOMINO_BF16;
+  return v;
+}
+domino_status check_paged_workspace(const void *ws, size_t have, size_t need) {
+  if (!ws) return fail(DOMINO_ERR_WORKSPACE, "workspace is NULL");
+  if ((uintptr_t)ws % 16) return fail(DOMINO_ERR_WORKSPACE, "workspace is not aligned to 16 bytes");
+  if (have < need) return fail(DOMINO_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", have, need);
+  return DOMINO_OK;
+}
+// packed rows of heads: aligned, and no rows on top of each other
+domino_status check_heads(const domino_paged_cache *c, const char *name, const void *p, int64_t stride, int32_t heads, int32_t tokens) {
+  const int64_t vec = c->dtype == DOMINO_BF16 ? 8 : 4;
+  if (!p) return fail(DOMINO_ERR_INVALID_ARG, "%s is NULL", name);
+  if ((uintptr_t)p % 16 || (tokens > 1 && (stride < (int64_t)heads * c->head_dim || stride % vec)))
+    return fail(DOMINO_ERR_INVALID_ARG, "%s: rows must be at least heads * head_dim apart and start at multiples of 16 bytes", name);
+  return DOMINO_OK;
+}
+domino_status check_tokens(const domino_paged_cache *c, int32_t layer, int32_t tokens, int32_t n_q_heads) {
+  if (layer < 0 || layer >= c->n_layers) return fail(DOMINO_ERR_INVALID_ARG, "layer must be in [0, n_layers)");
+  if (tokens < 1) return fail(DOMINO_ERR_INVALID_ARG, "tokens must be >= 1");
+  if (n_q_heads < 1 || n_q_heads % c->n_kv_heads) return fail(DOMINO_ERR_INVALID_ARG, "n_q_heads must be a multiple of n_kv_heads");
+  if ((int64_t)tokens * ((int64_t)n_q_heads + 2 * c->n_kv_heads) >= (1LL << 31) || tokens > kMaxBlocks)
+    return fail(DOMINO_ERR_UNSUPPORTED, "tokens * (n_q_heads + 2 n_kv_heads) must be below 2^31, tokens at most %ld", kMaxBlocks);
+  return DOMINO_OK;
+}
+struct PagedAttnLayout {
+  PagedAttnPlan plan;
+  size_t lse, ml, o, bytes;
+};
+domino_status paged_attn_layout(const domino_paged_cache *c, int32_t tokens, int32_t n_q_heads, int32_t max_new, int32_t max_len,
+                                int32_t accumulate, PagedAttnLayout &w) {
+  if (domino_status s = check_paged(c); s != DOMINO_OK) return s;
+  if (domino_status s = check_tokens(c, 0, tokens, n_q_heads); s != DOMINO_OK) return s;
+  if (max_new < 1 || max_len < 1) return fail(DOMINO_ERR_INVALID_ARG, "max_new and max_len must be >= 1");
+  if (max_len > c->max_pages * c->page_size) return fail(DOMINO_ERR_INVALID_ARG, "max_len must be at most max_pages * page_size");
+  if (accumulate && !c->weights) return fail(DOMINO_ERR_INVALID_ARG, "the cache has no weights to accumulate into");
+  w.plan = plan_paged_attn(c->dtype == DOMINO_BF16, tokens, c->batch, n_q_heads, c->n_kv_heads, std::min(max_new, tokens), max_len);
+  const int64_t slabs = accumulate ? (int64_t)c->batch * c->n_kv_heads * ((max_len + 127) / 128) : 0;
+  if ((double)w.plan.tiles * w.plan.splits * c->n_kv_heads > kMaxBlocks || slabs > kMaxBlocks ||
+      (int64_t)tokens * n_q_heads / 4 + 1 > kMaxBlocks)
+    return fail(DOMINO_ERR_UNSUPPORTED, "the call's work does not fit a launch");
+  const size_t rows = (size_t)tokens * n_q_heads;
+  w.lse = 256;
+  w.ml = w.lse + (accumulate ? align_up(rows * 4) : 0);
+  w.o = w.ml + (w.plan.splits > 1 ? align_up(rows * w.plan.splits * 8) : 0);
+  w.bytes = w.o + (w.plan.splits > 1 ? align_up(rows * w.plan.splits * c->head_dim * 4) : 0);
+  return DOMINO_OK;
+}
+domino_status check_evict(const domino_paged_cache *c, int32_t max_len, int32_t budget) {
+  if (domino_status s = check_paged(c); s != DOMINO_OK) return s;
+  if (!c->weights) return fail(DOMINO_ERR_INVALID_ARG, "the cache has no weights");
+  if (budget < 1 || max_len < 1) return fail(DOMINO_ERR_INVALID_ARG, "budget and max_len must be >= 1");
+  if (max_len > c->max_pages * c->page_size) return fail(DOMINO_ERR_INVALID_ARG, "max_len must be at most max_pages * page_size");
+  const int64_t heads = (int64_t)c->n_layers * c->batch * c->n_kv_heads;
+  if (budget > (1 << 21) || heads > (1 << 20) || heads * ((std::min(budget, max_len) + kEvictMoveRows - 1) / kEvictMoveRows) > kMaxBlocks)
+    return fail(DOMINO_ERR_UNSUPPORTED, "budget must be at most 2^21, n_layers * batch * n_kv_heads at most 2^20 and 2^30 / min(budget, max_len)");
+  return DOMINO_OK;
+}
+}  // namespace
+
+domino_status domino_rope_frequencies(int32_t rotary_dim, double theta, domino_rope_scaling scaling, double factor,
+                                      int32_t original_ctx, double beta_fast, double beta_slow, double *frequencies,
+                                      float *rope_scale) {
+  if (!frequencies || !rope_scale) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (rotary_dim < 2 || rotary_dim > 128 || rotary_dim % 2) return fail(DOMINO_ERR_INVALID_ARG, "rotary_dim must be even, in [2, 128]");
+  if (!(theta > 1.0) || !std::isfinite(theta)) return fail(DOMINO_ERR_INVALID_ARG, "theta must be above 1 and finite");
+  if (scaling < DOMINO_ROPE_NONE || scaling > DOMINO_ROPE_YARN) return fail(DOMINO_ERR_INVALID_ARG, "unknown scaling");
+  if (scaling != DOMINO_ROPE_NONE && (!(factor >= 1.0) || !std::isfinite(factor)))
+    return fail(DOMINO_ERR_INVALID_ARG, "factor must be at least 1 and finite");
+  if (scaling == DOMINO_ROPE_NTK && rotary_dim < 4) return fail(DOMINO_ERR_INVALID_ARG, "DOMINO_ROPE_NTK needs a rotary_dim of at least 4");
+  if (scaling == DOMINO_ROPE_YARN && (original_ctx < 1 || !(beta_slow > 0.0) || !(beta_fast > beta_slow) || !std::isfinite(beta_fast)))
+    return fail(DOMINO_ERR_INVALID_ARG, "DOMINO_ROPE_YARN needs original_ctx >= 1 and finite beta_fast > beta_slow > 0");
+  const double d = rotary_dim;
+  if (scaling == DOMINO_ROPE_NTK) theta *= std::pow(factor, d / (d - 2.0));
+  *rope_scale = scaling == DOMINO_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    double f = std::pow(theta, -2.0 * i / d);
+    if (scaling == DOMINO_ROPE_LINEAR) f /= factor;
+    if (scaling == DOMINO_ROPE_YARN) {
+      const double turns = original_ctx * f / 6.283185307179586;
+      const double keep = std::min(1.0, std::max(0.0, (turns - beta_slow) / (beta_fast - beta_slow)));
+      f = f * keep + f / factor * (1.0 - keep);
+    }
+    frequencies[i] = f;
+  }
+  return DOMINO_OK;
+}
+
+domino_status domino_paged_append(const domino_paged_cache *cache, int32_t layer, int32_t tokens, int32_t n_q_heads,
+                                  const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                                  int64_t v_stride, void *q_out, int64_t q_out_stride, const int32_t *seq_starts,
+                                  const int32_t *kv_lens, const int32_t *positions, const double *frequencies,
+                                  int32_t rotary_dim, int32_t interleaved, float rope_scale, const void *q_norm,
+                                  const void *k_norm, float rms_eps, void *workspace, size_t workspace_bytes, void *stream) {
+  if (domino_status s = check_paged(cache); s != DOMINO_OK) return s;
+  if (domino_status s = check_tokens(cache, layer, tokens, n_q_heads); s != DOMINO_OK) return s;
+  if (domino_status s = check_heads(cache, "q", q, q_stride, n_q_heads, tokens); s != DOMINO_OK) return s;
+  if (domino_status s = check_heads(cache, "k", k, k_stride, cache->n_kv_heads, tokens); s != DOMINO_OK) return s;
+  if (domino_status s = check_heads(cache, "v", v, v_stride, cache->n_kv_heads, tokens); s != DOMINO_OK) return s;
+  if (domino_status s = check_heads(cache, "q_out", q_out, q_out_stride, n_q_heads, tokens); s != DOMINO_OK) return s;
+  if (q_out == q && tokens > 1 && q_out_stride != q_stride)
+    return fail(DOMINO_ERR_INVALID_ARG, "q_out in q's place must have q's stride");
+  if (!seq_starts || !kv_lens) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (rotary_dim < 0 || rotary_dim > cache->head_dim) return fail(DOMINO_ERR_INVALID_ARG, "rotary_dim must be in [0, head_dim]");
+  if (rotary_dim % 16) return fail(DOMINO_ERR_UNSUPPORTED, "rotary_dim must be a multiple of 16");
+  if (rotary_dim && (!frequencies || (uintptr_t)frequencies % 8)) return fail(DOMINO_ERR_INVALID_ARG, "frequencies is NULL or not aligned to 8 bytes");
+  if (rotary_dim && !std::isfinite(rope_scale)) return fail(DOMINO_ERR_INVALID_ARG, "rope_scale must be finite");
+  if ((uintptr_t)q_norm % 16 || (uintptr_t)k_norm % 16) return fail(DOMINO_ERR_INVALID_ARG, "q_norm and k_norm must be aligned to 16 bytes");
+  if ((q_norm || k_norm) && (!(rms_eps >= 0.f) || !std::isfinite(rms_eps))) return fail(DOMINO_ERR_INVALID_ARG, "rms_eps must be >= 0 and finite");
+  if (domino_status s = check_paged_workspace(workspace, workspace_bytes, DOMINO_PAGED_WORKSPACE_BYTES); s != DOMINO_OK) return s;
+  PagedAppendArgs a;
+  a.c = paged_view(cache);
+  a.layer = layer;
+  a.tokens = tokens;
+  a.nq = n_q_heads;
+  a.q = q;
+  a.kn = k;
+  a.vn = v;
+  a.q_out = q_out;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.o_stride = q_out_stride;
+  a.starts = seq_starts;
+  a.lens = kv_lens;
+  a.positions = positions;
+  a.freq = frequencies;
+  a.rot = rotary_dim;
+  a.interleaved = interleaved != 0;
+  a.rope_scale = rope_scale;
+  a.eps = rms_eps;
+  a.q_norm = q_norm;
+  a.k_norm = k_norm;
+  a.err = (int32_t *)workspace;
+  launch_paged_append(a, (hipStream_t)stream);
+  hipError_t he = hipGetLastError();
+  if (he != hipSuccess) return fail(DOMINO_ERR_HIP, "paged_append launch: %s", hipGetErrorString(he));
+  return DOMINO_OK;
+}
+
+size_t domino_paged_attention_workspace_bytes(const domino_paged_cache *cache, int32_t tokens, int32_t n_q_heads,
+                                              int32_t max_new, int32_t max_len, int32_t accumulate) {
+  PagedAttnLayout w;
+  return paged_attn_layout(cache, tokens, n_q_heads, max_new, max_len, accumulate, w) == DOMINO_OK ? w.bytes : 0;
+}
+
+domino_status domino_paged_attention(const domino_paged_cache *cache, int32_t layer, int32_t tokens, int32_t n_q_heads,
+                                     int32_t max_new, int32_t max_len, const void *q, int64_t q_stride, void *out,
+                                     int64_t out_stride, const int32_t *seq_starts, const int32_t *kv_lens, float scale,
+                                     const uint8_t *mask, int64_t mask_ld, float *lse, int32_t accumulate, void *workspace,
+                                     size_t workspace_bytes, void *stream) {
+  PagedAttnLayout w;
+  if (domino_status s = paged_attn_layout(cache, tokens, n_q_heads, max_new, max_len, accumulate, w); s != DOMINO_OK) return s;
+  if (domino_status s = check_tokens(cache, layer, tokens, n_q_heads); s != DOMINO_OK) return s;
+  if (domino_status s = check_heads(cache, "q", q, q_stride, n_q_heads, tokens); s != DOMINO_OK) return s;
+  if (domino_status s = check_heads(cache, "out", out, out_stride, n_q_heads, tokens); s != DOMINO_OK) return s;
+  if (out == q) return fail(DOMINO_ERR_INVALID_ARG, "out must not be q");
+  if (!seq_starts || !kv_lens) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(DOMINO_ERR_INVALID_ARG, "scale must be positive and finite");
+  if (mask && mask_ld < max_new) return fail(DOMINO_ERR_INVALID_ARG, "mask_ld must be at least max_new");
+  if (domino_status s = check_paged_workspace(workspace, workspace_bytes, w.bytes); s != DOMINO_OK) return s;
+  char *ws = (char *)workspace;
+  PagedAttnArgs a;
+  a.c = paged_view(cache);
+  a.layer = layer;
+  a.tokens = tokens;
+  a.nq = n_q_heads;
+  a.max_new = std::min(max_new, tokens);
+  a.max_len = max_len;
+  a.q = q;
+  a.out = out;
+  a.q_stride = q_stride;
+  a.o_stride = out_stride;
+  a.starts = seq_starts;
+  a.lens = kv_lens;
+  a.mask = mask;
+  a.mask_ld = mask_ld;
+  a.scale = scale;
+  a.lse = lse ? lse : (accumulate ? (float *)(ws + w.lse) : nullptr);
+  a.part_ml = w.plan.splits > 1 ? (float *)(ws + w.ml) : nullptr;
+  a.part_o = w.plan.splits > 1 ? (float *)(ws + w.o) : nullptr;
+  a.accumulate = accumulate != 0;
+  a.err = (int32_t *)workspace;
+  launch_paged_attn(a, w.plan, (hipStream_t)stream);
+  hipError_t he = hipGetLastError();
+  if (he != hipSuccess) return fail(DOMINO_ERR_HIP, "paged_attention launch: %s", hipGetErrorString(he));
+  return DOMINO_OK;
+}
+
+size_t domino_paged_evict_workspace_bytes(const domino_paged_cache *cache, int32_t max_len, int32_t budget) {
+  if (check_evict(cache, max_len, budget) != DOMINO_OK) return 0;
+  return 256 + (size_t)cache->n_layers * cache->batch * cache->n_kv_heads * budget * 4;
+}
+
+domino_status domino_paged_evict(const domino_paged_cache *cache, const int32_t *kv_lens, int32_t *new_lens, int32_t max_len,
+                                 int32_t budget, int32_t sink, int32_t recent, const int32_t *new_table, int32_t new_pages,
+                                 int32_t *kept, void *workspace, size_t workspace_bytes, void *stream) {
+  if (domino_status s = check_evict(cache, max_len, budget); s != DOMINO_OK) return s;
+  if (!kv_lens || !new_lens) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (kv_lens == new_lens) return fail(DOMINO_ERR_INVALID_ARG, "new_lens must not be kv_lens");
+  if (sink < 0 || recent < 0 || (int64_t)sink + recent > budget) return fail(DOMINO_ERR_INVALID_ARG, "sink and recent must be >= 0 and at most budget together");
+  if (new_table && (int64_t)new_pages * cache->page_size < budget)
+    return fail(DOMINO_ERR_INVALID_ARG, "new_pages * page_size must be at least budget");
+  if (domino_status s = check_paged_workspace(workspace, workspace_bytes, domino_paged_evict_workspace_bytes(cache, max_len, budget)); s != DOMINO_OK) return s;
+  PagedEvictArgs a;
+  a.c = paged_view(cache);
+  a.lens = kv_lens;
+  a.new_lens = new_lens;
+  a.max_len = max_len;
+  a.budget = budget;
+  a.sink = sink;
+  a.recent = recent;
+  a.new_table = new_table;
+  a.new_pages = new_pages;
+  a.kept = kept ? kept : (int32_t *)((char *)workspace + 256);
+  a.err = (int32_t *)workspace;
+  launch_paged_evict(a, (hipStream_t)stream);
+  hipError_t he = hipGetLastError();
+  if (he != hipSuccess) return fail(DOMINO_ERR_HIP, "paged_evict launch: %s", hipGetErrorString(he));
+  return DOMINO_OK;
+}
+
+domino_status domino_paged_commit(const domino_paged_cache *cache, int32_t n_nodes, int32_t max_depth,
+                                  const int32_t *ctx_lens, const int32_t *accept_len, const int32_t *accepted_nodes,
+                                  int32_t *new_ctx_lens, void *workspace, size_t workspace_bytes, void *stream) {
+  if (domino_status s = check_paged(cache); s != DOMINO_OK) return s;
+  if (n_nodes < 1 || n_nodes > 1024) return fail(DOMINO_ERR_INVALID_ARG, "n_nodes must be in [1, 1024]");
+  if (max_depth < 1 || max_depth > 63) return fail(DOMINO_ERR_INVALID_ARG, "max_depth must be in [1, 63]");
+  if (!ctx_lens || !accept_len || !accepted_nodes || !new_ctx_lens) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (ctx_lens == new_ctx_lens) return fail(DOMINO_ERR_INVALID_ARG, "new_ctx_lens must not alias ctx_lens");
+  if ((int64_t)cache->n_layers * cache->batch * cache->n_kv_heads > kMaxBlocks)
+    return fail(DOMINO_ERR_UNSUPPORTED, "n_layers * batch * n_kv_heads must be at most %ld", kMaxBlocks);
+  if (domino_status s = check_paged_workspace(workspace, workspace_bytes, DOMINO_PAGED_WORKSPACE_BYTES); s != DOMINO_OK) return s;
+  launch_paged_commit(paged_view(cache), n_nodes, max_depth, ctx_lens, accept_len, accepted_nodes, new_ctx_lens,
+                      (int32_t *)workspace, (hipStream_t)stream);
+  hipError_t he = hipGetLastError();
+  if (he != hipSuccess) return fail(DOMINO_ERR_HIP, "paged_commit launch: %s", hipGetErrorString(he));
+  return DOMINO_OK;
+}
+
 domino_status domino_philox4x32_10(const uint32_t *counters, uint64_t key, uint32_t *out, int32_t n, void *stream) {
   if (n < 0) return fail(DOMINO_ERR_INVALID_ARG, "n must be >= 0");
   if (n > 0 && (!counters || !out)) return fail(DOMINO_ERR_INVALID_ARG, "counters/out is NULL");

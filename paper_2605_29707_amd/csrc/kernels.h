@@ -337,4 +337,71 @@ void launch_sum_parts(const float *parts, int np, size_t pstride, int rows, int 
 void launch_sum_parts_planes(const float *parts, int np, size_t pstride, int rows, int width, void *planes, int row0,
                              int nrb, hipStream_t st);
 
+// ---- paged cache (paged.hip, paged_attn.hip)
+// Strides in elements; k and v share them.  weights: [layers][n_pages][n_kv][page] fp32 or null.
+struct PagedView {
+  char *k, *v;
+  float *weights;
+  const int32_t *table;  // [batch][max_pages]
+  int64_t layer_stride, page_stride, slot_stride, head_stride;
+  int n_layers, n_pages, page_shift, n_kv, dh, batch, max_pages;
+  int bf16;
+};
+
+struct PagedAppendArgs {
+  PagedView c;
+  int layer, tokens, nq;
+  const void *q, *kn, *vn;
+  void *q_out;
+  int64_t q_stride, k_stride, v_stride, o_stride;  // elements between tokens; heads are dense
+  const int32_t *starts, *lens, *positions;
+  const double *freq;  // [rot / 2] radians a position
+  int rot, interleaved;
+  float rope_scale, eps;
+  const void *q_norm, *k_norm;
+  int32_t *err;
+};
+void launch_paged_append(const PagedAppendArgs &a, hipStream_t st);
+
+void launch_paged_commit(const PagedView &c, int n_nodes, int max_depth, const int32_t *ctx_lens, const int32_t *accept_len,
+                         const int32_t *accepted, int32_t *new_lens, int32_t *err, hipStream_t st);
+
+struct PagedEvictArgs {
+  PagedView c;
+  const int32_t *lens;
+  int32_t *new_lens;
+  int max_len, budget, sink, recent;
+  const int32_t *new_table;  // null: in place
+  int new_pages;             // entries a row of new_table
+  int32_t *kept;             // [layers][batch][n_kv][budget]
+  int32_t *err;
+};
+constexpr int kEvictMoveRows = 64;  // rows of a head that a workgroup moves to new pages
+void launch_paged_evict(const PagedEvictArgs &a, hipStream_t st);
+
+struct PagedAttnArgs {
+  PagedView c;
+  int layer, tokens, nq, max_new, max_len;
+  const void *q;
+  void *out;
+  int64_t q_stride, o_stride;
+  const int32_t *starts, *lens;
+  const uint8_t *mask;
+  int64_t mask_ld;
+  float scale;
+  float *lse;        // [tokens][nq] or null (needed with accumulate)
+  float *part_o;     // [splits][tokens][nq][dh], null: one split
+  float *part_ml;    // [splits][tokens][nq][2]: maximum (base 2) and sum
+  int accumulate;
+  int32_t *err;
+};
+// What a call launches, from sizes that the host knows.
+struct PagedAttnPlan {
+  int rows;        // query rows (new tokens x query heads of a kv head) of a workgroup's tile
+  long tiles;      // tiles that hold rows, at most
+  int splits, run; // a sequence's slots are cut into runs of `run`
+};
+PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv, int max_new, int max_len);
+void launch_paged_attn(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t st);
+
 }  // namespace dk

@@ -1,0 +1,502 @@
+// A cache of pages: the append of new tokens with their rotary positions, the commit of an
+// accepted path, and eviction by accumulated attention weight.
+#include "paged.h"
+
+namespace dk {
+
+// ---------------------------------------------------------------------------
+// append
+// ---------------------------------------------------------------------------
+// Eight elements of a head a lane: 16 (d_h 128) or 8 lanes a head.  A lane reads its own eight and, with rotated
+// halves, the eight that they are paired with, so nothing passes between lanes but a head's sum of squares.
+// Per pair (x, y) at angle a = position * frequency: (x cos a - y sin a, y cos a + x sin a).  The angle is a number of
+// turns in fp64, taken modulo one before it is rounded: positions in the millions keep fp32's accuracy.
+constexpr int kAppendThreads = 256;
+
+template <typename T>
+DEVI void load8(const T *p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    const u32x4 w = *(const u32x4 *)p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  } else {
+    const floatx4 a = *(const floatx4 *)p, b = *(const floatx4 *)(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = a[e];
+      x[4 + e] = b[e];
+    }
+  }
+}
+template <typename T>
+DEVI void store8(T *p, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)f32_to_bf16(x[2 * e]).v | ((uint32_t)f32_to_bf16(x[2 * e + 1]).v << 16);
+    *(u32x4 *)p = w;
+  } else {
+    *(floatx4 *)p = floatx4{x[0], x[1], x[2], x[3]};
+    *(floatx4 *)(p + 4) = floatx4{x[4], x[5], x[6], x[7]};
+  }
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedAppendArgs a) {
+  constexpr int LPH = DH / 8, GROUPS = kAppendThreads / LPH;
+  const int t = blockIdx.x, lane = threadIdx.x & 63, j = threadIdx.x % LPH, grp = threadIdx.x / LPH;
+  // the sequence of token t: how many sequences end at or before it
+  int b = 0;
+  for (int s0 = 0; s0 < a.c.batch; s0 += 64) {
+    const bool done = s0 + lane < a.c.batch && a.starts[s0 + lane + 1] <= t;
+    b += __popcll(__ballot(done));
+  }
+  if (b >= a.c.batch) return;  // rows behind the last sequence
+  SeqRange s;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.tokens, a.c.max_pages << a.c.page_shift, a.err, s)) return;
+  if (t < s.start || t >= s.start + s.n) {  // starts out of order
+    raise_error(a.err, DEV_BAD_CTX_LEN);
+    return;
+  }
+  const int slot = s.len - s.n + (t - s.start);
+  const int page = page_of(a.c, b, slot);
+  if (page < 0) raise_error(a.err, DEV_BAD_PAGE);
+  const int64_t off = slot_offset(a.c, max(page, 0), slot);
+
+  // factors of this lane's elements: out = own * cs + partner * sn
+  float cs[8], sn[8];
+  const int half = a.rot / 2, e0 = 8 * j;
+  const bool turned = e0 < a.rot;
+  int partner = e0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    cs[e] = 1.f;
+    sn[e] = 0.f;
+  }
+  if (turned) {
+    const double pos = a.positions ? a.positions[t] : slot;
+    const bool second = !a.interleaved && e0 >= half;
+    const int f0 = a.interleaved ? e0 / 2 : (second ? e0 - half : e0);
+    if (!a.interleaved) partner = second ? e0 - half : e0 + half;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (a.interleaved && (e & 1)) continue;
+      const double turns = pos * a.freq[f0 + (a.interleaved ? e / 2 : e)] * 0.15915494309189535;  // 1 / (2 pi)
+      float c, d;
+      sincospif(2.f * (float)(turns - rint(turns)), &d, &c);
+      c *= a.rope_scale;
+      d *= a.rope_scale;
+      if (a.interleaved) {
+        cs[e] = cs[e + 1] = c;
+        sn[e] = -d;
+        sn[e + 1] = d;
+      } else {
+        cs[e] = c;
+        sn[e] = second ? d : -d;
+      }
+    }
+  }
+
+  const int heads = a.nq + 2 * a.c.n_kv;
+  for (int h = blockIdx.y * GROUPS + grp; h < heads; h += gridDim.y * GROUPS) {
+    const bool is_q = h < a.nq, is_v = h >= a.nq + a.c.n_kv;
+    const int hk = is_q ? h : (is_v ? h - a.nq - a.c.n_kv : h - a.nq);
+    const T *src = is_q ? (const T *)a.q + (int64_t)t * a.q_stride + (int64_t)hk * DH
+                        : (is_v ? (const T *)a.vn + (int64_t)t * a.v_stride + (int64_t)hk * DH
+                                : (const T *)a.kn + (int64_t)t * a.k_stride + (int64_t)hk * DH);
+    T *dst = is_q ? (T *)a.q_out + (int64_t)t * a.o_stride + (int64_t)hk * DH
+                  : (T *)(is_v ? a.c.v : a.c.k) + a.layer * a.c.layer_stride + off + hk * a.c.head_stride;
+    float x[8], y[8];
+    load8(src + e0, x);
+    if (!is_v) {
+      const T *gain = (const T *)(is_q ? a.q_norm : a.k_norm);
+      float g[8], gp[8], r = 1.f;
+      const bool pair = turned && !a.interleaved;
+      if (pair) load8(src + partner, y);
+      if (gain) {
+        load8(gain + e0, g);
+        if (pair) load8(gain + partner, gp);
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
+#pragma unroll
+        for (int o = LPH / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 64);
+        r = 1.f / sqrtf(ss * (1.f / DH) + a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
+        if (pair) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = y[e] * r * gp[e];
+        }
+      }
+      if (turned) {
+        if (a.interleaved) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * cs[e] + y[e] * sn[e];
+      }
+    }
+    if (is_q || page >= 0) store8(dst + e0, x);
+    if (!is_q && !is_v && page >= 0 && a.c.weights && j == 0) a.c.weights[weight_offset(a.c, a.layer, page, hk, slot)] = 0.f;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// commit: rows n + node(d) move to n + d.  A workgroup has one head of one layer and sequence:
+// every source is in registers before the first row is written.
+// ---------------------------------------------------------------------------
+constexpr int kMoveThreads = 256;
+
+__global__ __launch_bounds__(kMoveThreads) void paged_commit_kernel(PagedView c, int nn, int max_depth,
+                                                                    const int32_t *__restrict__ ctx_lens,
+                                                                    const int32_t *__restrict__ accept_len,
+                                                                    const int32_t *__restrict__ accepted,
+                                                                    int32_t *__restrict__ new_lens, int32_t *err) {
+  const int head = blockIdx.x % c.n_kv, b = (blockIdx.x / c.n_kv) % c.batch, layer = blockIdx.x / c.n_kv / c.batch;
+  const int tid = threadIdx.x, n = ctx_lens[b], a = accept_len[b];
+  const bool lead = layer == 0 && head == 0 && tid == 0;
+  __shared__ int64_t from[64], to[64], w_from[64], w_to[64];
+  __shared__ int bad;
+  if (tid == 0) bad = 0;
+  __syncthreads();
+  if (n < 0 || a < 0 || a > max_depth || n > (c.max_pages << c.page_shift) - nn) {
+    if (lead) {
+      raise_error(err, DEV_BAD_CTX_LEN);
+      new_lens[b] = n;
+    }
+    return;
+  }
+  if (tid < a) {  // a <= 63
+    const int d = tid + 1, x = accepted[(size_t)b * max_depth + tid];
+    from[tid] = -1;  // stays
+    if (x < d || x >= nn) {
+      atomicOr(&bad, DEV_BAD_TREE);
+    } else if (x != d) {
+      const int pf = page_of(c, b, n + x), pt = page_of(c, b, n + d);
+      if (pf < 0 || pt < 0) atomicOr(&bad, DEV_BAD_PAGE);
+      from[tid] = slot_offset(c, max(pf, 0), n + x);
+      to[tid] = slot_offset(c, max(pt, 0), n + d);
+      w_from[tid] = weight_offset(c, layer, max(pf, 0), head, n + x);
+      w_to[tid] = weight_offset(c, layer, max(pt, 0), head, n + d);
+    }
+  }
+  __syncthreads();
+  if (bad) {
+    if (lead) {
+      raise_error(err, bad);
+      new_lens[b] = n;
+    }
+    return;
+  }
+  if (lead) new_lens[b] = n + 1 + a;
+  if (a == 0) return;
+  const int esz = c.bf16 ? 2 : 4, row16 = c.dh * esz / 16, items = 2 * a * row16;
+  constexpr int PER = 63 * 2 * 32 / kMoveThreads + 1;  // 63 rows of 128 fp32 values, k and v
+  const int64_t base = (layer * c.layer_stride + head * c.head_stride) * esz;
+  u32x4 v[PER];
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const int it = tid + q * kMoveThreads;
+    v[q] = u32x4{0, 0, 0, 0};
+    if (it < items) {
+      const int isv = it / (a * row16), rem = it % (a * row16), d = rem / row16;
+      if (from[d] >= 0) v[q] = *(const u32x4 *)((isv ? c.v : c.k) + base + from[d] * esz + (rem % row16) * 16);
+    }
+  }
+  float w = 0.f;
+  if (c.weights && tid < a && from[tid] >= 0) w = c.weights[w_from[tid]];
+#pragma unroll
+  for (int q = 0; q < PER; ++q) __asm__ volatile("" ::"v"(v[q]));  // every load has arrived before the barrier
+  __asm__ volatile("" ::"v"(w));
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const int it = tid + q * kMoveThreads;
+    if (it < items) {
+      const int isv = it / (a * row16), rem = it % (a * row16), d = rem / row16;
+      if (from[d] >= 0) *(u32x4 *)((isv ? c.v : c.k) + base + to[d] * esz + (rem % row16) * 16) = v[q];
+    }
+  }
+  if (c.weights && tid < a && from[tid] >= 0) c.weights[w_to[tid]] = w;
+}
+
+// ---------------------------------------------------------------------------
+// eviction
+// ---------------------------------------------------------------------------
+// Unsigned order of a weight: NaN and anything below zero as it compares, NaN lowest.
+DEVI uint32_t weight_key(float w) {
+  if (w != w) return 0;
+  const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+
+// Which slots of one (layer, sequence, head) stay, in order: the first `sink`, the last `recent`, and the m of greatest
+// weight between them.  The m-th greatest key is found by three counts over its digits (11, 11 and 10 bits); then every wave
+// counts the kept slots of its own stretch and writes them.
+__global__ __launch_bounds__(kSelThreads) void paged_evict_select_kernel(PagedEvictArgs a) {
+  const PagedView &c = a.c;
+  const int head = blockIdx.x % c.n_kv, b = (blockIdx.x / c.n_kv) % c.batch, layer = blockIdx.x / c.n_kv / c.batch;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool lead = layer == 0 && head == 0 && tid == 0;
+  int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
+  int n = a.lens[b];
+  if (n < 0 || n > a.max_len) {
+    if (lead) raise_error(a.err, DEV_BAD_CTX_LEN);
+    if (lead) a.new_lens[b] = n;
+    for (int i = tid; i < a.budget; i += kSelThreads) kept[i] = -1;
+    return;
+  }
+  if (n <= a.budget) {
+    if (lead) a.new_lens[b] = n;
+    for (int i = tid; i < a.budget; i += kSelThreads) kept[i] = i < n ? i : -1;
+    return;
+  }
+  if (lead) a.new_lens[b] = a.budget;
+  const int first = a.sink, last = n - a.recent, m = a.budget - a.sink - a.recent;
+  __shared__ uint32_t hist[2048];
+  __shared__ uint32_t wsum[kSelWaves], wtie[kSelWaves];
+  __shared__ uint32_t s_bin, s_above;
+  bool lost = false;
+  auto key_at = [&](int slot) -> uint32_t {
+    const int page = page_of(c, b, slot);
+    if (page < 0) {
+      lost = true;
+      return 0;
+    }
+    return weight_key(c.weights[weight_offset(c, layer, page, head, slot)]);
+  };
+  uint32_t prefix = 0, need = m;  // the wanted key's digits so far, its rank among those that share them
+  for (int pass = 0; pass < 3 && m > 0; ++pass) {
+    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
+    for (int i = tid; i < 2048; i += kSelThreads) hist[i] = 0;
+    __syncthreads();
+    for (int s0 = first + wave * 64; s0 < last; s0 += kSelThreads) {  // wave-uniform
+      const int slot = s0 + lane;
+      const uint32_t key = slot < last ? key_at(slot) : 0;
+      const bool in = slot < last && (pass == 0 || (key >> (shift + bits)) == prefix);
+      const uint32_t bin = (key >> shift) & ((1u << bits) - 1);
+      // the first lane's bin is counted once for all that share it: most slots may hold one value
+      const uint64_t live = __ballot(in);
+      if (live) {
+        const uint32_t b0 = __shfl(bin, __ffsll((unsigned long long)live) - 1, 64);
+        const uint64_t same = __ballot(in && bin == b0);
+        if (in && bin != b0) atomicAdd(&hist[bin], 1u);
+        if (lane == 0) atomicAdd(&hist[b0], (uint32_t)__popcll(same));
+      }
+    }
+    __syncthreads();
+    // from the top bin down: the bin where the running count reaches `need`
+    if (wave == 0) {
+      uint32_t mine = 0;
+      for (int i = 0; i < 32; ++i) mine += hist[2047 - (lane * 32 + i)];
+      uint32_t incl = mine;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t v = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += v;
+      }
+      uint32_t run = incl - mine;
+      if (run < need && incl >= need) {
+        for (int i = 0; i < 32; ++i) {
+          const int bin = 2047 - (lane * 32 + i);
+          const uint32_t h = hist[bin];
+          if (run < need && run + h >= need) {
+            s_bin = bin;
+            s_above = run;
+          }
+          run += h;
+        }
+      }
+    }
+    __syncthreads();
+    prefix = (prefix << bits) | s_bin;
+    need -= s_above;
+    __syncthreads();
+  }
+  // kept: keys above `prefix`, and the first `need` slots that equal it
+  const int per = (((n + kSelWaves - 1) / kSelWaves) + 63) / 64 * 64;
+  const int w0 = min(n, wave * per), w1 = min(n, w0 + per);
+  auto flags = [&](int slot, bool &sure, bool &tie) {
+    sure = slot < n && (slot < first || slot >= last);
+    tie = false;
+    if (slot >= first && slot < last && m > 0) {
+      const uint32_t key = key_at(slot);
+      sure = key > prefix;
+      tie = key == prefix;
+    }
+  };
+  uint32_t ns = 0, nt = 0;
+  for (int s0 = w0; s0 < w1; s0 += 64) {
+    bool sure, tie;
+    flags(s0 + lane < w1 ? s0 + lane : n, sure, tie);
+    ns += __popcll(__ballot(sure));
+    nt += __popcll(__ballot(tie));
+  }
+  if (lane == 0) {
+    wsum[wave] = ns;
+    wtie[wave] = nt;
+  }
+  __syncthreads();
+  ns = nt = 0;
+  for (int w = 0; w < wave; ++w) {
+    ns += wsum[w];
+    nt += wtie[w];
+  }
+  const uint64_t below = (1ull << lane) - 1;
+  for (int s0 = w0; s0 < w1; s0 += 64) {
+    bool sure, tie;
+    flags(s0 + lane < w1 ? s0 + lane : n, sure, tie);
+    const uint64_t bs = __ballot(sure), bt = __ballot(tie);
+    const uint32_t ties = nt + __popcll(bt & below);
+    if (sure || (tie && ties < need)) {
+      const uint32_t at = ns + __popcll(bs & below) + min(ties, need);
+      if (at < (uint32_t)a.budget) kept[at] = s0 + lane;
+    }
+    ns += __popcll(bs);
+    nt += __popcll(bt);
+  }
+  if (lost) raise_error(a.err, DEV_BAD_PAGE);
+}
+
+// Rows kept[i] move to slot i.  In place, a workgroup has one column slice of one head's keys or values (or the head's
+// weights) and goes up the slots in rounds: kept[i] >= i, so a round writes no slot that a later one reads, and reads all of its own
+// before it writes.  To new pages there is no such order: a workgroup has a stretch of rows.
+constexpr int kSlice16 = 4;  // 16-byte items of a row's slice
+
+template <bool WEIGHTS>
+DEVI void evict_in_place(const PagedEvictArgs &a, int b, int layer, int head, const int32_t *kept, int count, char *data,
+                         int64_t base, int esz, int slice) {
+  constexpr int PER = 8, ITEMS = WEIGHTS ? 1 : kSlice16, ROWS = kMoveThreads * PER / ITEMS;
+  const PagedView &c = a.c;
+  const int tid = threadIdx.x;
+  bool lost = false;
+  for (int r0 = 0; r0 < count; r0 += ROWS) {
+    u32x4 v[PER];
+    float w[PER];
+    int64_t to[PER];
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      const int it = tid + q * kMoveThreads, i = r0 + it / ITEMS;
+      to[q] = -1;
+      v[q] = u32x4{0, 0, 0, 0};
+      w[q] = 0.f;
+      if (i >= count) continue;
+      const int s = kept[i];
+      if (s <= i) continue;  // it stays
+      const int pf = page_of(c, b, s), pt = page_of(c, b, i);
+      if (pf < 0 || pt < 0) {
+        lost = true;
+        continue;
+      }
+      if (WEIGHTS) {
+        w[q] = c.weights[weight_offset(c, layer, pf, head, s)];
+        to[q] = weight_offset(c, layer, pt, head, i);
+      } else {
+        const int64_t col = (slice * kSlice16 + it % ITEMS) * 16;
+        v[q] = *(const u32x4 *)(data + base + slot_offset(c, pf, s) * esz + col);
+        to[q] = base + slot_offset(c, pt, i) * esz + col;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < PER; ++q) __asm__ volatile("" ::"v"(v[q]), "v"(w[q]));  // every load has arrived
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      if (to[q] < 0) continue;
+      if (WEIGHTS) c.weights[to[q]] = w[q];
+      else *(u32x4 *)(data + to[q]) = v[q];
+    }
+    __syncthreads();
+  }
+  if (lost) raise_error(a.err, DEV_BAD_PAGE);
+}
+
+__global__ __launch_bounds__(kMoveThreads) void paged_evict_in_place_kernel(PagedEvictArgs a) {
+  const PagedView &c = a.c;
+  const int head = blockIdx.x % c.n_kv, b = (blockIdx.x / c.n_kv) % c.batch, layer = blockIdx.x / c.n_kv / c.batch;
+  const int n = a.lens[b];
+  if (n <= a.budget || n > a.max_len) return;
+  const int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
+  const int esz = c.bf16 ? 2 : 4, slices = c.dh * esz / 16 / kSlice16;
+  const int part = blockIdx.y;  // slices of k, slices of v, weights
+  const int64_t base = (layer * c.layer_stride + head * c.head_stride) * esz;
+  if (part < 2 * slices)
+    evict_in_place<false>(a, b, layer, head, kept, a.budget, part < slices ? c.k : c.v, base, esz, part % slices);
+  else
+    evict_in_place<true>(a, b, layer, head, kept, a.budget, nullptr, 0, 0, 0);
+}
+
+__global__ __launch_bounds__(kMoveThreads) void paged_evict_gather_kernel(PagedEvictArgs a) {
+  const PagedView &c = a.c;
+  const int head = blockIdx.x % c.n_kv, b = (blockIdx.x / c.n_kv) % c.batch, layer = blockIdx.x / c.n_kv / c.batch;
+  const int n = a.lens[b], tid = threadIdx.x;
+  if (n < 0 || n > a.max_len) return;
+  const int count = min(n, a.budget), r0 = blockIdx.y * kEvictMoveRows;
+  if (r0 >= count) return;
+  const int rows = min(kEvictMoveRows, count - r0);
+  const int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
+  __shared__ int64_t from[kEvictMoveRows], to[kEvictMoveRows];
+  if (tid < rows) {
+    const int s = kept[r0 + tid], i = r0 + tid;
+    const int pf = page_of(c, b, s), pt = a.new_table[(int64_t)b * a.new_pages + (i >> c.page_shift)];
+    from[tid] = -1;
+    if (pf >= 0 && (unsigned)pt < (unsigned)c.n_pages) {
+      from[tid] = slot_offset(c, pf, s);
+      to[tid] = slot_offset(c, pt, i);
+      c.weights[weight_offset(c, layer, pt, head, i)] = c.weights[weight_offset(c, layer, pf, head, s)];
+    } else {
+      raise_error(a.err, DEV_BAD_PAGE);
+    }
+  }
+  __syncthreads();
+  const int esz = c.bf16 ? 2 : 4, row16 = c.dh * esz / 16;
+  const int64_t base = (layer * c.layer_stride + head * c.head_stride) * esz;
+  for (int it = tid; it < 2 * rows * row16; it += kMoveThreads) {
+    const int isv = it / (rows * row16), rem = it % (rows * row16), d = rem / row16;
+    if (from[d] < 0) continue;
+    char *p = (isv ? c.v : c.k) + base + (rem % row16) * 16;
+    *(u32x4 *)(p + to[d] * esz) = *(const u32x4 *)(p + from[d] * esz);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// launchers
+// ---------------------------------------------------------------------------
+template <typename T, int DH>
+static void append_of(const PagedAppendArgs &a, hipStream_t st) {
+  constexpr int GROUPS = kAppendThreads / (DH / 8);
+  const int heads = a.nq + 2 * a.c.n_kv;
+  const int ys = a.tokens < 1024 ? (heads + GROUPS - 1) / GROUPS : 1;
+  hipLaunchKernelGGL((paged_append_kernel<T, DH>), dim3(a.tokens, ys), dim3(kAppendThreads), 0, st, a);
+}
+void launch_paged_append(const PagedAppendArgs &a, hipStream_t st) {
+  if (a.c.bf16) a.c.dh == 128 ? append_of<bf16_t, 128>(a, st) : append_of<bf16_t, 64>(a, st);
+  else a.c.dh == 128 ? append_of<float, 128>(a, st) : append_of<float, 64>(a, st);
+}
+
+void launch_paged_commit(const PagedView &c, int n_nodes, int max_depth, const int32_t *ctx_lens, const int32_t *accept_len,
+                         const int32_t *accepted, int32_t *new_lens, int32_t *err, hipStream_t st) {
+  hipLaunchKernelGGL(paged_commit_kernel, dim3(c.n_layers * c.batch * c.n_kv), dim3(kMoveThreads), 0, st, c, n_nodes, max_depth,
+                     ctx_lens, accept_len, accepted, new_lens, err);
+}
+
+void launch_paged_evict(const PagedEvictArgs &a, hipStream_t st) {
+  const int heads = a.c.n_layers * a.c.batch * a.c.n_kv;
+  hipLaunchKernelGGL(paged_evict_select_kernel, dim3(heads), dim3(kSelThreads), 0, st, a);
+  if (a.new_table) {
+    hipLaunchKernelGGL(paged_evict_gather_kernel, dim3(heads, (min(a.budget, a.max_len) + kEvictMoveRows - 1) / kEvictMoveRows),
+                       dim3(kMoveThreads), 0, st, a);
+  } else {
+    const int slices = a.c.dh * (a.c.bf16 ? 2 : 4) / 16 / kSlice16;
+    hipLaunchKernelGGL(paged_evict_in_place_kernel, dim3(heads, 2 * slices + 1), dim3(kMoveThreads), 0, st, a);
+  }
+}
+
+}  // namespace dk

@@ -1,0 +1,542 @@
+// Attention of new tokens over a cache of pages, and the weights that it gives to every slot.
+//   o_r = sum_s p_rs v_s,  p_rs = exp(scale q_r k_s - lse_r) over the slots s that row r sees
+// Rows are the new tokens of a sequence times the query heads of one kv head: row i G + h.
+#include "mfma.h"
+#include "paged.h"
+
+namespace dk {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+typedef __attribute__((ext_vector_type(4))) short short4v;
+
+DEVI float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// One 16-row tile's place: sequence, lengths, first row, what it sees.
+struct Tile {
+  int b, row0, rows, vis;  // rows: of the sequence; vis: no row of the tile sees a slot from here on
+  SeqRange s;
+};
+
+// Sequences whose lengths disagree set the error word: one wave of a launch looks at all of them.
+DEVI void report_lengths(const PagedAttnArgs &a) {
+  SeqRange s;
+  for (int b = threadIdx.x & 63; b < a.c.batch; b += 64) seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, a.err, s);
+}
+
+// The tile-th tile of M rows over all sequences; false behind the last.  A sequence's last tiles come
+// first: with causal rows they are the longest.
+DEVI bool find_tile(const PagedAttnArgs &a, long tile, int M, Tile &t) {
+  const int lane = threadIdx.x & 63, G = a.nq / a.c.n_kv;
+  long base = 0;
+  for (int s0 = 0; s0 < a.c.batch; s0 += 64) {
+    const int b = s0 + lane;
+    SeqRange s{0, 0, 0};
+    if (b < a.c.batch) seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s);
+    const long n = ((long)s.n * G + M - 1) / M;
+    long incl = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const long v = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += v;
+    }
+    const uint64_t here = __ballot(base + incl > tile);
+    if (here) {
+      const int l = __ffsll((unsigned long long)here) - 1;
+      t.b = s0 + l;
+      t.s.start = __builtin_amdgcn_readlane(s.start, l);
+      t.s.n = __builtin_amdgcn_readlane(s.n, l);
+      t.s.len = __builtin_amdgcn_readlane(s.len, l);
+      t.rows = t.s.n * G;
+      // (tile - first tile of the sequence) counts from its last one
+      t.row0 = ((t.rows + M - 1) / M - 1 - __builtin_amdgcn_readlane((int)(tile - (base + incl - n)), l)) * M;
+      const int last = (min(t.row0 + M, t.rows) - 1) / G;
+      t.vis = a.mask ? t.s.len : t.s.len - t.s.n + last + 1;
+      return true;
+    }
+    base += (long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)incl, 63) |
+                   ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(incl >> 32), 63) << 32));
+  }
+  return false;
+}
+
+// Operands of the two products.  Scores: S^T = K Q^T in tiles of 16 slots x 16 rows, lane (g, r) = 16 g + r with
+// the scores of row r and slots 4 g .. 4 g + 3.  That is the second operand of O^T = V^T P^T as it stands,
+// if the slots of a step are taken in the order (4 g .. 4 g + 3, 16 + 4 g .. 16 + 4 g + 3).
+template <typename T, int DH> struct Ops;
+
+template <int DH> struct Ops<bf16_t, DH> {
+  static constexpr int KST = DH / 32, OT = DH / 16;
+  // lds: this wave's 32 rows of v, 32 bytes of padding each, so that the 16 rows that a transposed read takes lie
+  // in different banks
+  static constexpr int LDSROW = DH * 2 + 32, LDSBYTES = 32 * LDSROW, VN = DH / 16;
+  DEVI static u32x4 row_frag(const char *row, int st, int g) { return *(const u32x4 *)(row + (st * 32 + g * 8) * 2); }
+  DEVI static floatx4 score(const u32x4 (&k)[KST], const u32x4 (&q)[KST]) {
+    floatx4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < KST; ++st)
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[st]), __builtin_bit_cast(bf16x8, q[st]), s, 0, 0, 0);
+    return s;
+  }
+  // v: VN 16-byte items of the 32 rows, item n of lane l at row n * (64 / LPR) + l / LPR
+  static constexpr int LPR = DH / 8;
+  DEVI static int v_row(int n, int lane) { return n * (64 / LPR) + lane / LPR; }
+  DEVI static int v_col(int lane) { return (lane % LPR) * 16; }
+  // Which of the 32 slots hold NaN or an infinity in v (the same in every lane); those values become 0.
+  DEVI static uint32_t take_odd(u32x4 (&v)[VN], int lane) {
+    uint32_t odd = 0;
+#pragma unroll
+    for (int n = 0; n < VN; ++n) {
+      bool mine = false;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const bool lo = (v[n][c] & 0x7f80u) == 0x7f80u, hi = (v[n][c] & 0x7f800000u) == 0x7f800000u;
+        v[n][c] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+        mine |= lo || hi;
+      }
+      const uint64_t all = __ballot(mine);
+#pragma unroll
+      for (int y = 0; y < 64 / LPR; ++y)
+        if (all >> (y * LPR) & ((1ull << LPR) - 1)) odd |= 1u << (n * (64 / LPR) + y);
+    }
+    return odd;
+  }
+  // p: weights of slots 16 tt + 4 g + e, as high and low bf16 parts: with one part the rounding of the weights
+  // (2^-9 of each) would add as much error as the output's own
+  DEVI static void add(char *lds, const float (&p)[8], floatx4 (&o)[OT], int lane) {
+    const int g = lane >> 4, r = lane & 15;
+    bf16x8 hi, lo;
+    split8(p, hi, lo);
+#pragma unroll
+    for (int t = 0; t < OT; ++t) {
+      typedef __attribute__((address_space(3))) short4v lds4;
+      const char *at = lds + (4 * g + r / 4) * LDSROW + (16 * t + (r % 4) * 4) * 2;
+      const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)at);
+      const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(at + 16 * LDSROW));
+      typedef __attribute__((ext_vector_type(8))) short short8v;
+      const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, o[t], 0, 0, 0);
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, o[t], 0, 0, 0);
+    }
+  }
+  // first column of the four that o[t] holds in lane group g
+  DEVI static int out_col(int t, int g) { return 16 * t + 4 * g; }
+  static constexpr int OSTEP = 1;  // and their distance
+};
+
+template <int DH> struct Ops<float, DH> {
+  static constexpr int KST = DH / 16, OT = DH / 16;
+  static constexpr int LDSROW = 0, LDSBYTES = 0, VN = DH / 8;
+  DEVI static u32x4 row_frag(const char *row, int st, int g) { return *(const u32x4 *)(row + (st * 16 + g * 4) * 4); }
+  DEVI static floatx4 score(const u32x4 (&k)[KST], const u32x4 (&q)[KST]) {
+    floatx4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < KST; ++st)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[st][e]), __uint_as_float(q[st][e]), s, 0, 0, 0);
+    return s;
+  }
+  // v: item n = (slot 16 tt + 4 g + e, 64 columns jj) as n = (tt * 4 + e) * (DH / 64) + jj: four columns 64 jj + 4 r
+  static constexpr int JJ = DH / 64;
+  DEVI static int v_row(int n, int lane) { return 16 * (n / JJ / 4) + 4 * (lane >> 4) + n / JJ % 4; }
+  DEVI static uint32_t take_odd(u32x4 (&v)[VN], int lane) {
+    uint32_t odd = 0;
+#pragma unroll
+    for (int n = 0; n < VN; ++n) {
+      bool mine = false;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const bool bad = (v[n][c] & 0x7f800000u) == 0x7f800000u;
+        v[n][c] = bad ? 0u : v[n][c];
+        mine |= bad;
+      }
+      const uint64_t all = __ballot(mine);
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        if (all >> (16 * y) & 0xffffull) odd |= 1u << (16 * (n / JJ / 4) + 4 * y + n / JJ % 4);
+    }
+    return odd;
+  }
+  DEVI static void add(const u32x4 (&v)[VN], const float (&p)[8], floatx4 (&o)[OT]) {
+#pragma unroll
+    for (int n = 0; n < VN; ++n)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        o[n % JJ * 4 + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[n][c]), p[n / JJ], o[n % JJ * 4 + c], 0, 0, 0);
+  }
+  // o[jj * 4 + c], lane group g, element e: column 64 jj + 16 g + 4 e + c
+  DEVI static int out_col(int t, int g) { return 64 * (t / 4) + 16 * g + t % 4; }
+  static constexpr int OSTEP = 4;
+};
+
+// Scores of 32 slots and a tile of 16 rows: lane (g, r) gets row r's of slots 16 (e / 4) + 4 g + e % 4.  (Single values from
+// here on: with elements of the product's vectors replaced under the branches of a mask, this compiler (ROCm 7.2) wrote one
+// element over the other three.)
+template <typename T, int DH>
+DEVI void score8(const u32x4 (&k)[2][Ops<T, DH>::KST], const u32x4 (&q)[Ops<T, DH>::KST], float (&x)[8]) {
+  const floatx4 s0 = Ops<T, DH>::score(k[0], q), s1 = Ops<T, DH>::score(k[1], q);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = s0[e];
+    x[4 + e] = s1[e];
+  }
+}
+
+// A slot that holds NaN or infinities in v, which the products took as 0: they go, weighted, to the rows that see it.
+template <typename T, int DH>
+DEVI void add_odd(const char *row, int slot, const float (&p)[8], uint32_t dark, floatx4 (&o)[Ops<T, DH>::OT], int lane) {
+  using O = Ops<T, DH>;
+  const int g = lane >> 4, src = 16 * (slot % 16 / 4) + (lane & 15), e = 4 * (slot / 16) + slot % 4;
+  float w = 0.f;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) w = x == e ? p[x] : w;
+  w = __shfl(w, src, 64);
+  const bool seen = !(__shfl(dark, src, 64) >> e & 1);
+#pragma unroll
+  for (int t = 0; t < O::OT; ++t)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float v = to_f32(((const T *)row)[O::out_col(t, g) + c * O::OSTEP]);
+      const bool bad = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
+      o[t][c] += bad && seen ? w * v : 0.f;
+    }
+}
+
+constexpr int kPaThreads = 256, kPaWaves = 4, kPaStep = 32;
+
+// A workgroup has a tile of 16 NT rows and a run of slots, a wave every fourth 32 slots of it; the waves' results are
+// joined in LDS.  Bound by the cache's bytes where rows are few.
+template <typename T, int DH, int NT, bool MASKED>
+__global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a, int splits, int run) {
+  using O = Ops<T, DH>;
+  constexpr int M = 16 * NT, ESZ = sizeof(T);
+  constexpr int MERGE = kPaWaves * 16 * (DH + 4) * 4;
+  constexpr int VBYTES = kPaWaves * O::LDSBYTES;
+  __shared__ __align__(16) char lds[MERGE > VBYTES ? MERGE : VBYTES];
+  __shared__ float s_m[kPaWaves][M], s_l[kPaWaves][M];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
+  const int kvh = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % splits;
+  const long tile = blockIdx.x / a.c.n_kv / splits;
+  Tile t;
+  if (blockIdx.x == gridDim.x - 1 && wave == 0) report_lengths(a);
+  if (!find_tile(a, tile, M, t)) return;
+  const int k0 = split * run, k1 = min(t.vis, k0 + run);
+  if (k0 >= k1) return;
+  const int G = a.nq / a.c.n_kv, n0 = t.s.len - t.s.n;
+
+  u32x4 q[NT][O::KST];
+  int lim[NT];  // the last slot that this lane's row sees, causally
+  const uint8_t *mrow[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = t.row0 + 16 * nt + r, i = min(row, t.rows - 1) / G;
+    lim[nt] = row < t.rows ? n0 + i : -1;
+    if (MASKED) mrow[nt] = a.mask + (int64_t)(t.s.start + i) * a.mask_ld;
+    const char *p = (const char *)a.q + ((int64_t)(t.s.start + i) * a.q_stride + (int64_t)(kvh * G + min(row, t.rows - 1) % G) * DH) * ESZ;
+#pragma unroll
+    for (int st = 0; st < O::KST; ++st) q[nt][st] = O::row_frag(p, st, g);
+  }
+  float m[NT], l[NT];
+  floatx4 o[NT][O::OT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    m[nt] = -INFINITY;
+    l[nt] = 0.f;
+#pragma unroll
+    for (int x = 0; x < O::OT; ++x) o[nt][x] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float sc = a.scale * kLog2e;
+  const char *kb = a.c.k + (a.layer * a.c.layer_stride + kvh * a.c.head_stride) * ESZ;
+  const char *vb = a.c.v + (a.layer * a.c.layer_stride + kvh * a.c.head_stride) * ESZ;
+  char *mylds = lds + wave * O::LDSBYTES;
+  bool lost = false;
+
+  for (int kt = k0 + wave * kPaStep; kt < k1; kt += kPaWaves * kPaStep) {
+    // lane x's slot kt + x % 32: its page, and so every lane's rows'
+    int page = page_of(a.c, t.b, min(kt + (lane & 31), k1 - 1));
+    if (page < 0) {
+      lost = true;
+      page = 0;
+    }
+    auto row_at = [&](const char *base, int x) {
+      return base + slot_offset(a.c, __shfl(page, x, 64), min(kt + x, k1 - 1)) * ESZ;
+    };
+    u32x4 k[2][O::KST], v[O::VN];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const char *p = row_at(kb, 16 * tt + r);
+#pragma unroll
+      for (int st = 0; st < O::KST; ++st) k[tt][st] = O::row_frag(p, st, g);
+    }
+    // rows past the run's end are zeros: a weight of 0 times what lies there might be NaN
+#pragma unroll
+    for (int n = 0; n < O::VN; ++n) {
+      const int x = O::v_row(n, lane);
+      const char *p = row_at(vb, x);
+      if constexpr (ESZ == 2) v[n] = *(const u32x4 *)(p + O::v_col(lane));
+      else v[n] = *(const u32x4 *)(p + (64 * (n % O::JJ) + 4 * r) * 4);
+      if (kt + x >= k1) v[n] = u32x4{0, 0, 0, 0};
+    }
+    const bool whole = kt + kPaStep <= min(n0, k1);
+    uint32_t odd = 0;  // slots of this step, some of them hidden from some row, whose v holds NaN or an infinity
+    if (!whole) odd = O::take_odd(v, lane);
+    if constexpr (ESZ == 2) {
+#pragma unroll
+      for (int n = 0; n < O::VN; ++n) *(u32x4 *)(mylds + O::v_row(n, lane) * O::LDSROW + O::v_col(lane)) = v[n];
+      __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float x[8];
+      score8<T, DH>(k, q[nt], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= sc;
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int slot = kt + 16 * (e / 4) + 4 * g + e % 4;
+          bool seen = slot < k1;
+          if (MASKED) seen = seen && (slot < n0 || mrow[nt][max(0, min(slot, t.s.len - 1) - n0)] != 0);
+          else seen = seen && slot <= lim[nt];
+          x[e] = seen ? x[e] : -INFINITY;
+        }
+      }
+      uint32_t dark = 0;  // hidden among this lane's eight
+      float top = x[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+      if (odd) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dark |= x[e] == -INFINITY ? 1u << e : 0u;
+      }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float mn = fmaxf(m[nt], top), ms = mn == -INFINITY ? 0.f : mn;
+      const float alpha = fast_exp2(m[nt] - ms);
+      m[nt] = mn;
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = fast_exp2(x[e] - ms);
+        sum += x[e];
+      }
+      l[nt] = l[nt] * alpha + sum;
+#pragma unroll
+      for (int y = 0; y < O::OT; ++y) o[nt][y] *= alpha;
+      if constexpr (ESZ == 2) O::add(mylds, x, o[nt], lane);
+      else O::add(v, x, o[nt]);
+      if (odd) {
+#pragma unroll 1
+        for (int e = 0; e < 32; ++e)
+          if (odd >> e & 1)
+            add_odd<T, DH>(vb + slot_offset(a.c, __builtin_amdgcn_readlane(page, e), kt + e) * ESZ, e, x, dark, o[nt], lane);
+      }
+    }
+    if constexpr (ESZ == 2) __builtin_amdgcn_wave_barrier();
+  }
+  if (lost) raise_error(a.err, DEV_BAD_PAGE);
+
+  // the waves' maxima and sums, then their rows 16 at a time
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    l[nt] += __shfl_xor(l[nt], 16, 64);
+    l[nt] += __shfl_xor(l[nt], 32, 64);
+    if (g == 0) {
+      s_m[wave][16 * nt + r] = m[nt];
+      s_l[wave][16 * nt + r] = l[nt];
+    }
+  }
+  float *om = (float *)lds;
+  constexpr int LD = DH + 4;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < O::OT; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) om[(wave * 16 + r) * LD + O::out_col(x, g) + e * O::OSTEP] = o[nt][x][e];
+    __syncthreads();
+    // 16 threads a row
+    const int rr = threadIdx.x / 16, c0 = threadIdx.x % 16, row = t.row0 + 16 * nt + rr;
+    if (row >= t.rows) continue;
+    float top = -INFINITY, sum = 0.f, f[kPaWaves];
+#pragma unroll
+    for (int w = 0; w < kPaWaves; ++w) top = fmaxf(top, s_m[w][16 * nt + rr]);
+    const float ms = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < kPaWaves; ++w) {
+      f[w] = fast_exp2(s_m[w][16 * nt + rr] - ms);
+      sum += s_l[w][16 * nt + rr] * f[w];
+    }
+    const int tok = t.s.start + row / G, head = kvh * G + row % G;
+    const int64_t at = ((int64_t)split * a.tokens + tok) * a.nq + head;
+    const float inv = a.part_o ? 1.f : (sum == 0.f ? 0.f : 1.f / sum);
+#pragma unroll
+    for (int cc = 0; cc < DH / 64; ++cc) {
+      const int c = cc * 64 + c0 * 4;
+      floatx4 y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kPaWaves; ++w) y += *(const floatx4 *)(om + (w * 16 + rr) * LD + c) * f[w];
+      y *= inv;
+      if (a.part_o) {
+        *(floatx4 *)(a.part_o + at * DH + c) = y;
+      } else {
+        T *dst = (T *)a.out + (int64_t)tok * a.o_stride + (int64_t)head * DH + c;
+        if constexpr (ESZ == 2) {
+          *(uint2 *)dst = make_uint2((uint32_t)f32_to_bf16(y[0]).v | ((uint32_t)f32_to_bf16(y[1]).v << 16),
+                                     (uint32_t)f32_to_bf16(y[2]).v | ((uint32_t)f32_to_bf16(y[3]).v << 16));
+        } else {
+          *(floatx4 *)dst = y;
+        }
+      }
+    }
+    if (c0 == 0) {
+      if (a.part_o) *(float2 *)(a.part_ml + at * 2) = make_float2(top, sum);
+      else if (a.lse) a.lse[(int64_t)tok * a.nq + head] = (top + log2f(sum)) * kLn2;
+    }
+  }
+}
+
+// Joins the runs of one row (a new token's query head), a wave a row.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, int M, int run) {
+  const int lane = threadIdx.x & 63;
+  const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= (long)a.tokens * a.nq) return;
+  const int tok = (int)(at / a.nq), head = (int)(at % a.nq), G = a.nq / a.c.n_kv;
+  int b = 0;
+  for (int s0 = 0; s0 < a.c.batch; s0 += 64) b += __popcll(__ballot(s0 + lane < a.c.batch && a.starts[s0 + lane + 1] <= tok));
+  SeqRange s;
+  if (b >= a.c.batch || !seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s)) return;
+  if (tok < s.start || tok >= s.start + s.n) return;
+  const int row = (tok - s.start) * G + head % G, last = (min((row / M + 1) * M, s.n * G) - 1) / G;
+  const int vis = a.mask ? s.len : s.len - s.n + last + 1, runs = (vis + run - 1) / run;
+  const int64_t step = (int64_t)a.tokens * a.nq;
+  // a lane's runs as one (maximum, sum), then over the lanes
+  float m = -INFINITY, l = 0.f;
+  for (int x = lane; x < runs; x += 64) {
+    const float2 v = *(const float2 *)(a.part_ml + (at + x * step) * 2);
+    const float mn = fmaxf(m, v.x), ms = mn == -INFINITY ? 0.f : mn;
+    l = l * fast_exp2(m - ms) + v.y * fast_exp2(v.x - ms);
+    m = mn;
+  }
+  const float top = wave_max(m), ms = top == -INFINITY ? 0.f : top;
+  const float sum = wave_sum(l * fast_exp2(m - ms));
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  constexpr int E = DH / 64;
+  float y[E] = {};
+  for (int x = 0; x < runs; ++x) {
+    const float f = fast_exp2(a.part_ml[(at + x * step) * 2] - ms) * inv;
+    const float *p = a.part_o + (at + x * step) * DH + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] += p[e] * f;
+  }
+  T *dst = (T *)a.out + (int64_t)tok * a.o_stride + (int64_t)head * DH + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) store_as(dst + e, y[e]);
+  if (lane == 0 && a.lse) a.lse[at] = (top + log2f(sum)) * kLn2;
+}
+
+// weights[slot] += the sum over the call's rows of p: a wave has 32 slots of one kv head and goes over every row that may
+// see them, in order (so the sum is the same every time).
+template <typename T, int DH, bool MASKED>
+__global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs a, int slabs) {
+  using O = Ops<T, DH>;
+  constexpr int ESZ = sizeof(T);
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv / slabs;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kt = (blockIdx.x / a.c.n_kv % slabs * kPaWaves + wave) * kPaStep;
+  SeqRange s;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || kt >= s.len) return;
+  const int G = a.nq / a.c.n_kv, n0 = s.len - s.n, rows = s.n * G;
+  const int page = page_of(a.c, b, min(kt + (lane & 31), s.len - 1));
+  const char *kb = a.c.k + (a.layer * a.c.layer_stride + kvh * a.c.head_stride) * ESZ;
+  u32x4 k[2][O::KST];
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt) {
+    const int x = 16 * tt + r;
+    const char *p = kb + slot_offset(a.c, max(__shfl(page, x, 64), 0), min(kt + x, s.len - 1)) * ESZ;
+#pragma unroll
+    for (int st = 0; st < O::KST; ++st) k[tt][st] = O::row_frag(p, st, g);
+  }
+  const float sc = a.scale * kLog2e;
+  float sum[8] = {};
+  // the first row that sees slot kt
+  const int first = MASKED ? 0 : max(0, kt - n0) * G / 16 * 16;
+  for (int row0 = first; row0 < rows; row0 += 16) {
+    const int row = min(row0 + r, rows - 1), i = row / G, head = kvh * G + row % G;
+    const int64_t tok = s.start + i;
+    const char *p = (const char *)a.q + (tok * a.q_stride + (int64_t)head * DH) * ESZ;
+    u32x4 q[O::KST];
+#pragma unroll
+    for (int st = 0; st < O::KST; ++st) q[st] = O::row_frag(p, st, g);
+    const float ls = a.lse[tok * a.nq + head] * kLog2e;
+    const bool live = row0 + r < rows && ls != -INFINITY;
+    float x[8];
+    score8<T, DH>(k, q, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int slot = kt + 16 * (e / 4) + 4 * g + e % 4;
+      bool seen = live && slot < s.len;
+      if (MASKED) seen = seen && (slot < n0 || a.mask[tok * a.mask_ld + max(0, min(slot, s.len - 1) - n0)] != 0);
+      else seen = seen && slot <= n0 + i;
+      const float w = fast_exp2(x[e] * sc - ls);
+      sum[e] += seen ? w : 0.f;
+    }
+  }
+  // over the 16 rows of a lane group
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float v = sum[e];
+    v += row_ror<8>(v);
+    v += row_ror<4>(v);
+    v += row_ror<2>(v);
+    v += row_ror<1>(v);
+    const int x = 16 * (e / 4) + 4 * g + e % 4, pg = __shfl(page, x, 64);
+    if (r == 0 && kt + x < s.len && pg >= 0) a.c.weights[weight_offset(a.c, a.layer, pg, kvh, kt + x)] += v;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// launchers
+// ---------------------------------------------------------------------------
+PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv, int max_new, int max_len) {
+  (void)bf16;
+  const int G = nq / n_kv;
+  PagedAttnPlan p;
+  p.rows = (long)max_new * G <= 16 ? 16 : 32;
+  p.tiles = (long)tokens * G / p.rows + (tokens < batch ? tokens : batch);
+  // runs of whole 128 slots, as many as give each CU a few workgroups
+  const long groups = p.tiles * n_kv;
+  const long want = groups >= 1024 ? 1 : (1024 + groups - 1) / groups;
+  const int pieces = (int)(((long)max_len + 127) / 128);
+  const int splits = (int)(want < pieces ? want : pieces);
+  p.run = (pieces + splits - 1) / splits * 128;
+  p.splits = (int)(((long)max_len + p.run - 1) / p.run);
+  return p;
+}
+
+template <typename T, int DH, bool MASKED>
+static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t st) {
+  const dim3 grid((unsigned)(p.tiles * p.splits * a.c.n_kv)), block(kPaThreads);
+  if (p.rows == 16) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 1, MASKED>), grid, block, 0, st, a, p.splits, p.run);
+  else hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED>), grid, block, 0, st, a, p.splits, p.run);
+  if (p.splits > 1)
+    hipLaunchKernelGGL((paged_attn_join_kernel<T, DH>), dim3((unsigned)(((long)a.tokens * a.nq + 3) / 4)), dim3(256), 0, st, a, p.rows, p.run);
+  if (a.accumulate) {
+    const int slabs = (a.max_len + kPaWaves * kPaStep - 1) / (kPaWaves * kPaStep);
+    hipLaunchKernelGGL((paged_weights_kernel<T, DH, MASKED>), dim3((unsigned)((long)slabs * a.c.batch * a.c.n_kv)), block, 0, st, a, slabs);
+  }
+}
+template <typename T, int DH>
+static void attn_masked(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t st) {
+  a.mask ? attn_of<T, DH, true>(a, p, st) : attn_of<T, DH, false>(a, p, st);
+}
+void launch_paged_attn(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t st) {
+  if (a.c.bf16) a.c.dh == 128 ? attn_masked<bf16_t, 128>(a, p, st) : attn_masked<bf16_t, 64>(a, p, st);
+  else a.c.dh == 128 ? attn_masked<float, 128>(a, p, st) : attn_masked<float, 64>(a, p, st);
+}
+
+}  // namespace dk
