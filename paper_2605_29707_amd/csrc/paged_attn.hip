@@ -296,9 +296,9 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int slot = kt + 16 * (e / 4) + 4 * g + e % 4;
-          bool seen = slot < k1;
-          if (MASKED) seen = seen && (slot < n0 || mrow[nt][max(0, min(slot, t.s.len - 1) - n0)] != 0);
-          else seen = seen && slot <= lim[nt];
+          bool seen = slot <= lim[nt];
+          if (MASKED) seen = (slot < n0) | (mrow[nt][max(0, min(slot, t.s.len - 1) - n0)] != 0);
+          seen &= slot < k1;
           x[e] = seen ? x[e] : -INFINITY;
         }
       }
@@ -398,6 +398,239 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
   }
 }
 
+// ---------------------------------------------------------------------------
+// Chunks: a workgroup has 128 rows, 32 a wave, and goes over a run's slots 64 at a time through two LDS buffers.  The
+// products are 32 x 32 x 16: scores S^T = K Q^T leave lane l = 32 h + r with row r's of slots 8 (e / 4) + 4 h + e % 4, which is
+// again the second operand of O^T = V^T P^T for the slots of a step in the order (4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3).
+// Weights are rounded to bf16 for that product (half a step of each, as far off as the output's own rounding).
+// A wave reads every row of k and v from LDS once: as many bytes a clock as the products of 32 rows take.  In both
+// buffers a row's 16-byte items are permuted by the row, so that neither read has bank conflicts: k's 16 rows of one item,
+// v's eight rows of 32 bytes.
+// ---------------------------------------------------------------------------
+constexpr int kChunkRows = 128, kChunkStep = 64;
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+template <int DH, bool MASKED>
+__global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, int splits, int run) {
+  constexpr int RB = DH * 2, CH = RB / 16, KST = DH / 16, DT = DH / 32, LPT = kChunkStep * CH / 256, TILE = kChunkStep * RB;
+  __shared__ __align__(16) char s_k[2][TILE], s_v[2][TILE];
+  __shared__ uint64_t s_odd[2][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, r = lane & 31;
+  const int kvh = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % splits;
+  const long tile = blockIdx.x / a.c.n_kv / splits;
+  Tile t;
+  if (blockIdx.x == gridDim.x - 1 && wave == 0) report_lengths(a);
+  if (!find_tile(a, tile, kChunkRows, t)) return;
+  const int k0 = split * run, k1 = min(t.vis, k0 + run);
+  if (k0 >= k1) return;
+  const int G = a.nq / a.c.n_kv, n0 = t.s.len - t.s.n;
+  // slots below this are seen by all rows of the workgroup
+  const int clear = min(k1, MASKED ? n0 : n0 + t.row0 / G + 1);
+
+  const int row = t.row0 + wave * 32 + r, row_in = min(row, t.rows - 1), tok = t.s.start + row_in / G;
+  const int lim = row < t.rows ? n0 + row_in / G : -1;
+  const uint8_t *mrow = MASKED ? a.mask + (int64_t)tok * a.mask_ld : nullptr;
+  u32x4 q[KST];
+  {
+    const char *p = (const char *)a.q + ((int64_t)tok * a.q_stride + (int64_t)(kvh * G + row_in % G) * DH) * 2;
+#pragma unroll
+    for (int st = 0; st < KST; ++st) q[st] = *(const u32x4 *)(p + st * 32 + h * 16);
+  }
+  const float sc = a.scale * kLog2e;
+  const int64_t head = a.layer * a.c.layer_stride + kvh * a.c.head_stride;
+  const char *kb = a.c.k + head * 2, *vb = a.c.v + head * 2;
+
+  // this thread's items of a tile: 16 bytes of row (tid + 256 i) / CH
+  const int my_row = tid / CH, my_col = tid % CH;
+  bool lost = false;
+  u32x4 kr[LPT], vr[LPT];
+  auto load = [&](int kt) {
+#pragma unroll
+    for (int i = 0; i < LPT; ++i) {
+      const int slot = min(kt + my_row + i * (256 / CH), k1 - 1);
+      int page = page_of(a.c, t.b, slot);
+      if (page < 0) {
+        lost = true;
+        page = 0;
+      }
+      const int64_t at = slot_offset(a.c, page, slot) * 2 + my_col * 16;
+      kr[i] = *(const u32x4 *)(kb + at);
+      vr[i] = *(const u32x4 *)(vb + at);
+    }
+  };
+  auto swz_k = [](int x) { return CH == 16 ? x & 15 : (x >> 1) & 7; };
+  auto swz_v = [](int x) { return (CH == 16 ? (x & 3) << 2 : (x & 2) << 1) | ((x >> 1) & 2); };
+  auto store = [&](int kt, int buf) {
+    if (kt + kChunkStep > clear) {  // workgroup-uniform
+      uint64_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < LPT; ++i) {
+        const int x = my_row + i * (256 / CH);
+        bool mine = false;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const bool lo = (vr[i][c] & 0x7f80u) == 0x7f80u, hi = (vr[i][c] & 0x7f800000u) == 0x7f800000u;
+          vr[i][c] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+          mine |= lo || hi;
+        }
+        // rows past the run's end count for nothing
+        const uint64_t all = __ballot(mine && kt + x < k1);
+#pragma unroll
+        for (int y = 0; y < 64 / CH; ++y)
+          if (all >> (y * CH) & ((1ull << CH) - 1)) odd |= 1ull << (wave * (64 / CH) + i * (256 / CH) + y);
+      }
+      if (lane == 0) s_odd[buf][wave] = odd;
+    }
+#pragma unroll
+    for (int i = 0; i < LPT; ++i) {
+      const int x = my_row + i * (256 / CH);
+      *(u32x4 *)(s_k[buf] + x * RB + (my_col ^ swz_k(x)) * 16) = kr[i];
+      *(u32x4 *)(s_v[buf] + x * RB + (my_col ^ swz_v(x)) * 16) = vr[i];
+    }
+  };
+
+  float m = -INFINITY, l = 0.f;
+  floatx16 o[DT];
+#pragma unroll
+  for (int x = 0; x < DT; ++x)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[x][e] = 0.f;
+  const int k_at = r * RB + (h ^ swz_k(r)) * 16;  // item 2 st + h: with the bits of st
+  const int v_i = lane & 15, v_x = 4 * h + v_i / 4, v_half = (lane >> 4) & 1;
+
+  load(k0);
+  store(k0, 0);
+  __syncthreads();
+  int buf = 0;
+  for (int kt = k0; kt < k1; kt += kChunkStep, buf ^= 1) {
+    const bool more = kt + kChunkStep < k1;
+    if (more) load(kt + kChunkStep);
+    floatx16 s[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[y][e] = 0.f;
+#pragma unroll
+      for (int st = 0; st < KST; ++st) {
+        const u32x4 f = *(const u32x4 *)(s_k[buf] + y * 32 * RB + (k_at ^ (st * 32)));
+        s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, q[st]), s[y], 0, 0, 0);
+      }
+    }
+    float x[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) x[e] = s[e / 16][e % 16];
+    uint64_t odd = 0;
+    uint32_t dark = 0;
+    if (kt + kChunkStep > clear) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) odd |= s_odd[buf][w];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const int slot = kt + 32 * (e / 16) + 8 * (e % 16 / 4) + 4 * h + e % 4;
+        bool seen = slot <= lim;
+        if (MASKED) seen = (slot < n0) | (mrow[max(0, min(slot, t.s.len - 1) - n0)] != 0);
+        seen &= slot < k1;
+        x[e] = seen ? x[e] : -INFINITY;
+        dark |= x[e] == -INFINITY ? 1u << e : 0u;
+      }
+    }
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < 32; ++e) top = fmaxf(top, x[e]);
+    {
+      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * sc;
+    }
+    // the sums' common factor 2^-m moves only when a row's maximum passes it by 2^6: weights stay below 2^6, and most steps
+    // leave the output as it is
+    if (__ballot(top > m + 6.f)) {
+      const float mn = fmaxf(m, top), alpha = fast_exp2(m - (mn == -INFINITY ? 0.f : mn));
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int y = 0; y < DT; ++y) o[y] *= alpha;
+    }
+    const float ms = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      x[e] = fast_exp2(fmaf(x[e], sc, -ms));
+      sum += x[e];
+    }
+    l += sum;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      bf16x8 p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = (__bf16)x[8 * u + e];
+#pragma unroll
+      for (int y = 0; y < DT; ++y) {
+        typedef __attribute__((address_space(3))) short4v lds4;
+        typedef __attribute__((ext_vector_type(8))) short short8v;
+        const int c = (y * 4 + v_half * 2 + (v_i & 3) / 2) ^ swz_v(v_x);
+        const char *at = s_v[buf] + (16 * u + v_x) * RB + c * 16 + (v_i & 1) * 8;
+        const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)at);
+        const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(at + 8 * RB));
+        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o[y], 0, 0, 0);
+      }
+    }
+    if (odd) {  // values that the product took as 0 go, weighted, to the rows that see them
+#pragma unroll 1
+      for (int e = 0; e < kChunkStep; ++e) {
+        if (!(odd >> e & 1)) continue;
+        const int page = max(page_of(a.c, t.b, kt + e), 0);
+        const uint16_t *vrow = (const uint16_t *)(vb + slot_offset(a.c, page, kt + e) * 2);
+        const int src = 32 * ((e >> 2) & 1) + r, at = 16 * (e >> 5) + 4 * ((e >> 3) & 3) + (e & 3);
+        float w = 0.f;
+#pragma unroll
+        for (int y = 0; y < 32; ++y) w = y == at ? x[y] : w;
+        w = __shfl(w, src, 64);
+        const bool seen = !(__shfl(dark, src, 64) >> at & 1);
+#pragma unroll
+        for (int y = 0; y < DT; ++y)
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            const float v = __uint_as_float((uint32_t)vrow[32 * y + 8 * (c / 4) + 4 * h + c % 4] << 16);
+            const bool bad = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
+            o[y][c] += bad && seen ? w * v : 0.f;
+          }
+      }
+    }
+    if (more) store(kt + kChunkStep, buf ^ 1);
+    __syncthreads();
+  }
+  if (lost) raise_error(a.err, DEV_BAD_PAGE);
+  {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+  }
+  if (row >= t.rows) return;
+  const int qh = kvh * G + row % G;
+  const int64_t at = ((int64_t)split * a.tokens + tok) * a.nq + qh;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int y = 0; y < DT; ++y)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int col = 32 * y + 8 * c + 4 * h;
+      if (a.part_o) {
+        *(floatx4 *)(a.part_o + at * DH + col) = floatx4{o[y][4 * c], o[y][4 * c + 1], o[y][4 * c + 2], o[y][4 * c + 3]};
+      } else {
+        float z[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = o[y][4 * c + e] * inv;
+        bf16_t *dst = (bf16_t *)a.out + (int64_t)tok * a.o_stride + (int64_t)qh * DH + col;
+        *(uint2 *)dst = make_uint2((uint32_t)f32_to_bf16(z[0]).v | ((uint32_t)f32_to_bf16(z[1]).v << 16),
+                                   (uint32_t)f32_to_bf16(z[2]).v | ((uint32_t)f32_to_bf16(z[3]).v << 16));
+      }
+    }
+  if (h == 0) {
+    if (a.part_o) *(float2 *)(a.part_ml + at * 2) = make_float2(m, l);
+    else if (a.lse) a.lse[(int64_t)tok * a.nq + qh] = (m + log2f(l)) * kLn2;
+  }
+}
+
 // Joins the runs of one row (a new token's query head), a wave a row.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, int M, int run) {
@@ -479,9 +712,9 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int slot = kt + 16 * (e / 4) + 4 * g + e % 4;
-      bool seen = live && slot < s.len;
-      if (MASKED) seen = seen && (slot < n0 || a.mask[tok * a.mask_ld + max(0, min(slot, s.len - 1) - n0)] != 0);
-      else seen = seen && slot <= n0 + i;
+      bool seen = slot <= n0 + i;
+      if (MASKED) seen = (slot < n0) | (a.mask[tok * a.mask_ld + max(0, min(slot, s.len - 1) - n0)] != 0);
+      seen = seen & live & (slot < s.len);
       const float w = fast_exp2(x[e] * sc - ls);
       sum[e] += seen ? w : 0.f;
     }
@@ -503,10 +736,9 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
 // launchers
 // ---------------------------------------------------------------------------
 PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv, int max_new, int max_len) {
-  (void)bf16;
   const int G = nq / n_kv;
   PagedAttnPlan p;
-  p.rows = (long)max_new * G <= 16 ? 16 : 32;
+  p.rows = (long)max_new * G <= 16 ? 16 : (bf16 && (long)max_new * G > 32 ? kChunkRows : 32);
   p.tiles = (long)tokens * G / p.rows + (tokens < batch ? tokens : batch);
   // runs of whole 128 slots, as many as give each CU a few workgroups
   const long groups = p.tiles * n_kv;
@@ -521,8 +753,10 @@ PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv
 template <typename T, int DH, bool MASKED>
 static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t st) {
   const dim3 grid((unsigned)(p.tiles * p.splits * a.c.n_kv)), block(kPaThreads);
+  if constexpr (sizeof(T) == 2)
+    if (p.rows == kChunkRows) hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED>), grid, block, 0, st, a, p.splits, p.run);
   if (p.rows == 16) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 1, MASKED>), grid, block, 0, st, a, p.splits, p.run);
-  else hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED>), grid, block, 0, st, a, p.splits, p.run);
+  else if (p.rows == 32) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED>), grid, block, 0, st, a, p.splits, p.run);
   if (p.splits > 1)
     hipLaunchKernelGGL((paged_attn_join_kernel<T, DH>), dim3((unsigned)(((long)a.tokens * a.nq + 3) / 4)), dim3(256), 0, st, a, p.rows, p.run);
   if (a.accumulate) {
