@@ -504,7 +504,8 @@ domino_status domino_sample_logits(int32_t rows, int32_t vocab, const void *logi
  * (strides, k and v).  No two rows overlap.
  *  k, v            device, storage type; K is post k-norm and RoPE
  *  weights         device fp32 [n_layers][n_pages][n_kv_heads][page_size], the attention
- *                  weight that every slot has received, or NULL (domino_paged_evict needs it)
+ *                  weight that every slot has received, aligned to 16 bytes, or NULL (domino_paged_evict
+ *                  needs it)
  *  page_table      device int32 [batch][max_pages]; only entries of slots in use are read
  *  page_size       a power of two up to 65536; max_pages * page_size below 2^30
  *  head_dim        64 or 128

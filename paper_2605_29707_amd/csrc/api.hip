@@ -1449,7 +1449,7 @@ domino_status check_paged(const domino_paged_cache *c) {
   for (const auto &d : dims)
     if (d.n > 1 && (d.stride < c->head_dim || d.stride % vec))
       return fail(DOMINO_ERR_INVALID_ARG, "a stride of the cache is below head_dim or no multiple of 16 bytes");
-  if ((uintptr_t)c->k % 16 || (uintptr_t)c->v % 16 || (uintptr_t)c->weights % 4 || (uintptr_t)c->page_table % 4)
+  if ((uintptr_t)c->k % 16 || (uintptr_t)c->v % 16 || (uintptr_t)c->weights % 16 || (uintptr_t)c->page_table % 4)
     return fail(DOMINO_ERR_INVALID_ARG, "a pointer of the cache is not aligned");
   return DOMINO_OK;
 }
@@ -1497,7 +1497,7 @@ domino_status check_tokens(const domino_paged_cache *c, int32_t layer, int32_t t
 }
 struct PagedAttnLayout {
   PagedAttnPlan plan;
-  size_t lse, ml, o, bytes;
+  size_t lse, ml, o, scores, bytes;
 };
 domino_status paged_attn_layout(const domino_paged_cache *c, int32_t tokens, int32_t n_q_heads, int32_t max_new, int32_t max_len,
                                 int32_t accumulate, PagedAttnLayout &w) {
@@ -1506,7 +1506,8 @@ domino_status paged_attn_layout(const domino_paged_cache *c, int32_t tokens, int
   if (max_new < 1 || max_len < 1) return fail(DOMINO_ERR_INVALID_ARG, "max_new and max_len must be >= 1");
   if (max_len > c->max_pages * c->page_size) return fail(DOMINO_ERR_INVALID_ARG, "max_len must be at most max_pages * page_size");
   if (accumulate && !c->weights) return fail(DOMINO_ERR_INVALID_ARG, "the cache has no weights to accumulate into");
-  w.plan = plan_paged_attn(c->dtype == DOMINO_BF16, tokens, c->batch, n_q_heads, c->n_kv_heads, std::min(max_new, tokens), max_len);
+  w.plan = plan_paged_attn(c->dtype == DOMINO_BF16, tokens, c->batch, n_q_heads, c->n_kv_heads, std::min(max_new, tokens), max_len,
+                           accumulate != 0);
   const int64_t slabs = accumulate ? (int64_t)c->batch * c->n_kv_heads * ((max_len + 127) / 128) : 0;
   if ((double)w.plan.tiles * w.plan.splits * c->n_kv_heads > kMaxBlocks || slabs > kMaxBlocks ||
       (int64_t)tokens * n_q_heads / 4 + 1 > kMaxBlocks)
@@ -1515,7 +1516,8 @@ domino_status paged_attn_layout(const domino_paged_cache *c, int32_t tokens, int
   w.lse = 256;
   w.ml = w.lse + (accumulate ? align_up(rows * 4) : 0);
   w.o = w.ml + (w.plan.splits > 1 ? align_up(rows * w.plan.splits * 8) : 0);
-  w.bytes = w.o + (w.plan.splits > 1 ? align_up(rows * w.plan.splits * c->head_dim * 4) : 0);
+  w.scores = w.o + (w.plan.splits > 1 ? align_up(rows * w.plan.splits * c->head_dim * 4) : 0);
+  w.bytes = w.scores + align_up(rows * w.plan.scores_ld * 4);
   return DOMINO_OK;
 }
 domino_status check_evict(const domino_paged_cache *c, int32_t max_len, int32_t budget) {
@@ -1651,6 +1653,8 @@ domino_status domino_paged_attention(const domino_paged_cache *cache, int32_t la
   a.lse = lse ? lse : (accumulate ? (float *)(ws + w.lse) : nullptr);
   a.part_ml = w.plan.splits > 1 ? (float *)(ws + w.ml) : nullptr;
   a.part_o = w.plan.splits > 1 ? (float *)(ws + w.o) : nullptr;
+  a.scores = w.plan.scores_ld ? (float *)(ws + w.scores) : nullptr;
+  a.scores_ld = w.plan.scores_ld;
   a.accumulate = accumulate != 0;
   a.err = (int32_t *)workspace;
   launch_paged_attn(a, w.plan, (hipStream_t)stream);

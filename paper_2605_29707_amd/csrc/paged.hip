@@ -236,17 +236,19 @@ DEVI uint32_t weight_key(float w) {
 }
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+constexpr int kSelStep = 256, kSelBatch = 4;  // slots of a wave's step (four neighbours a lane), steps whose loads are out together
 
 // Which slots of one (layer, sequence, head) stay, in order: the first `sink`, the last `recent`, and the m of greatest
-// weight between them.  The m-th greatest key is found by three counts over its digits (11, 11 and 10 bits); then every wave
-// counts the kept slots of its own stretch and writes them.
+// weight between them.  A wave has a stretch of the slots.  The m-th greatest key is found by three counts over its digits (11, 11
+// and 10 bits); then every wave counts the kept slots of its stretch, and writes them behind those of the waves before it.  Up to
+// 16384 slots the keys stay in registers, else every one of the five passes reads the weights again (from the L2).
 __global__ __launch_bounds__(kSelThreads) void paged_evict_select_kernel(PagedEvictArgs a) {
   const PagedView &c = a.c;
   const int head = blockIdx.x % c.n_kv, b = (blockIdx.x / c.n_kv) % c.batch, layer = blockIdx.x / c.n_kv / c.batch;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool lead = layer == 0 && head == 0 && tid == 0;
   int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
-  int n = a.lens[b];
+  const int n = a.lens[b];
   if (n < 0 || n > a.max_len) {
     if (lead) raise_error(a.err, DEV_BAD_CTX_LEN);
     if (lead) a.new_lens[b] = n;
@@ -264,33 +266,79 @@ __global__ __launch_bounds__(kSelThreads) void paged_evict_select_kernel(PagedEv
   __shared__ uint32_t wsum[kSelWaves], wtie[kSelWaves];
   __shared__ uint32_t s_bin, s_above;
   bool lost = false;
-  auto key_at = [&](int slot) -> uint32_t {
-    const int page = page_of(c, b, slot);
-    if (page < 0) {
-      lost = true;
-      return 0;
+  // a wave's stretch: whole steps, so that a lane's four neighbours lie in one page of four slots or more
+  const int per = (n + kSelWaves * kSelStep - 1) / (kSelWaves * kSelStep) * kSelStep;
+  const int w0 = min(n, wave * per), w1 = min(n, w0 + per);
+  const float *weights = c.weights + (((int64_t)layer * c.n_pages * c.n_kv + head) << c.page_shift);
+  const int64_t page_step = (int64_t)c.n_kv << c.page_shift;
+  const int in_page = (1 << c.page_shift) - 1;
+  auto load = [&](int s0, uint32_t (&key)[kSelBatch][4]) {
+    int page[kSelBatch][4];
+#pragma unroll
+    for (int x = 0; x < kSelBatch; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int slot = min(s0 + x * kSelStep + lane * 4 + e, n - 1);
+        if (e == 0 || c.page_shift < 2) {
+          page[x][e] = page_of(c, b, slot);
+          lost |= page[x][e] < 0;
+        } else {
+          page[x][e] = page[x][0];
+        }
+      }
+    floatx4 w[kSelBatch];
+#pragma unroll
+    for (int x = 0; x < kSelBatch; ++x) {
+      const int slot = s0 + x * kSelStep + lane * 4;
+      if (c.page_shift >= 2) {
+        w[x] = *(const floatx4 *)(weights + max(page[x][0], 0) * page_step + (min(slot, (n - 1) & ~3) & in_page));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[x][e] = weights[max(page[x][e], 0) * page_step + (min(slot + e, n - 1) & in_page)];
+      }
     }
-    return weight_key(c.weights[weight_offset(c, layer, page, head, slot)]);
+#pragma unroll
+    for (int x = 0; x < kSelBatch; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) key[x][e] = page[x][e] < 0 ? 0 : weight_key(w[x][e]);
+  };
+  uint32_t own[kSelBatch][4];
+  const bool keep_keys = per <= kSelBatch * kSelStep;
+  if (keep_keys) load(w0, own);
+  // fn(first slot of the lane's four, their keys) for every step of the wave's stretch
+  auto each = [&](auto fn) {
+    if (keep_keys) {
+#pragma unroll
+      for (int x = 0; x < kSelBatch; ++x)
+        if (w0 + x * kSelStep < w1) fn(w0 + x * kSelStep + lane * 4, own[x]);
+    } else {
+      for (int s0 = w0; s0 < w1; s0 += kSelBatch * kSelStep) {
+        uint32_t key[kSelBatch][4];
+        load(s0, key);
+#pragma unroll
+        for (int x = 0; x < kSelBatch; ++x)
+          if (s0 + x * kSelStep < w1) fn(s0 + x * kSelStep + lane * 4, key[x]);
+      }
+    }
   };
   uint32_t prefix = 0, need = m;  // the wanted key's digits so far, its rank among those that share them
   for (int pass = 0; pass < 3 && m > 0; ++pass) {
     const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
     for (int i = tid; i < 2048; i += kSelThreads) hist[i] = 0;
     __syncthreads();
-    for (int s0 = first + wave * 64; s0 < last; s0 += kSelThreads) {  // wave-uniform
-      const int slot = s0 + lane;
-      const uint32_t key = slot < last ? key_at(slot) : 0;
-      const bool in = slot < last && (pass == 0 || (key >> (shift + bits)) == prefix);
-      const uint32_t bin = (key >> shift) & ((1u << bits) - 1);
-      // the first lane's bin is counted once for all that share it: most slots may hold one value
-      const uint64_t live = __ballot(in);
-      if (live) {
-        const uint32_t b0 = __shfl(bin, __ffsll((unsigned long long)live) - 1, 64);
-        const uint64_t same = __ballot(in && bin == b0);
-        if (in && bin != b0) atomicAdd(&hist[bin], 1u);
-        if (lane == 0) atomicAdd(&hist[b0], (uint32_t)__popcll(same));
+    each([&](int slot, const uint32_t (&key)[4]) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = slot + e >= first && slot + e < min(last, w1) && (pass == 0 || (key[e] >> (shift + bits)) == prefix);
+        if (in) {
+          // the first lane's bin is counted once for all that share it: most slots may hold one value
+          const uint32_t bin = (key[e] >> shift) & ((1u << bits) - 1), b0 = __builtin_amdgcn_readfirstlane(bin);
+          const uint64_t same = __ballot(bin == b0);
+          if (bin != b0) atomicAdd(&hist[bin], 1u);
+          else if (lane == __ffsll((unsigned long long)same) - 1) atomicAdd(&hist[b0], (uint32_t)__popcll(same));
+        }
       }
-    }
+    });
     __syncthreads();
     // from the top bin down: the bin where the running count reaches `need`
     if (wave == 0) {
@@ -318,27 +366,17 @@ __global__ __launch_bounds__(kSelThreads) void paged_evict_select_kernel(PagedEv
     __syncthreads();
     prefix = (prefix << bits) | s_bin;
     need -= s_above;
-    __syncthreads();
   }
   // kept: keys above `prefix`, and the first `need` slots that equal it
-  const int per = (((n + kSelWaves - 1) / kSelWaves) + 63) / 64 * 64;
-  const int w0 = min(n, wave * per), w1 = min(n, w0 + per);
-  auto flags = [&](int slot, bool &sure, bool &tie) {
-    sure = slot < n && (slot < first || slot >= last);
-    tie = false;
-    if (slot >= first && slot < last && m > 0) {
-      const uint32_t key = key_at(slot);
-      sure = key > prefix;
-      tie = key == prefix;
-    }
-  };
   uint32_t ns = 0, nt = 0;
-  for (int s0 = w0; s0 < w1; s0 += 64) {
-    bool sure, tie;
-    flags(s0 + lane < w1 ? s0 + lane : n, sure, tie);
-    ns += __popcll(__ballot(sure));
-    nt += __popcll(__ballot(tie));
-  }
+  each([&](int slot, const uint32_t (&key)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool in = slot + e >= first && slot + e < last;
+      ns += __popcll(__ballot(slot + e < w1 && (!in || (m > 0 && key[e] > prefix))));
+      nt += __popcll(__ballot(slot + e < w1 && in && m > 0 && key[e] == prefix));
+    }
+  });
   if (lane == 0) {
     wsum[wave] = ns;
     wtie[wave] = nt;
@@ -350,18 +388,34 @@ __global__ __launch_bounds__(kSelThreads) void paged_evict_select_kernel(PagedEv
     nt += wtie[w];
   }
   const uint64_t below = (1ull << lane) - 1;
-  for (int s0 = w0; s0 < w1; s0 += 64) {
-    bool sure, tie;
-    flags(s0 + lane < w1 ? s0 + lane : n, sure, tie);
-    const uint64_t bs = __ballot(sure), bt = __ballot(tie);
-    const uint32_t ties = nt + __popcll(bt & below);
-    if (sure || (tie && ties < need)) {
-      const uint32_t at = ns + __popcll(bs & below) + min(ties, need);
-      if (at < (uint32_t)a.budget) kept[at] = s0 + lane;
+  each([&](int slot, const uint32_t (&key)[4]) {
+    uint32_t bs = 0, bt = 0, as = 0, at = 0;  // before this lane's four, and of the whole step
+    uint32_t sure = 0, tie = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool in = slot + e >= first && slot + e < last;
+      const bool s = slot + e < w1 && (!in || (m > 0 && key[e] > prefix)), t = slot + e < w1 && in && m > 0 && key[e] == prefix;
+      const uint64_t vs = __ballot(s), vt = __ballot(t);
+      bs += __popcll(vs & below);
+      bt += __popcll(vt & below);
+      as += __popcll(vs);
+      at += __popcll(vt);
+      sure |= s ? 1u << e : 0u;
+      tie |= t ? 1u << e : 0u;
     }
-    ns += __popcll(bs);
-    nt += __popcll(bt);
-  }
+    bs += ns;
+    bt += nt;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool s = sure >> e & 1, t = tie >> e & 1;
+      const uint32_t to = bs + min(bt, need);
+      if ((s || (t && bt < need)) && to < (uint32_t)a.budget) kept[to] = slot + e;
+      bs += s;
+      bt += t;
+    }
+    ns += as;
+    nt += at;
+  });
   if (lost) raise_error(a.err, DEV_BAD_PAGE);
 }
 

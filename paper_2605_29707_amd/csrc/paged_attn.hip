@@ -302,6 +302,11 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
           x[e] = seen ? x[e] : -INFINITY;
         }
       }
+      if (NT == 1 && a.scores && t.row0 + r < t.rows) {
+        float *to = a.scores + ((int64_t)(t.s.start + (t.row0 + r) / G) * a.nq + kvh * G + (t.row0 + r) % G) * a.scores_ld + kt + 4 * g;
+        *(floatx4 *)to = floatx4{x[0], x[1], x[2], x[3]};
+        *(floatx4 *)(to + 16) = floatx4{x[4], x[5], x[6], x[7]};
+      }
       uint32_t dark = 0;  // hidden among this lane's eight
       float top = x[0];
 #pragma unroll
@@ -440,22 +445,45 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
   const int64_t head = a.layer * a.c.layer_stride + kvh * a.c.head_stride;
   const char *kb = a.c.k + head * 2, *vb = a.c.v + head * 2;
 
-  // this thread's items of a tile: 16 bytes of row (tid + 256 i) / CH
+  // this thread's items of a tile: 16 bytes of row (tid + 256 i) / CH.  Where a wave's rows of one i (64 / CH neighbours) lie in one
+  // page its address is a scalar, and the page's number is loaded a step before the rows.
+  constexpr int NEAR = 64 / CH;
   const int my_row = tid / CH, my_col = tid % CH;
+  const bool one_page = (1 << a.c.page_shift) >= NEAR && a.c.slot_stride < (1 << 24);
+  const uint32_t lane_at = one_page ? (uint32_t)(lane / CH) * (uint32_t)a.c.slot_stride * 2 + my_col * 16 : 0;
   bool lost = false;
   u32x4 kr[LPT], vr[LPT];
+  int ahead[LPT];
+  auto first_of = [&](int kt, int i) { return min(kt + wave * NEAR + i * (256 / CH), (k1 - 1) & ~(NEAR - 1)); };
+  auto look = [&](int kt) {
+    if (one_page) {
+#pragma unroll
+      for (int i = 0; i < LPT; ++i) ahead[i] = a.c.table[(int64_t)t.b * a.c.max_pages + (first_of(kt, i) >> a.c.page_shift)];
+    }
+  };
   auto load = [&](int kt) {
 #pragma unroll
     for (int i = 0; i < LPT; ++i) {
-      const int slot = min(kt + my_row + i * (256 / CH), k1 - 1);
-      int page = page_of(a.c, t.b, slot);
-      if (page < 0) {
-        lost = true;
-        page = 0;
+      if (one_page) {
+        int page = __builtin_amdgcn_readfirstlane(ahead[i]);
+        if ((unsigned)page >= (unsigned)a.c.n_pages) {
+          lost = true;
+          page = 0;
+        }
+        const int64_t at = slot_offset(a.c, page, first_of(kt, i)) * 2;
+        kr[i] = *(const u32x4 *)(kb + at + lane_at);
+        vr[i] = *(const u32x4 *)(vb + at + lane_at);
+      } else {
+        const int slot = min(kt + my_row + i * (256 / CH), k1 - 1);
+        int page = page_of(a.c, t.b, slot);
+        if (page < 0) {
+          lost = true;
+          page = 0;
+        }
+        const int64_t at = slot_offset(a.c, page, slot) * 2 + my_col * 16;
+        kr[i] = *(const u32x4 *)(kb + at);
+        vr[i] = *(const u32x4 *)(vb + at);
       }
-      const int64_t at = slot_offset(a.c, page, slot) * 2 + my_col * 16;
-      kr[i] = *(const u32x4 *)(kb + at);
-      vr[i] = *(const u32x4 *)(vb + at);
     }
   };
   auto swz_k = [](int x) { return CH == 16 ? x & 15 : (x >> 1) & 7; };
@@ -498,13 +526,16 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
   const int k_at = r * RB + (h ^ swz_k(r)) * 16;  // item 2 st + h: with the bits of st
   const int v_i = lane & 15, v_x = 4 * h + v_i / 4, v_half = (lane >> 4) & 1;
 
+  look(k0);
   load(k0);
+  look(k0 + kChunkStep);
   store(k0, 0);
   __syncthreads();
   int buf = 0;
   for (int kt = k0; kt < k1; kt += kChunkStep, buf ^= 1) {
     const bool more = kt + kChunkStep < k1;
     if (more) load(kt + kChunkStep);
+    look(kt + 2 * kChunkStep);
     floatx16 s[2];
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
@@ -671,6 +702,38 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, i
   if (lane == 0 && a.lse) a.lse[at] = (top + log2f(sum)) * kLn2;
 }
 
+// weights[slot] += the sum of p over the rows of a sequence's kv head, at most 16, whose scores (base 2) the attention left: four
+// slots a thread.  Bound by their bytes, a few hundredths of k's, which the kernel below would read again.
+__global__ __launch_bounds__(256) void paged_weights_of_scores_kernel(PagedAttnArgs a, int slabs) {
+  const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv / slabs;
+  const int slot = (blockIdx.x / a.c.n_kv % slabs * 256 + threadIdx.x) * 4;
+  SeqRange s;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || slot >= s.len) return;
+  const int G = a.nq / a.c.n_kv;
+  floatx4 sum{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < s.n; ++i)
+    for (int h = 0; h < G; ++h) {
+      const int64_t row = (int64_t)(s.start + i) * a.nq + kvh * G + h;
+      const float ls = a.lse[row] * kLog2e;
+      const floatx4 x = *(const floatx4 *)(a.scores + row * a.scores_ld + slot);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += ls == -INFINITY ? 0.f : fast_exp2(x[e] - ls);
+    }
+  if (a.c.page_shift >= 2 && slot + 4 <= s.len) {
+    const int page = page_of(a.c, b, slot);
+    if (page < 0) return;
+    floatx4 *w = (floatx4 *)(a.c.weights + weight_offset(a.c, a.layer, page, kvh, slot));
+    *w += sum;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (slot + e >= s.len) break;
+      const int page = page_of(a.c, b, slot + e);
+      if (page >= 0) a.c.weights[weight_offset(a.c, a.layer, page, kvh, slot + e)] += sum[e];
+    }
+  }
+}
+
 // weights[slot] += the sum over the call's rows of p: a wave has 32 slots of one kv head and goes over every row that may
 // see them, in order (so the sum is the same every time).
 template <typename T, int DH, bool MASKED>
@@ -735,11 +798,15 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
-PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv, int max_new, int max_len) {
+PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv, int max_new, int max_len, bool accumulate) {
   const int G = nq / n_kv;
   PagedAttnPlan p;
   p.rows = (long)max_new * G <= 16 ? 16 : (bf16 && (long)max_new * G > 32 ? kChunkRows : 32);
   p.tiles = (long)tokens * G / p.rows + (tokens < batch ? tokens : batch);
+  // Weights of few rows are summed from their scores (64 sequences of 8700 slots and 32 heads: 34 us for what takes 335 from q
+  // and k), as long as those take at most 1 GB
+  p.scores_ld = ((long)max_len + 31) / 32 * 32;
+  if (!accumulate || p.rows != 16 || (double)p.scores_ld * tokens * nq * 4 > 1e9) p.scores_ld = 0;
   // runs of whole 128 slots, as many as give each CU a few workgroups
   const long groups = p.tiles * n_kv;
   const long want = groups >= 1024 ? 1 : (1024 + groups - 1) / groups;
@@ -759,7 +826,10 @@ static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t 
   else if (p.rows == 32) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED>), grid, block, 0, st, a, p.splits, p.run);
   if (p.splits > 1)
     hipLaunchKernelGGL((paged_attn_join_kernel<T, DH>), dim3((unsigned)(((long)a.tokens * a.nq + 3) / 4)), dim3(256), 0, st, a, p.rows, p.run);
-  if (a.accumulate) {
+  if (a.accumulate && a.scores) {
+    const int slabs = (a.max_len + 1023) / 1024;
+    hipLaunchKernelGGL(paged_weights_of_scores_kernel, dim3((unsigned)((long)slabs * a.c.batch * a.c.n_kv)), block, 0, st, a, slabs);
+  } else if (a.accumulate) {
     const int slabs = (a.max_len + kPaWaves * kPaStep - 1) / (kPaWaves * kPaStep);
     hipLaunchKernelGGL((paged_weights_kernel<T, DH, MASKED>), dim3((unsigned)((long)slabs * a.c.batch * a.c.n_kv)), block, 0, st, a, slabs);
   }

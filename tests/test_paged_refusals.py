@@ -31,7 +31,7 @@ CACHE = [(dict(k=None), INV), (dict(v=None), INV), (dict(page_table=None), INV),
          (dict(n_kv_heads=0), INV), (dict(batch=0), INV), (dict(max_pages=0), INV), (dict(dtype=2), INV), (dict(page_size=0), UNS),
          (dict(page_size=24), UNS), (dict(page_size=131072), UNS), (dict(max_pages=1 << 26), UNS), (dict(head_dim=96), UNS),
          (dict(page_stride=63), INV), (dict(slot_stride=132), INV), (dict(head_stride=0), INV), (dict(layer_stride=-8), INV),
-         (dict(k=P + 8), INV), (dict(v=P + 2), INV), (dict(weights=P + 1), INV)]
+         (dict(k=P + 8), INV), (dict(v=P + 2), INV), (dict(weights=P + 4), INV)]
 
 
 def call(name, args, c=None, **kw):
