@@ -1510,14 +1510,14 @@ domino_status paged_attn_layout(const domino_paged_cache *c, int32_t tokens, int
                            accumulate != 0);
   const int64_t slabs = accumulate ? (int64_t)c->batch * c->n_kv_heads * ((max_len + 127) / 128) : 0;
   if ((double)w.plan.tiles * w.plan.splits * c->n_kv_heads > kMaxBlocks || slabs > kMaxBlocks ||
-      (int64_t)tokens * n_q_heads / 4 + 1 > kMaxBlocks)
+      (w.plan.splits > 1 && (int64_t)tokens * n_q_heads > kMaxBlocks))
     return fail(DOMINO_ERR_UNSUPPORTED, "the call's work does not fit a launch");
   const size_t rows = (size_t)tokens * n_q_heads;
   w.lse = 256;
   w.ml = w.lse + (accumulate ? align_up(rows * 4) : 0);
   w.o = w.ml + (w.plan.splits > 1 ? align_up(rows * w.plan.splits * 8) : 0);
   w.scores = w.o + (w.plan.splits > 1 ? align_up(rows * w.plan.splits * c->head_dim * 4) : 0);
-  w.bytes = w.scores + align_up(rows * w.plan.scores_ld * 4);
+  w.bytes = w.scores + align_up((size_t)w.plan.scores_steps * w.plan.scores_rows * 128 * c->batch * c->n_kv_heads);
   return DOMINO_OK;
 }
 domino_status check_evict(const domino_paged_cache *c, int32_t max_len, int32_t budget) {
@@ -1653,8 +1653,9 @@ domino_status domino_paged_attention(const domino_paged_cache *cache, int32_t la
   a.lse = lse ? lse : (accumulate ? (float *)(ws + w.lse) : nullptr);
   a.part_ml = w.plan.splits > 1 ? (float *)(ws + w.ml) : nullptr;
   a.part_o = w.plan.splits > 1 ? (float *)(ws + w.o) : nullptr;
-  a.scores = w.plan.scores_ld ? (float *)(ws + w.scores) : nullptr;
-  a.scores_ld = w.plan.scores_ld;
+  a.scores = w.plan.scores_steps ? (float *)(ws + w.scores) : nullptr;
+  a.scores_steps = w.plan.scores_steps;
+  a.scores_rows = w.plan.scores_rows;
   a.accumulate = accumulate != 0;
   a.err = (int32_t *)workspace;
   launch_paged_attn(a, w.plan, (hipStream_t)stream);

@@ -392,8 +392,8 @@ struct PagedAttnArgs {
   float *lse;        // [tokens][nq] or null (needed with accumulate)
   float *part_o;     // [splits][tokens][nq][dh], null: one split
   float *part_ml;    // [splits][tokens][nq][2]: maximum (base 2) and sum
-  float *scores;     // [tokens][nq][scores_ld] base-2 scores, where the weights come from them
-  int64_t scores_ld;
+  float *scores;     // [batch][n_kv][scores_steps][scores_rows][32] base-2 scores, where the weights come from them
+  int scores_steps, scores_rows;
   int accumulate;
   int32_t *err;
 };
@@ -402,7 +402,7 @@ struct PagedAttnPlan {
   int rows;        // query rows (new tokens x query heads of a kv head) of a workgroup's tile
   long tiles;      // tiles that hold rows, at most
   int splits, run; // a sequence's slots are cut into runs of `run`
-  long scores_ld;  // 0: no scores are kept
+  int scores_steps, scores_rows;  // steps 0: no scores are kept
 };
 PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv, int max_new, int max_len,
                               bool accumulate);

@@ -1,6 +1,9 @@
 // Attention of new tokens over a cache of pages, and the weights that it gives to every slot.
 //   o_r = sum_s p_rs v_s,  p_rs = exp(scale q_r k_s - lse_r) over the slots s that row r sees
 // Rows are the new tokens of a sequence times the query heads of one kv head: row i G + h.
+#include <algorithm>
+#include <type_traits>
+
 #include "mfma.h"
 #include "paged.h"
 
@@ -139,6 +142,7 @@ template <int DH> struct Ops<float, DH> {
   }
   // v: item n = (slot 16 tt + 4 g + e, 64 columns jj) as n = (tt * 4 + e) * (DH / 64) + jj: four columns 64 jj + 4 r
   static constexpr int JJ = DH / 64;
+  DEVI static int v_col(int lane) { return (lane & 15) * 16; }
   DEVI static int v_row(int n, int lane) { return 16 * (n / JJ / 4) + 4 * (lane >> 4) + n / JJ % 4; }
   DEVI static uint32_t take_odd(u32x4 (&v)[VN], int lane) {
     uint32_t odd = 0;
@@ -203,11 +207,16 @@ DEVI void add_odd(const char *row, int slot, const float (&p)[8], uint32_t dark,
     }
 }
 
+// Where the scores (base 2) of 32 slots and a row of a sequence's kv head are kept: step by step, the rows' 128 bytes side by side.
+DEVI float *scores_at(const PagedAttnArgs &a, int b, int kvh, int slot, int row) {
+  return a.scores + (((int64_t)(b * a.c.n_kv + kvh) * a.scores_steps + slot / 32) * a.scores_rows + row) * 32;
+}
+
 constexpr int kPaThreads = 256, kPaWaves = 4, kPaStep = 32;
 
 // A workgroup has a tile of 16 NT rows and a run of slots, a wave every fourth 32 slots of it; the waves' results are
 // joined in LDS.  Bound by the cache's bytes where rows are few.
-template <typename T, int DH, int NT, bool MASKED>
+template <typename T, int DH, int NT, bool MASKED, bool ONE_PAGE>
 __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a, int splits, int run) {
   using O = Ops<T, DH>;
   constexpr int M = 16 * NT, ESZ = sizeof(T);
@@ -250,33 +259,85 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
   const char *kb = a.c.k + (a.layer * a.c.layer_stride + kvh * a.c.head_stride) * ESZ;
   const char *vb = a.c.v + (a.layer * a.c.layer_stride + kvh * a.c.head_stride) * ESZ;
   char *mylds = lds + wave * O::LDSBYTES;
+  // A step's rows: ONE_PAGE, its 32 slots lie in one page (page_size >= 32), their address is a scalar and a lane's offset in the page
+  // the same every step; else every lane looks up one slot and takes its rows' pages from the others.  The page's number is loaded
+  // a step before the rows (and ahead of that step's: loads return in order), k's rows once the scores have used the last ones, v's once those are in LDS (or used): a wave has
+  // one step's rows on their way all the time.
+  const int near_k = r * (int)a.c.slot_stride * ESZ;
+  int page = 0;
   bool lost = false;
-
-  for (int kt = k0 + wave * kPaStep; kt < k1; kt += kPaWaves * kPaStep) {
-    // lane x's slot kt + x % 32: its page, and so every lane's rows'
-    int page = page_of(a.c, t.b, min(kt + (lane & 31), k1 - 1));
-    if (page < 0) {
-      lost = true;
-      page = 0;
+  auto look = [&](int kt) {
+    const int slot = ONE_PAGE ? kt : kt + (lane & 31);
+    return a.c.table[(int64_t)t.b * a.c.max_pages + (min(slot, k1 - 1) >> a.c.page_shift)];
+  };
+  auto settle = [&](int p) {
+    if (ONE_PAGE) p = __builtin_amdgcn_readfirstlane(p);
+    if ((unsigned)p < (unsigned)a.c.n_pages) return p;
+    lost = true;
+    return 0;
+  };
+  auto row_at = [&](const char *base, int kt, int x) {
+    return base + slot_offset(a.c, __shfl(page, x, 64), min(kt + x, k1 - 1)) * ESZ;
+  };
+  u32x4 k[2][O::KST], v[O::VN];
+  auto load_k = [&](int kt) {
+    if constexpr (ONE_PAGE) {
+      const char *p = kb + slot_offset(a.c, page, kt) * ESZ;
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int st = 0; st < O::KST; ++st) k[tt][st] = O::row_frag(p + tt * 16 * a.c.slot_stride * ESZ + near_k, st, g);
+    } else {
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const char *p = row_at(kb, kt, 16 * tt + r);
+#pragma unroll
+        for (int st = 0; st < O::KST; ++st) k[tt][st] = O::row_frag(p, st, g);
+      }
     }
-    auto row_at = [&](const char *base, int x) {
-      return base + slot_offset(a.c, __shfl(page, x, 64), min(kt + x, k1 - 1)) * ESZ;
-    };
-    u32x4 k[2][O::KST], v[O::VN];
+  };
+  auto load_v = [&](int kt) {
+    if constexpr (ONE_PAGE) {
+      const char *p = vb + slot_offset(a.c, page, kt) * ESZ;
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const char *p = row_at(kb, 16 * tt + r);
+      for (int n = 0; n < O::VN; ++n) {
+        const int col = ESZ == 2 ? O::v_col(lane) : O::v_col(lane) + n % (DH / 64) * 256;
+        // (a lane's row: that of item 0, and the same distance further for all lanes)
+        v[n] = *(const u32x4 *)(p + (O::v_row(n, lane) - O::v_row(0, lane)) * a.c.slot_stride * ESZ +
+                                (O::v_row(0, lane) * (int)a.c.slot_stride * ESZ + col));
+      }
+    } else {
 #pragma unroll
-      for (int st = 0; st < O::KST; ++st) k[tt][st] = O::row_frag(p, st, g);
+      for (int n = 0; n < O::VN; ++n) {
+        const int col = ESZ == 2 ? O::v_col(lane) : O::v_col(lane) + n % (DH / 64) * 256;
+        v[n] = *(const u32x4 *)(row_at(vb, kt, O::v_row(n, lane)) + col);
+      }
+    }
+  };
+  constexpr int STRIDE = kPaWaves * kPaStep;
+  int kt = k0 + wave * kPaStep, ahead = 0;
+  if (kt < k1) {
+    page = settle(look(kt));
+    ahead = look(kt + STRIDE);
+    load_k(kt);
+    load_v(kt);
+  }
+  auto step = [&](auto next) {  // next: loads for the step after this one go out
+    constexpr bool more = decltype(next)::value;
+    const int page_now = page;
+    float sx[NT][8];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) score8<T, DH>(k, q[nt], sx[nt]);
+    if (more) {
+      page = settle(ahead);
+      ahead = look(kt + 2 * STRIDE);
+      load_k(kt + STRIDE);
     }
     // rows past the run's end are zeros: a weight of 0 times what lies there might be NaN
+    if (kt + kPaStep > k1) {
 #pragma unroll
-    for (int n = 0; n < O::VN; ++n) {
-      const int x = O::v_row(n, lane);
-      const char *p = row_at(vb, x);
-      if constexpr (ESZ == 2) v[n] = *(const u32x4 *)(p + O::v_col(lane));
-      else v[n] = *(const u32x4 *)(p + (64 * (n % O::JJ) + 4 * r) * 4);
-      if (kt + x >= k1) v[n] = u32x4{0, 0, 0, 0};
+      for (int n = 0; n < O::VN; ++n)
+        if (kt + O::v_row(n, lane) >= k1) v[n] = u32x4{0, 0, 0, 0};
     }
     const bool whole = kt + kPaStep <= min(n0, k1);
     uint32_t odd = 0;  // slots of this step, some of them hidden from some row, whose v holds NaN or an infinity
@@ -285,13 +346,13 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
 #pragma unroll
       for (int n = 0; n < O::VN; ++n) *(u32x4 *)(mylds + O::v_row(n, lane) * O::LDSROW + O::v_col(lane)) = v[n];
       __builtin_amdgcn_wave_barrier();
+      if (more) load_v(kt + STRIDE);
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float x[8];
-      score8<T, DH>(k, q[nt], x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= sc;
+      for (int e = 0; e < 8; ++e) x[e] = sx[nt][e] * sc;
       if (!whole) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -303,7 +364,7 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
         }
       }
       if (NT == 1 && a.scores && t.row0 + r < t.rows) {
-        float *to = a.scores + ((int64_t)(t.s.start + (t.row0 + r) / G) * a.nq + kvh * G + (t.row0 + r) % G) * a.scores_ld + kt + 4 * g;
+        float *to = scores_at(a, t.b, kvh, kt, r) + 4 * g;
         *(floatx4 *)to = floatx4{x[0], x[1], x[2], x[3]};
         *(floatx4 *)(to + 16) = floatx4{x[4], x[5], x[6], x[7]};
       }
@@ -335,11 +396,14 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
 #pragma unroll 1
         for (int e = 0; e < 32; ++e)
           if (odd >> e & 1)
-            add_odd<T, DH>(vb + slot_offset(a.c, __builtin_amdgcn_readlane(page, e), kt + e) * ESZ, e, x, dark, o[nt], lane);
+            add_odd<T, DH>(vb + slot_offset(a.c, __builtin_amdgcn_readlane(page_now, e), kt + e) * ESZ, e, x, dark, o[nt], lane);
       }
     }
     if constexpr (ESZ == 2) __builtin_amdgcn_wave_barrier();
-  }
+    else if (more) load_v(kt + STRIDE);
+  };
+  for (; kt + STRIDE < k1; kt += STRIDE) step(std::true_type{});
+  if (kt < k1) step(std::false_type{});
   if (lost) raise_error(a.err, DEV_BAD_PAGE);
 
   // the waves' maxima and sums, then their rows 16 at a time
@@ -662,12 +726,14 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
   }
 }
 
-// Joins the runs of one row (a new token's query head), a wave a row.
-template <typename T, int DH>
+// Joins the runs of one row (a new token's query head): a wave takes every W-th run, eight at a time, and the row's W waves'
+// sums meet in LDS.  One wave a row up to eight runs, which is one round trip; four above.
+template <typename T, int DH, int W>
 __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, int M, int run) {
-  const int lane = threadIdx.x & 63;
-  const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= (long)a.tokens * a.nq) return;
+  constexpr int E = DH / 64, U = 8;
+  const int lane = threadIdx.x & 63, unit = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = unit % W;
+  const int64_t at = (int64_t)blockIdx.x * (4 / W) + unit / W;
+  if (at >= (int64_t)a.tokens * a.nq) return;
   const int tok = (int)(at / a.nq), head = (int)(at % a.nq), G = a.nq / a.c.n_kv;
   int b = 0;
   for (int s0 = 0; s0 < a.c.batch; s0 += 64) b += __popcll(__ballot(s0 + lane < a.c.batch && a.starts[s0 + lane + 1] <= tok));
@@ -677,28 +743,67 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, i
   const int row = (tok - s.start) * G + head % G, last = (min((row / M + 1) * M, s.n * G) - 1) / G;
   const int vis = a.mask ? s.len : s.len - s.n + last + 1, runs = (vis + run - 1) / run;
   const int64_t step = (int64_t)a.tokens * a.nq;
-  // a lane's runs as one (maximum, sum), then over the lanes
-  float m = -INFINITY, l = 0.f;
-  for (int x = lane; x < runs; x += 64) {
-    const float2 v = *(const float2 *)(a.part_ml + (at + x * step) * 2);
-    const float mn = fmaxf(m, v.x), ms = mn == -INFINITY ? 0.f : mn;
-    l = l * fast_exp2(m - ms) + v.y * fast_exp2(v.x - ms);
-    m = mn;
-  }
-  const float top = wave_max(m), ms = top == -INFINITY ? 0.f : top;
-  const float sum = wave_sum(l * fast_exp2(m - ms));
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  constexpr int E = DH / 64;
-  float y[E] = {};
-  for (int x = 0; x < runs; ++x) {
-    const float f = fast_exp2(a.part_ml[(at + x * step) * 2] - ms) * inv;
-    const float *p = a.part_o + (at + x * step) * DH + lane * E;
+  const float *po = a.part_o + at * DH + lane * E, *pm = a.part_ml + at * 2;
+  float m = -INFINITY, l = 0.f, y[E] = {};
+  for (int x0 = wave; x0 < runs; x0 += W * U) {
+    float2 ml[U];
+    float v[U][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) y[e] += p[e] * f;
+    for (int u = 0; u < U; ++u) {
+      const int64_t x = min(x0 + W * u, runs - 1);
+      ml[u] = *(const float2 *)(pm + x * step * 2);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[u][e] = po[x * step * DH + e];
+    }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (x0 + W * u >= runs) ml[u].x = -INFINITY;
+      top = fmaxf(top, ml[u].x);
+    }
+    const float ms = top == -INFINITY ? 0.f : top, f0 = fast_exp2(m - ms);
+    m = top;
+    l *= f0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] *= f0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (x0 + W * u >= runs) break;  // wave-uniform
+      const float f = fast_exp2(ml[u].x - ms);
+      l += ml[u].y * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] += v[u][e] * f;
+    }
   }
+  float sum = l, top = m;
+  if constexpr (W > 1) {
+    __shared__ float s_m[W], s_l[W], s_y[W][DH];
+    if (lane == 0) {
+      s_m[wave] = m;
+      s_l[wave] = l;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_y[wave][lane * E + e] = y[e];
+    __syncthreads();
+    if (wave != 0) return;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 1; w < W; ++w) top = fmaxf(top, s_m[w]);
+    const float ms = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = fast_exp2(s_m[w] - ms);
+      sum += s_l[w] * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] += s_y[w][lane * E + e] * f;
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T *dst = (T *)a.out + (int64_t)tok * a.o_stride + (int64_t)head * DH + lane * E;
 #pragma unroll
-  for (int e = 0; e < E; ++e) store_as(dst + e, y[e]);
+  for (int e = 0; e < E; ++e) store_as(dst + e, y[e] * inv);
   if (lane == 0 && a.lse) a.lse[at] = (top + log2f(sum)) * kLn2;
 }
 
@@ -715,7 +820,7 @@ __global__ __launch_bounds__(256) void paged_weights_of_scores_kernel(PagedAttnA
     for (int h = 0; h < G; ++h) {
       const int64_t row = (int64_t)(s.start + i) * a.nq + kvh * G + h;
       const float ls = a.lse[row] * kLog2e;
-      const floatx4 x = *(const floatx4 *)(a.scores + row * a.scores_ld + slot);
+      const floatx4 x = *(const floatx4 *)(scores_at(a, b, kvh, slot, i * G + h) + slot % 32);
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] += ls == -INFINITY ? 0.f : fast_exp2(x[e] - ls);
     }
@@ -802,16 +907,22 @@ PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv
   const int G = nq / n_kv;
   PagedAttnPlan p;
   p.rows = (long)max_new * G <= 16 ? 16 : (bf16 && (long)max_new * G > 32 ? kChunkRows : 32);
-  p.tiles = (long)tokens * G / p.rows + (tokens < batch ? tokens : batch);
+  // tiles of rows: at most one part-filled for each sequence, and no more than every sequence's longest
+  const long busy = tokens < batch ? tokens : batch;
+  p.tiles = std::min((long)tokens * G / p.rows + busy, busy * (((long)max_new * G + p.rows - 1) / p.rows));
   // Weights of few rows are summed from their scores (64 sequences of 8700 slots and 32 heads: 34 us for what takes 335 from q
   // and k), as long as those take at most 1 GB
-  p.scores_ld = ((long)max_len + 31) / 32 * 32;
-  if (!accumulate || p.rows != 16 || (double)p.scores_ld * tokens * nq * 4 > 1e9) p.scores_ld = 0;
-  // runs of whole 128 slots, as many as give each CU a few workgroups
+  p.scores_rows = max_new * G;
+  p.scores_steps = (max_len + 31) / 32;
+  if (!accumulate || p.rows != 16 || (double)p.scores_steps * 128 * p.scores_rows * batch * n_kv > 1e9) p.scores_steps = 0;
+  // Runs of whole 128 slots, as few as give each CU two workgroups (one sequence of 8192 slots 17.8 us, 22.8 with runs of
+  // 128; 64 of 1000 54 us, 65 with 128).  With few rows runs of more than 1024 are cut further, so that sequences of different
+  // lengths end together (64 of 4096 to 16385 slots, weights and all: 622 us, 681 in runs of 8320).
   const long groups = p.tiles * n_kv;
-  const long want = groups >= 1024 ? 1 : (1024 + groups - 1) / groups;
   const int pieces = (int)(((long)max_len + 127) / 128);
-  const int splits = (int)(want < pieces ? want : pieces);
+  long want = (511 + groups) / groups;
+  if (p.rows == 16) want = std::max(want, std::min((8191 + groups) / groups, (long)max_len / 1024));
+  const int splits = (int)std::min(want, (long)std::min(pieces, 128));
   p.run = (pieces + splits - 1) / splits * 128;
   p.splits = (int)(((long)max_len + p.run - 1) / p.run);
   return p;
@@ -822,10 +933,15 @@ static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t 
   const dim3 grid((unsigned)(p.tiles * p.splits * a.c.n_kv)), block(kPaThreads);
   if constexpr (sizeof(T) == 2)
     if (p.rows == kChunkRows) hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED>), grid, block, 0, st, a, p.splits, p.run);
-  if (p.rows == 16) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 1, MASKED>), grid, block, 0, st, a, p.splits, p.run);
-  else if (p.rows == 32) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED>), grid, block, 0, st, a, p.splits, p.run);
-  if (p.splits > 1)
-    hipLaunchKernelGGL((paged_attn_join_kernel<T, DH>), dim3((unsigned)(((long)a.tokens * a.nq + 3) / 4)), dim3(256), 0, st, a, p.rows, p.run);
+  const bool one_page = a.c.page_shift >= 5 && a.c.slot_stride < (1 << 24);
+  if (p.rows == 16 && one_page) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 1, MASKED, true>), grid, block, 0, st, a, p.splits, p.run);
+  else if (p.rows == 16) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 1, MASKED, false>), grid, block, 0, st, a, p.splits, p.run);
+  else if (p.rows == 32 && one_page) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, true>), grid, block, 0, st, a, p.splits, p.run);
+  else if (p.rows == 32) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, false>), grid, block, 0, st, a, p.splits, p.run);
+  if (p.splits > 8)
+    hipLaunchKernelGGL((paged_attn_join_kernel<T, DH, 4>), dim3((unsigned)((long)a.tokens * a.nq)), block, 0, st, a, p.rows, p.run);
+  else if (p.splits > 1)
+    hipLaunchKernelGGL((paged_attn_join_kernel<T, DH, 1>), dim3((unsigned)(((long)a.tokens * a.nq + 3) / 4)), block, 0, st, a, p.rows, p.run);
   if (a.accumulate && a.scores) {
     const int slabs = (a.max_len + 1023) / 1024;
     hipLaunchKernelGGL(paged_weights_of_scores_kernel, dim3((unsigned)((long)slabs * a.c.batch * a.c.n_kv)), block, 0, st, a, slabs);
