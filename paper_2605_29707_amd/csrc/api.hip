@@ -1526,9 +1526,24 @@ domino_status check_evict(const domino_paged_cache *c, int32_t max_len, int32_t 
   if (budget < 1 || max_len < 1) return fail(DOMINO_ERR_INVALID_ARG, "budget and max_len must be >= 1");
   if (max_len > c->max_pages * c->page_size) return fail(DOMINO_ERR_INVALID_ARG, "max_len must be at most max_pages * page_size");
   const int64_t heads = (int64_t)c->n_layers * c->batch * c->n_kv_heads;
+  if ((double)heads * ((max_len + kEvictSlice - 1) / kEvictSlice) > kMaxBlocks / 4)
+    return fail(DOMINO_ERR_UNSUPPORTED, "n_layers * batch * n_kv_heads * max_len does not fit a launch");
   if (budget > (1 << 21) || heads > (1 << 20) || heads * ((std::min(budget, max_len) + kEvictMoveRows - 1) / kEvictMoveRows) > kMaxBlocks)
     return fail(DOMINO_ERR_UNSUPPORTED, "budget must be at most 2^21, n_layers * batch * n_kv_heads at most 2^20 and 2^30 / min(budget, max_len)");
   return DOMINO_OK;
+}
+struct PagedEvictLayout {
+  size_t kept, state, sums, parts, bytes;
+};
+PagedEvictLayout paged_evict_layout(const domino_paged_cache *c, int32_t max_len, int32_t budget) {
+  const size_t heads = (size_t)c->n_layers * c->batch * c->n_kv_heads, slices = (max_len + kEvictSlice - 1) / kEvictSlice;
+  PagedEvictLayout w;
+  w.kept = 256;
+  w.state = w.kept + align_up(heads * budget * 4);
+  w.sums = w.state + (slices > 1 ? align_up(heads * 2 * 8) : 0);
+  w.parts = w.sums + (slices > 1 ? align_up(heads * slices * 4) : 0);
+  w.bytes = w.parts + (slices > 1 ? 2 * heads * slices * 2048 * 4 : 0);
+  return w;
 }
 }  // namespace
 
@@ -1666,7 +1681,7 @@ domino_status domino_paged_attention(const domino_paged_cache *cache, int32_t la
 
 size_t domino_paged_evict_workspace_bytes(const domino_paged_cache *cache, int32_t max_len, int32_t budget) {
   if (check_evict(cache, max_len, budget) != DOMINO_OK) return 0;
-  return 256 + (size_t)cache->n_layers * cache->batch * cache->n_kv_heads * budget * 4;
+  return paged_evict_layout(cache, max_len, budget).bytes;
 }
 
 domino_status domino_paged_evict(const domino_paged_cache *cache, const int32_t *kv_lens, int32_t *new_lens, int32_t max_len,
@@ -1689,7 +1704,11 @@ domino_status domino_paged_evict(const domino_paged_cache *cache, const int32_t 
   a.recent = recent;
   a.new_table = new_table;
   a.new_pages = new_pages;
-  a.kept = kept ? kept : (int32_t *)((char *)workspace + 256);
+  const PagedEvictLayout w = paged_evict_layout(cache, max_len, budget);
+  a.kept = kept ? kept : (int32_t *)((char *)workspace + w.kept);
+  a.state = (uint2 *)((char *)workspace + w.state);
+  a.sums = (uint32_t *)((char *)workspace + w.sums);
+  a.parts = (uint32_t *)((char *)workspace + w.parts);
   a.err = (int32_t *)workspace;
   launch_paged_evict(a, (hipStream_t)stream);
   hipError_t he = hipGetLastError();

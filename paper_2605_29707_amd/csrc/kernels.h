@@ -374,8 +374,11 @@ struct PagedEvictArgs {
   const int32_t *new_table;  // null: in place
   int new_pages;             // entries a row of new_table
   int32_t *kept;             // [layers][batch][n_kv][budget]
+  uint2 *state;              // where a sequence may have more slots than a slice: [heads][2]
+  uint32_t *sums, *parts;    // [heads][slices], [2][heads][slices][2048]
   int32_t *err;
 };
+constexpr int kEvictSlice = 16384;  // slots of a head that one workgroup chooses from
 constexpr int kEvictMoveRows = 64;  // rows of a head that a workgroup moves to new pages
 void launch_paged_evict(const PagedEvictArgs &a, hipStream_t st);
 

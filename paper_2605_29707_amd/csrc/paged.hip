@@ -235,188 +235,309 @@ DEVI uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+// Which slots of one (layer, sequence, head) stay, in order: the first `sink`, the last `recent`, and the m of greatest weight
+// between them.  A workgroup has a slice of 16384 slots, a wave 1024 of them, whose keys it keeps in registers (16 a lane).  The m-th
+// greatest key is found by three counts over its digits (11, 11 and 10 bits): kept are the keys above it and the first `need` that
+// equal it.  Then every wave counts the kept slots of its stretch, and writes them behind those of the waves before it.
+//   one slice    one launch: bound by the chain of its steps (1100 slots 13 us, 16000 21)
+//   more slices  a launch for each count and one that writes; a slice's counts are its own, and the next launch adds them up.
+//                (100003 slots of 16 heads in one workgroup each took 125 us: bound by its instructions)
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
-constexpr int kSelStep = 256, kSelBatch = 4;  // slots of a wave's step (four neighbours a lane), steps whose loads are out together
+constexpr int kSelStep = 256, kSelSteps = 4;  // slots of a wave's step (four neighbours a lane), steps of a wave's stretch
+constexpr int kSelWave = kSelStep * kSelSteps;
+static_assert(kSelWaves * kSelWave == kEvictSlice, "a slice is what a workgroup's registers hold");
 
-// Which slots of one (layer, sequence, head) stay, in order: the first `sink`, the last `recent`, and the m of greatest
-// weight between them.  A wave has a stretch of the slots.  The m-th greatest key is found by three counts over its digits (11, 11
-// and 10 bits); then every wave counts the kept slots of its stretch, and writes them behind those of the waves before it.  Up to
-// 16384 slots the keys stay in registers, else every one of the five passes reads the weights again (from the L2).
-__global__ __launch_bounds__(kSelThreads) void paged_evict_select_kernel(PagedEvictArgs a) {
+// A workgroup's slice of one head: its wave's stretch [w0, w1) of the n slots, those of [first, last) with a choice.
+struct Slice {
+  int n, first, last, m, w0, w1;
+  bool lost;
+  uint32_t key[kSelSteps][4];  // of slots w0 + x * kSelStep + lane * 4 + e
+};
+
+template <bool TINY_PAGES>
+DEVI void slice_load(const PagedEvictArgs &a, int b, int layer, int head, int slice, int n, Slice &s) {
   const PagedView &c = a.c;
-  const int head = blockIdx.x % c.n_kv, b = (blockIdx.x / c.n_kv) % c.batch, layer = blockIdx.x / c.n_kv / c.batch;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool lead = layer == 0 && head == 0 && tid == 0;
-  int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
-  const int n = a.lens[b];
-  if (n < 0 || n > a.max_len) {
-    if (lead) raise_error(a.err, DEV_BAD_CTX_LEN);
-    if (lead) a.new_lens[b] = n;
-    for (int i = tid; i < a.budget; i += kSelThreads) kept[i] = -1;
-    return;
-  }
-  if (n <= a.budget) {
-    if (lead) a.new_lens[b] = n;
-    for (int i = tid; i < a.budget; i += kSelThreads) kept[i] = i < n ? i : -1;
-    return;
-  }
-  if (lead) a.new_lens[b] = a.budget;
-  const int first = a.sink, last = n - a.recent, m = a.budget - a.sink - a.recent;
-  __shared__ uint32_t hist[2048];
-  __shared__ uint32_t wsum[kSelWaves], wtie[kSelWaves];
-  __shared__ uint32_t s_bin, s_above;
-  bool lost = false;
-  // a wave's stretch: whole steps, so that a lane's four neighbours lie in one page of four slots or more
-  const int per = (n + kSelWaves * kSelStep - 1) / (kSelWaves * kSelStep) * kSelStep;
-  const int w0 = min(n, wave * per), w1 = min(n, w0 + per);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  s.n = n;
+  s.first = a.sink;
+  s.last = n - a.recent;
+  s.m = a.budget - a.sink - a.recent;
+  // (a sequence that one workgroup has alone is spread over its waves)
+  const int per = n > kEvictSlice ? kSelWave : (n + kSelWaves * kSelStep - 1) / (kSelWaves * kSelStep) * kSelStep;
+  s.w0 = min(n, slice * kEvictSlice + wave * per);
+  s.w1 = min(n, s.w0 + per);
+  s.lost = false;
+  if (s.w0 == s.w1) return;
   const float *weights = c.weights + (((int64_t)layer * c.n_pages * c.n_kv + head) << c.page_shift);
   const int64_t page_step = (int64_t)c.n_kv << c.page_shift;
   const int in_page = (1 << c.page_shift) - 1;
-  auto load = [&](int s0, uint32_t (&key)[kSelBatch][4]) {
-    int page[kSelBatch][4];
+  constexpr int PE = TINY_PAGES ? 4 : 1;  // four neighbours lie in one page of four slots or more
+  int page[kSelSteps][PE];
 #pragma unroll
-    for (int x = 0; x < kSelBatch; ++x)
+  for (int x = 0; x < kSelSteps; ++x)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int slot = min(s0 + x * kSelStep + lane * 4 + e, n - 1);
-        if (e == 0 || c.page_shift < 2) {
-          page[x][e] = page_of(c, b, slot);
-          lost |= page[x][e] < 0;
-        } else {
-          page[x][e] = page[x][0];
-        }
-      }
-    floatx4 w[kSelBatch];
+    for (int e = 0; e < PE; ++e) page[x][e] = page_of(c, b, min(s.w0 + x * kSelStep + lane * 4 + e, n - 1));
+  floatx4 w[kSelSteps];
 #pragma unroll
-    for (int x = 0; x < kSelBatch; ++x) {
-      const int slot = s0 + x * kSelStep + lane * 4;
-      if (c.page_shift >= 2) {
-        w[x] = *(const floatx4 *)(weights + max(page[x][0], 0) * page_step + (min(slot, (n - 1) & ~3) & in_page));
-      } else {
+  for (int x = 0; x < kSelSteps; ++x) {
+    const int slot = s.w0 + x * kSelStep + lane * 4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[x][e] = weights[max(page[x][e], 0) * page_step + (min(slot + e, n - 1) & in_page)];
-      }
+    for (int e = 0; e < PE; ++e) {
+      const float *at = weights + max(page[x][e], 0) * page_step;
+      if (TINY_PAGES) w[x][e] = at[min(slot + e, n - 1) & in_page];
+      else w[x] = *(const floatx4 *)(at + (min(slot, (n - 1) & ~3) & in_page));
     }
-#pragma unroll
-    for (int x = 0; x < kSelBatch; ++x)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) key[x][e] = page[x][e] < 0 ? 0 : weight_key(w[x][e]);
-  };
-  uint32_t own[kSelBatch][4];
-  const bool keep_keys = per <= kSelBatch * kSelStep;
-  if (keep_keys) load(w0, own);
-  // fn(first slot of the lane's four, their keys) for every step of the wave's stretch
-  auto each = [&](auto fn) {
-    if (keep_keys) {
-#pragma unroll
-      for (int x = 0; x < kSelBatch; ++x)
-        if (w0 + x * kSelStep < w1) fn(w0 + x * kSelStep + lane * 4, own[x]);
-    } else {
-      for (int s0 = w0; s0 < w1; s0 += kSelBatch * kSelStep) {
-        uint32_t key[kSelBatch][4];
-        load(s0, key);
-#pragma unroll
-        for (int x = 0; x < kSelBatch; ++x)
-          if (s0 + x * kSelStep < w1) fn(s0 + x * kSelStep + lane * 4, key[x]);
-      }
-    }
-  };
-  uint32_t prefix = 0, need = m;  // the wanted key's digits so far, its rank among those that share them
-  for (int pass = 0; pass < 3 && m > 0; ++pass) {
-    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < 2048; i += kSelThreads) hist[i] = 0;
-    __syncthreads();
-    each([&](int slot, const uint32_t (&key)[4]) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool in = slot + e >= first && slot + e < min(last, w1) && (pass == 0 || (key[e] >> (shift + bits)) == prefix);
-        if (in) {
-          // the first lane's bin is counted once for all that share it: most slots may hold one value
-          const uint32_t bin = (key[e] >> shift) & ((1u << bits) - 1), b0 = __builtin_amdgcn_readfirstlane(bin);
-          const uint64_t same = __ballot(bin == b0);
-          if (bin != b0) atomicAdd(&hist[bin], 1u);
-          else if (lane == __ffsll((unsigned long long)same) - 1) atomicAdd(&hist[b0], (uint32_t)__popcll(same));
-        }
-      }
-    });
-    __syncthreads();
-    // from the top bin down: the bin where the running count reaches `need`
-    if (wave == 0) {
-      uint32_t mine = 0;
-      for (int i = 0; i < 32; ++i) mine += hist[2047 - (lane * 32 + i)];
-      uint32_t incl = mine;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t v = __shfl_up(incl, o, 64);
-        if (lane >= o) incl += v;
-      }
-      uint32_t run = incl - mine;
-      if (run < need && incl >= need) {
-        for (int i = 0; i < 32; ++i) {
-          const int bin = 2047 - (lane * 32 + i);
-          const uint32_t h = hist[bin];
-          if (run < need && run + h >= need) {
-            s_bin = bin;
-            s_above = run;
-          }
-          run += h;
-        }
-      }
-    }
-    __syncthreads();
-    prefix = (prefix << bits) | s_bin;
-    need -= s_above;
   }
-  // kept: keys above `prefix`, and the first `need` slots that equal it
-  uint32_t ns = 0, nt = 0;
-  each([&](int slot, const uint32_t (&key)[4]) {
+#pragma unroll
+  for (int x = 0; x < kSelSteps; ++x)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const bool in = slot + e >= first && slot + e < last;
-      ns += __popcll(__ballot(slot + e < w1 && (!in || (m > 0 && key[e] > prefix))));
-      nt += __popcll(__ballot(slot + e < w1 && in && m > 0 && key[e] == prefix));
+      const bool known = page[x][TINY_PAGES ? e : 0] >= 0;
+      s.lost |= !known;
+      s.key[x][e] = known ? weight_key(w[x][e]) : 0;
     }
-  });
-  if (lane == 0) {
-    wsum[wave] = ns;
-    wtie[wave] = nt;
+}
+
+constexpr int digit_shift(int pass) { return pass == 0 ? 21 : (pass == 1 ? 10 : 0); }
+constexpr int digit_bits(int pass) { return pass == 2 ? 10 : 11; }
+
+// hist[d] = how many keys of the slice with a choice share `prefix` and have d for the next digit
+DEVI void slice_count(const Slice &s, int pass, uint32_t prefix, uint32_t *hist) {
+  const int lane = threadIdx.x & 63, shift = digit_shift(pass), bits = digit_bits(pass);
+  for (int i = threadIdx.x; i < 2048; i += kSelThreads) hist[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < kSelSteps; ++x) {
+    const int s0 = s.w0 + x * kSelStep;
+    if (s0 >= s.w1) break;
+    const bool inner = s0 >= s.first && s0 + kSelStep <= min(s.last, s.w1);  // wave-uniform
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int slot = s0 + lane * 4 + e;
+      bool in = pass == 0 || (s.key[x][e] >> (shift + bits)) == prefix;
+      if (!inner) in = in && slot >= s.first && slot < min(s.last, s.w1);
+      if (in) {
+        // slots that all share one digit are counted at once: most may hold one value
+        const uint32_t bin = (s.key[x][e] >> shift) & ((1u << bits) - 1), b0 = __builtin_amdgcn_readfirstlane(bin);
+        const uint64_t all = __ballot(true);
+        if (__ballot(bin == b0) == all) {
+          if (lane == __ffsll((unsigned long long)all) - 1) atomicAdd(&hist[b0], (uint32_t)__popcll(all));
+        } else {
+          atomicAdd(&hist[bin], 1u);
+        }
+      }
+    }
   }
   __syncthreads();
-  ns = nt = 0;
-  for (int w = 0; w < wave; ++w) {
-    ns += wsum[w];
-    nt += wtie[w];
-  }
-  const uint64_t below = (1ull << lane) - 1;
-  each([&](int slot, const uint32_t (&key)[4]) {
-    uint32_t bs = 0, bt = 0, as = 0, at = 0;  // before this lane's four, and of the whole step
-    uint32_t sure = 0, tie = 0;
+}
+
+// From the top digit down: the one where the running count reaches `need`, by 64 groups of 32 and then in one of them; it joins the
+// prefix, and what lies above it leaves `need`.  (All counts together are over `need`: more slots have a choice than stay.)
+DEVI void next_digit(const uint32_t *hist, int pass, uint32_t &prefix, uint32_t &need) {
+  __shared__ uint32_t s_bin, s_above;
+  const int lane = threadIdx.x & 63;
+  if (threadIdx.x < 64) {
+    uint32_t mine = 0;
+    for (int i = 0; i < 32; ++i) mine += hist[2047 - (lane * 32 + ((i + lane) & 31))];  // (rotated: one bank each)
+    auto running = [&](uint32_t v) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool in = slot + e >= first && slot + e < last;
-      const bool s = slot + e < w1 && (!in || (m > 0 && key[e] > prefix)), t = slot + e < w1 && in && m > 0 && key[e] == prefix;
-      const uint64_t vs = __ballot(s), vt = __ballot(t);
-      bs += __popcll(vs & below);
-      bt += __popcll(vt & below);
-      as += __popcll(vs);
-      at += __popcll(vt);
-      sure |= s ? 1u << e : 0u;
-      tie |= t ? 1u << e : 0u;
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t u = __shfl_up(v, o, 64);
+        if (lane >= o) v += u;
+      }
+      return v;
+    };
+    const uint32_t incl = running(mine);
+    const int group = max(__ffsll((unsigned long long)__ballot(incl >= need)) - 1, 0);
+    const uint32_t before = __shfl(incl - mine, group, 64);
+    const uint32_t h = lane < 32 ? hist[2047 - (group * 32 + lane)] : 0, upto = before + running(h);
+    const int bin = max(__ffsll((unsigned long long)__ballot(upto >= need)) - 1, 0);
+    if (lane == bin) {
+      s_bin = 2047 - (group * 32 + bin);
+      s_above = upto - h;
     }
-    bs += ns;
-    bt += nt;
+  }
+  __syncthreads();
+  prefix = (prefix << digit_bits(pass)) | s_bin;
+  need -= s_above;
+  __syncthreads();
+}
+
+// bit masks over the lanes of a step's slots that stay for sure, and of those that equal the last key that does
+DEVI void slice_marks(const Slice &s, int x, uint32_t prefix, uint64_t (&sure)[4], uint64_t (&tie)[4]) {
+  const int lane = threadIdx.x & 63, s0 = s.w0 + x * kSelStep;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int slot = s0 + lane * 4 + e;
+    const bool in = slot >= s.first && slot < s.last;
+    sure[e] = __ballot(slot < s.w1 && (!in || (s.m > 0 && s.key[x][e] > prefix)));
+    tie[e] = __ballot(slot < s.w1 && in && s.m > 0 && s.key[x][e] == prefix);
+  }
+}
+// what the wave's stretch holds of both
+DEVI uint2 slice_sum(const Slice &s, uint32_t prefix) {
+  uint2 sum = make_uint2(0, 0);
+#pragma unroll
+  for (int x = 0; x < kSelSteps; ++x) {
+    if (s.w0 + x * kSelStep >= s.w1) break;
+    uint64_t sure[4], tie[4];
+    slice_marks(s, x, prefix, sure, tie);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const bool s = sure >> e & 1, t = tie >> e & 1;
+      sum.x += __popcll(sure[e]);
+      sum.y += __popcll(tie[e]);
+    }
+  }
+  return sum;
+}
+// writes the wave's kept slots; `before`: what the stretches before it hold of both
+DEVI void slice_write(const Slice &s, uint32_t prefix, uint32_t need, uint2 before, int32_t *kept, int budget) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int x = 0; x < kSelSteps; ++x) {
+    const int s0 = s.w0 + x * kSelStep;
+    if (s0 >= s.w1) break;
+    uint64_t sure[4], tie[4];
+    slice_marks(s, x, prefix, sure, tie);
+    uint32_t bs = before.x, bt = before.y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bs += __popcll(sure[e] & below);
+      bt += __popcll(tie[e] & below);
+      before.x += __popcll(sure[e]);
+      before.y += __popcll(tie[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool in = sure[e] >> lane & 1, t = tie[e] >> lane & 1;
       const uint32_t to = bs + min(bt, need);
-      if ((s || (t && bt < need)) && to < (uint32_t)a.budget) kept[to] = slot + e;
-      bs += s;
+      if ((in || (t && bt < need)) && to < (uint32_t)budget) kept[to] = s0 + lane * 4 + e;
+      bs += in;
       bt += t;
     }
-    ns += as;
-    nt += at;
-  });
-  if (lost) raise_error(a.err, DEV_BAD_PAGE);
+  }
+}
+// the waves' sums of the workgroup added up before this one's
+DEVI uint2 sums_before(uint2 mine) {
+  __shared__ uint2 s_sum[kSelWaves];
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) s_sum[wave] = mine;
+  __syncthreads();
+  uint2 before = make_uint2(0, 0);
+  for (int w = 0; w < wave; ++w) before = make_uint2(before.x + s_sum[w].x, before.y + s_sum[w].y);
+  return before;
+}
+
+// Sequences with nothing to choose: new length and kept slots.  True for those.
+DEVI bool evict_trivial(const PagedEvictArgs &a, int b, bool lead, int n, int32_t *kept) {
+  const bool bad = n < 0 || n > a.max_len;
+  if (lead && threadIdx.x == 0) {
+    if (bad) raise_error(a.err, DEV_BAD_CTX_LEN);
+    a.new_lens[b] = bad ? n : min(n, a.budget);
+  }
+  if (!bad && n > a.budget) return false;
+  for (int i = threadIdx.x; i < a.budget; i += kSelThreads) kept[i] = !bad && i < n ? i : -1;
+  return true;
+}
+
+template <bool TINY_PAGES>
+__global__ __launch_bounds__(kSelThreads) void paged_evict_select_kernel(PagedEvictArgs a) {
+  const PagedView &c = a.c;
+  const int head = blockIdx.x % c.n_kv, b = (blockIdx.x / c.n_kv) % c.batch, layer = blockIdx.x / c.n_kv / c.batch;
+  int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
+  const int n = a.lens[b];
+  if (evict_trivial(a, b, layer == 0 && head == 0, n, kept)) return;
+  __shared__ uint32_t hist[2048];
+  Slice s;
+  slice_load<TINY_PAGES>(a, b, layer, head, 0, n, s);
+  uint32_t prefix = 0, need = s.m;
+  for (int pass = 0; pass < 3 && s.m > 0; ++pass) {
+    slice_count(s, pass, prefix, hist);
+    next_digit(hist, pass, prefix, need);
+  }
+  const uint2 before = sums_before(slice_sum(s, prefix));
+  slice_write(s, prefix, need, before, kept, a.budget);
+  if (s.lost) raise_error(a.err, DEV_BAD_PAGE);
+}
+
+// The sum of `v` over a workgroup's threads.
+DEVI uint32_t block_sum(uint32_t v) {
+  __shared__ uint32_t s_v[kSelWaves];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s_v[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0;
+  for (int w = 0; w < kSelWaves; ++w) v += s_v[w];
+  return v;
+}
+
+// The same over several slices, phase by phase: 0 to 2 count a digit, 3 writes.  Between them a head's slices leave `parts`
+// [2][head][slices][2048], a phase's counts beside those that it reads; `state` [head][2], (prefix, need) after the first two digits; and
+// `sums` [head][slices], the slice's keys above those digits.  So the last phase knows how many slots stay in the slices before its own.
+template <bool TINY_PAGES>
+__global__ __launch_bounds__(kSelThreads) void paged_evict_phase_kernel(PagedEvictArgs a, int phase, int slices) {
+  const PagedView &c = a.c;
+  const int slice = blockIdx.x % slices, at = blockIdx.x / slices;
+  const int head = at % c.n_kv, b = (at / c.n_kv) % c.batch, layer = at / c.n_kv / c.batch;
+  int32_t *kept = a.kept + (size_t)at * a.budget;
+  const size_t half = (size_t)gridDim.x * 2048, mine = (size_t)at * slices * 2048;
+  const uint32_t *counted = a.parts + ((phase & 1) ^ 1) * half + mine;
+  uint2 *state = a.state + (size_t)at * 2;
+  uint32_t *sums = a.sums + (size_t)at * slices;
+  const int n = a.lens[b];
+  if (phase == 0 && slice == 0 && evict_trivial(a, b, layer == 0 && head == 0, n, kept)) return;
+  if (n <= a.budget || n > a.max_len || slice * kEvictSlice >= n) return;
+  __shared__ uint32_t hist[2048];
+  const int used = (n + kEvictSlice - 1) / kEvictSlice;
+  Slice s;
+  slice_load<TINY_PAGES>(a, b, layer, head, slice, n, s);
+  uint32_t prefix = 0, need = s.m;
+  uint2 before = make_uint2(0, 0);
+  if (s.m > 0 && phase > 0) {
+    if (phase > 1) {
+      prefix = state[phase - 2].x;
+      need = state[phase - 2].y;
+    }
+    for (int i = threadIdx.x; i < 2048; i += kSelThreads) {  // the digit that the last phase counted
+      uint32_t sum = 0;
+      for (int x = 0; x < used; ++x) sum += counted[(size_t)x * 2048 + i];
+      hist[i] = sum;
+    }
+    __syncthreads();
+    next_digit(hist, phase - 1, prefix, need);
+    if (slice == 0 && threadIdx.x == 0 && phase < 3) state[phase - 1] = make_uint2(prefix, need);
+    const int bin = prefix & ((1u << digit_bits(phase - 1)) - 1);
+    // keys above it: this slice's, or in the end those of the slices before
+    uint32_t above = 0;
+    for (int x = phase < 3 ? slice : 0; x < (phase < 3 ? slice + 1 : slice); ++x)
+      for (int i = threadIdx.x; i < 2048; i += kSelThreads) above += i > bin ? counted[(size_t)x * 2048 + i] : 0;
+    above = block_sum(above);
+    if (phase < 3) {
+      if (threadIdx.x == 0) sums[slice] = (phase == 1 ? 0 : sums[slice]) + above;
+    } else {
+      before.x = above;
+      for (int x = 0; x < slice; ++x) {
+        before.x += sums[x];
+        before.y += counted[(size_t)x * 2048 + bin];
+      }
+    }
+  }
+  if (phase < 3) {
+    if (s.m > 0) {
+      slice_count(s, phase, prefix, hist);
+      uint32_t *to = a.parts + (phase & 1) * half + mine + (size_t)slice * 2048;
+      for (int i = threadIdx.x; i < 2048; i += kSelThreads) to[i] = hist[i];
+    }
+  } else {
+    const int past = slice * kEvictSlice;  // slots of the slices before, some of them without a choice
+    before.x += min(past, s.first) + max(0, past - s.last);
+    const uint2 waves = sums_before(slice_sum(s, prefix));
+    slice_write(s, prefix, need, make_uint2(before.x + waves.x, before.y + waves.y), kept, a.budget);
+    if (s.lost) raise_error(a.err, DEV_BAD_PAGE);
+  }
 }
 
 // Rows kept[i] move to slot i.  In place, a workgroup has one column slice of one head's keys or values (or the head's
@@ -543,7 +664,17 @@ void launch_paged_commit(const PagedView &c, int n_nodes, int max_depth, const i
 
 void launch_paged_evict(const PagedEvictArgs &a, hipStream_t st) {
   const int heads = a.c.n_layers * a.c.batch * a.c.n_kv;
-  hipLaunchKernelGGL(paged_evict_select_kernel, dim3(heads), dim3(kSelThreads), 0, st, a);
+  const bool tiny = a.c.page_shift < 2;
+  const int slices = (a.max_len + kEvictSlice - 1) / kEvictSlice;
+  if (slices == 1) {
+    if (tiny) hipLaunchKernelGGL(paged_evict_select_kernel<true>, dim3(heads), dim3(kSelThreads), 0, st, a);
+    else hipLaunchKernelGGL(paged_evict_select_kernel<false>, dim3(heads), dim3(kSelThreads), 0, st, a);
+  } else {
+    for (int phase = 0; phase < 4; ++phase) {
+      if (tiny) hipLaunchKernelGGL(paged_evict_phase_kernel<true>, dim3(heads * slices), dim3(kSelThreads), 0, st, a, phase, slices);
+      else hipLaunchKernelGGL(paged_evict_phase_kernel<false>, dim3(heads * slices), dim3(kSelThreads), 0, st, a, phase, slices);
+    }
+  }
   if (a.new_table) {
     hipLaunchKernelGGL(paged_evict_gather_kernel, dim3(heads, (min(a.budget, a.max_len) + kEvictMoveRows - 1) / kEvictMoveRows),
                        dim3(kMoveThreads), 0, st, a);

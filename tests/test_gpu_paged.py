@@ -246,6 +246,33 @@ def test_evict(dtype, dh, order, page, new_pages, budget, sink, recent, values):
         np.testing.assert_array_equal(got, want)
 
 
+@pytest.mark.parametrize("page,values", [(1, "random"), (2, "few"), (64, "random"), (64, "one"), (512, "few")])
+@pytest.mark.parametrize("new_pages", [False, True])
+def test_evict_long(page, values, new_pages):
+    """Sequences of more slots than one workgroup chooses from, beside short ones."""
+    lens, budget, sink, recent = [16384, 16385, 50000, 700, 32768], 1003, 5, 300
+    c = Pages(lens, page=page, nkv=2, dh=64, weights=True, stale="", spare=5 * -(-budget // page) + 2)
+    g = torch.Generator().manual_seed(9)
+    if values != "random":   # equal weights, over all slices or but for a few
+        c.w.copy_(torch.randint(0, 4, c.w.shape, generator=g) if values == "few" else torch.ones(c.w.shape))
+    k, v, w = c.copies()
+    per = -(-budget // page)
+    new_table = c.free[:5 * per].reshape(5, per).copy() if new_pages else None
+    want_lens, want_kept = po.evict(k, v, w, c.table, np.asarray(lens), budget, sink, recent, new_table)
+    kept = torch.full((1, 5, 2, budget), 9, dtype=torch.int32, device=DEV)
+    out = torch.zeros(5, dtype=torch.int32, device=DEV)
+    ws = c.workspace(bd.domino_paged_evict_workspace_bytes(c.cache, 50000, budget)).fill_(77)
+    ws[:16] = 0
+    for _ in range(1 if new_table is None else 2):   # (to new pages, the second call finds what the first did)
+        bd.domino_paged_evict(c.cache, i32(lens), out, 50000, budget, ws, sink=sink, recent=recent,
+                              new_table=None if new_table is None else i32(new_table), kept=kept)
+    no_error(ws)
+    np.testing.assert_array_equal(out.cpu().numpy(), want_lens)
+    np.testing.assert_array_equal(kept.cpu().numpy(), want_kept)
+    for got, want in zip(c.copies(), (k, v, w)):
+        np.testing.assert_array_equal(got, want)
+
+
 @pytest.mark.parametrize("dtype,dh,order,page,weights", [("bf16", 128, "slot", 16, True), ("bf16", 64, "head", 1, False),
                                                           ("f32", 128, "head", 32, True), ("f32", 64, "slot", 8, True)])
 @pytest.mark.parametrize("nodes,depth", [(61, 15), (16, 15), (2, 1), (1024, 63)])
