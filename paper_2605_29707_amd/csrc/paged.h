@@ -27,14 +27,11 @@ struct SeqRange {
   int start, n, len;
 };
 // false: nothing to do for the sequence (no new tokens, or lengths that disagree, which sets the error word)
-DEVI bool seq_range(const int32_t *starts, const int32_t *lens, int b, int tokens, int max_new, int max_len, int32_t *err,
-                    SeqRange &s) {
-  const int lo = starts[b], hi = starts[b + 1];
+DEVI bool check_range(int lo, int hi, int len, int tokens, int max_new, int max_len, int32_t *err, SeqRange &s) {
   s.start = lo;
   s.n = 0;
   s.len = 0;
   if (lo == hi) return false;
-  const int len = lens[b];
   // (hi - lo fits: both are in [0, tokens] once the first two hold)
   if (lo < 0 || hi > tokens || hi < lo || hi - lo > max_new || len < hi - lo || len > max_len) {
     if (err) raise_error(err, DEV_BAD_CTX_LEN);
@@ -43,6 +40,49 @@ DEVI bool seq_range(const int32_t *starts, const int32_t *lens, int b, int token
   s.n = hi - lo;
   s.len = len;
   return true;
+}
+DEVI bool seq_range(const int32_t *starts, const int32_t *lens, int b, int tokens, int max_new, int max_len, int32_t *err,
+                    SeqRange &s) {
+  const int lo = starts[b], hi = starts[b + 1], len = lens[b];  // one round trip
+  return check_range(lo, hi, len, tokens, max_new, max_len, err, s);
+}
+
+// The sequence of packed row t, found by a whole wave (the same t in every lane): a lane loads a sequence's starts and length.  False for
+// rows behind the last sequence, and where the starts are out of order or the lengths disagree (which sets the error word).
+DEVI bool seq_of_token(const int32_t *starts, const int32_t *lens, int batch, int t, int tokens, int max_new, int max_len, int32_t *err,
+                       int &b, SeqRange &s) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < batch; s0 += 64) {
+    const int i = min(s0 + lane, batch - 1);
+    const int lo = starts[i], hi = starts[i + 1], len = lens[i];
+    const int ended = __popcll(__ballot(s0 + lane < batch && hi <= t));
+    if (ended == min(64, batch - s0)) continue;
+    b = s0 + ended;
+    const int first = __builtin_amdgcn_readlane(lo, ended), end = __builtin_amdgcn_readlane(hi, ended);
+    if (!check_range(first, end, __builtin_amdgcn_readlane(len, ended), tokens, max_new, max_len, err, s)) return false;
+    if (t >= first && t < end) return true;
+    if (err) raise_error(err, DEV_BAD_CTX_LEN);
+    return false;
+  }
+  return false;
+}
+
+// two fp32 values as neighbouring bf16 values, rounded to the nearest (even) by the conversion instruction
+DEVI uint32_t pack_bf16(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// Running sum over the lanes of a wave, by lane moves alone.
+DEVI int wave_running_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast 15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast 31 into rows 2 and 3
+  return v;
 }
 
 }  // namespace dk

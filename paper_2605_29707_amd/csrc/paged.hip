@@ -36,7 +36,7 @@ DEVI void store8(T *p, const float (&x)[8]) {
   if constexpr (sizeof(T) == 2) {
     u32x4 w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)f32_to_bf16(x[2 * e]).v | ((uint32_t)f32_to_bf16(x[2 * e + 1]).v << 16);
+    for (int e = 0; e < 4; ++e) w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
     *(u32x4 *)p = w;
   } else {
     *(floatx4 *)p = floatx4{x[0], x[1], x[2], x[3]};
@@ -47,20 +47,10 @@ DEVI void store8(T *p, const float (&x)[8]) {
 template <typename T, int DH>
 __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedAppendArgs a) {
   constexpr int LPH = DH / 8, GROUPS = kAppendThreads / LPH;
-  const int t = blockIdx.x, lane = threadIdx.x & 63, j = threadIdx.x % LPH, grp = threadIdx.x / LPH;
-  // the sequence of token t: how many sequences end at or before it
-  int b = 0;
-  for (int s0 = 0; s0 < a.c.batch; s0 += 64) {
-    const bool done = s0 + lane < a.c.batch && a.starts[s0 + lane + 1] <= t;
-    b += __popcll(__ballot(done));
-  }
-  if (b >= a.c.batch) return;  // rows behind the last sequence
+  const int t = blockIdx.x, j = threadIdx.x % LPH, grp = threadIdx.x / LPH;
+  int b;
   SeqRange s;
-  if (!seq_range(a.starts, a.lens, b, a.tokens, a.tokens, a.c.max_pages << a.c.page_shift, a.err, s)) return;
-  if (t < s.start || t >= s.start + s.n) {  // starts out of order
-    raise_error(a.err, DEV_BAD_CTX_LEN);
-    return;
-  }
+  if (!seq_of_token(a.starts, a.lens, a.c.batch, t, a.tokens, a.tokens, a.c.max_pages << a.c.page_shift, a.err, b, s)) return;
   const int slot = s.len - s.n + (t - s.start);
   const int page = page_of(a.c, b, slot);
   if (page < 0) raise_error(a.err, DEV_BAD_PAGE);

@@ -21,29 +21,21 @@ struct Tile {
   SeqRange s;
 };
 
-// Sequences whose lengths disagree set the error word: one wave of a launch looks at all of them.
-DEVI void report_lengths(const PagedAttnArgs &a) {
-  SeqRange s;
-  for (int b = threadIdx.x & 63; b < a.c.batch; b += 64) seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, a.err, s);
-}
-
 // The tile-th tile of M rows over all sequences; false behind the last.  A sequence's last tiles come
-// first: with causal rows they are the longest.
-DEVI bool find_tile(const PagedAttnArgs &a, long tile, int M, Tile &t) {
+// first: with causal rows they are the longest.  With `err`, sequences whose lengths disagree set it: one workgroup of a launch looks
+// at all of them.
+DEVI bool find_tile(const PagedAttnArgs &a, int tile, int M, int32_t *err, Tile &t) {
   const int lane = threadIdx.x & 63, G = a.nq / a.c.n_kv;
-  long base = 0;
-  for (int s0 = 0; s0 < a.c.batch; s0 += 64) {
-    const int b = s0 + lane;
+  int base = 0;
+  bool found = false;
+  for (int s0 = 0; s0 < a.c.batch && (!found || err); s0 += 64) {
     SeqRange s{0, 0, 0};
-    if (b < a.c.batch) seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s);
-    const long n = ((long)s.n * G + M - 1) / M;
-    long incl = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const long v = __shfl_up(incl, o, 64);
-      if (lane >= o) incl += v;
-    }
-    const uint64_t here = __ballot(base + incl > tile);
+    const int i = min(s0 + lane, a.c.batch - 1);
+    const bool live = seq_range(a.starts, a.lens, i, a.tokens, a.max_new, a.max_len, err, s) && s0 + lane < a.c.batch;
+    if (found) continue;
+    // (a launch has fewer than 2^24 tiles, and `base` stays at most `tile`: nothing passes 32 bits)
+    const int n = live ? min((int)(((int64_t)s.n * G + M - 1) / M), 1 << 24) : 0, upto = base + wave_running_sum(n);
+    const uint64_t here = __ballot(upto > tile);
     if (here) {
       const int l = __ffsll((unsigned long long)here) - 1;
       t.b = s0 + l;
@@ -52,15 +44,15 @@ DEVI bool find_tile(const PagedAttnArgs &a, long tile, int M, Tile &t) {
       t.s.len = __builtin_amdgcn_readlane(s.len, l);
       t.rows = t.s.n * G;
       // (tile - first tile of the sequence) counts from its last one
-      t.row0 = ((t.rows + M - 1) / M - 1 - __builtin_amdgcn_readlane((int)(tile - (base + incl - n)), l)) * M;
+      t.row0 = ((t.rows + M - 1) / M - 1 - (tile - __builtin_amdgcn_readlane(upto - n, l))) * M;
       const int last = (min(t.row0 + M, t.rows) - 1) / G;
       t.vis = a.mask ? t.s.len : t.s.len - t.s.n + last + 1;
-      return true;
+      found = true;
+    } else {
+      base = __builtin_amdgcn_readlane(upto, 63);
     }
-    base += (long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)incl, 63) |
-                   ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(incl >> 32), 63) << 32));
   }
-  return false;
+  return found;
 }
 
 // Operands of the two products.  Scores: S^T = K Q^T in tiles of 16 slots x 16 rows, lane (g, r) = 16 g + r with
@@ -226,10 +218,8 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
   __shared__ float s_m[kPaWaves][M], s_l[kPaWaves][M];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
   const int kvh = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % splits;
-  const long tile = blockIdx.x / a.c.n_kv / splits;
   Tile t;
-  if (blockIdx.x == gridDim.x - 1 && wave == 0) report_lengths(a);
-  if (!find_tile(a, tile, M, t)) return;
+  if (!find_tile(a, blockIdx.x / a.c.n_kv / splits, M, blockIdx.x == gridDim.x - 1 ? a.err : nullptr, t)) return;
   const int k0 = split * run, k1 = min(t.vis, k0 + run);
   if (k0 >= k1) return;
   const int G = a.nq / a.c.n_kv, n0 = t.s.len - t.s.n;
@@ -453,8 +443,7 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
       } else {
         T *dst = (T *)a.out + (int64_t)tok * a.o_stride + (int64_t)head * DH + c;
         if constexpr (ESZ == 2) {
-          *(uint2 *)dst = make_uint2((uint32_t)f32_to_bf16(y[0]).v | ((uint32_t)f32_to_bf16(y[1]).v << 16),
-                                     (uint32_t)f32_to_bf16(y[2]).v | ((uint32_t)f32_to_bf16(y[3]).v << 16));
+          *(uint2 *)dst = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
         } else {
           *(floatx4 *)dst = y;
         }
@@ -486,10 +475,8 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
   __shared__ uint64_t s_odd[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, r = lane & 31;
   const int kvh = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % splits;
-  const long tile = blockIdx.x / a.c.n_kv / splits;
   Tile t;
-  if (blockIdx.x == gridDim.x - 1 && wave == 0) report_lengths(a);
-  if (!find_tile(a, tile, kChunkRows, t)) return;
+  if (!find_tile(a, blockIdx.x / a.c.n_kv / splits, kChunkRows, blockIdx.x == gridDim.x - 1 ? a.err : nullptr, t)) return;
   const int k0 = split * run, k1 = min(t.vis, k0 + run);
   if (k0 >= k1) return;
   const int G = a.nq / a.c.n_kv, n0 = t.s.len - t.s.n;
@@ -712,12 +699,9 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
       if (a.part_o) {
         *(floatx4 *)(a.part_o + at * DH + col) = floatx4{o[y][4 * c], o[y][4 * c + 1], o[y][4 * c + 2], o[y][4 * c + 3]};
       } else {
-        float z[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = o[y][4 * c + e] * inv;
         bf16_t *dst = (bf16_t *)a.out + (int64_t)tok * a.o_stride + (int64_t)qh * DH + col;
-        *(uint2 *)dst = make_uint2((uint32_t)f32_to_bf16(z[0]).v | ((uint32_t)f32_to_bf16(z[1]).v << 16),
-                                   (uint32_t)f32_to_bf16(z[2]).v | ((uint32_t)f32_to_bf16(z[3]).v << 16));
+        *(uint2 *)dst = make_uint2(pack_bf16(o[y][4 * c] * inv, o[y][4 * c + 1] * inv),
+                                   pack_bf16(o[y][4 * c + 2] * inv, o[y][4 * c + 3] * inv));
       }
     }
   if (h == 0) {
@@ -735,11 +719,9 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, i
   const int64_t at = (int64_t)blockIdx.x * (4 / W) + unit / W;
   if (at >= (int64_t)a.tokens * a.nq) return;
   const int tok = (int)(at / a.nq), head = (int)(at % a.nq), G = a.nq / a.c.n_kv;
-  int b = 0;
-  for (int s0 = 0; s0 < a.c.batch; s0 += 64) b += __popcll(__ballot(s0 + lane < a.c.batch && a.starts[s0 + lane + 1] <= tok));
+  int b;
   SeqRange s;
-  if (b >= a.c.batch || !seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s)) return;
-  if (tok < s.start || tok >= s.start + s.n) return;
+  if (!seq_of_token(a.starts, a.lens, a.c.batch, tok, a.tokens, a.max_new, a.max_len, nullptr, b, s)) return;
   const int row = (tok - s.start) * G + head % G, last = (min((row / M + 1) * M, s.n * G) - 1) / G;
   const int vis = a.mask ? s.len : s.len - s.n + last + 1, runs = (vis + run - 1) / run;
   const int64_t step = (int64_t)a.tokens * a.nq;
@@ -920,7 +902,8 @@ PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv
   // lengths end together (64 of 4096 to 16385 slots, weights and all: 622 us, 681 in runs of 8320).
   const long groups = p.tiles * n_kv;
   const int pieces = (int)(((long)max_len + 127) / 128);
-  long want = (511 + groups) / groups;
+  const long target = 512;
+  long want = (target - 1 + groups) / groups;
   if (p.rows == 16) want = std::max(want, std::min((8191 + groups) / groups, (long)max_len / 1024));
   const int splits = (int)std::min(want, (long)std::min(pieces, 128));
   p.run = (pieces + splits - 1) / splits * 128;
