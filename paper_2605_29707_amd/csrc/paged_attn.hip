@@ -468,7 +468,8 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
 constexpr int kChunkRows = 128, kChunkStep = 64;
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-template <int DH, bool MASKED>
+// PAGES, how a step's 64 slots lie in pages: 2, in one; 1, those of a wave's load (64 / (items a row) neighbours) do; 0, anyhow.
+template <int DH, bool MASKED, int PAGES>
 __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, int splits, int run) {
   constexpr int RB = DH * 2, CH = RB / 16, KST = DH / 16, DT = DH / 32, LPT = kChunkStep * CH / 256, TILE = kChunkStep * RB;
   __shared__ __align__(16) char s_k[2][TILE], s_v[2][TILE];
@@ -496,34 +497,42 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
   const int64_t head = a.layer * a.c.layer_stride + kvh * a.c.head_stride;
   const char *kb = a.c.k + head * 2, *vb = a.c.v + head * 2;
 
-  // this thread's items of a tile: 16 bytes of row (tid + 256 i) / CH.  Where a wave's rows of one i (64 / CH neighbours) lie in one
-  // page its address is a scalar, and the page's number is loaded a step before the rows.
-  constexpr int NEAR = 64 / CH;
+  // This thread's items of a step: 16 bytes of row (tid + 256 i) / CH.  Where a load's rows lie in one page its address is a scalar and
+  // a lane's offset, and the page's number is loaded a step before the rows.
+  constexpr int NEAR = 64 / CH, LOOKS = PAGES == 2 ? 1 : LPT;
   const int my_row = tid / CH, my_col = tid % CH;
-  const bool one_page = (1 << a.c.page_shift) >= NEAR && a.c.slot_stride < (1 << 24);
-  const uint32_t lane_at = one_page ? (uint32_t)(lane / CH) * (uint32_t)a.c.slot_stride * 2 + my_col * 16 : 0;
+  const uint32_t lane_at = PAGES ? (uint32_t)(PAGES == 2 ? my_row : lane / CH) * (uint32_t)a.c.slot_stride * 2 + my_col * 16 : 0;
   bool lost = false;
   u32x4 kr[LPT], vr[LPT];
-  int ahead[LPT];
-  auto first_of = [&](int kt, int i) { return min(kt + wave * NEAR + i * (256 / CH), (k1 - 1) & ~(NEAR - 1)); };
+  int ahead[LOOKS];
+  // the first slot of a load's rows; behind the run, of the last one
+  auto first_of = [&](int kt, int i) {
+    return PAGES == 2 ? min(kt, (k1 - 1) & ~(kChunkStep - 1)) : min(kt + wave * NEAR + i * (256 / CH), (k1 - 1) & ~(NEAR - 1));
+  };
   auto look = [&](int kt) {
-    if (one_page) {
+    if constexpr (PAGES != 0) {
 #pragma unroll
-      for (int i = 0; i < LPT; ++i) ahead[i] = a.c.table[(int64_t)t.b * a.c.max_pages + (first_of(kt, i) >> a.c.page_shift)];
+      for (int i = 0; i < LOOKS; ++i) ahead[i] = a.c.table[(int64_t)t.b * a.c.max_pages + (first_of(kt, i) >> a.c.page_shift)];
     }
   };
   auto load = [&](int kt) {
+    const char *kp = nullptr, *vp = nullptr;
 #pragma unroll
     for (int i = 0; i < LPT; ++i) {
-      if (one_page) {
-        int page = __builtin_amdgcn_readfirstlane(ahead[i]);
-        if ((unsigned)page >= (unsigned)a.c.n_pages) {
-          lost = true;
-          page = 0;
+      if constexpr (PAGES != 0) {
+        if (i < LOOKS) {
+          int page = __builtin_amdgcn_readfirstlane(ahead[i]);
+          if ((unsigned)page >= (unsigned)a.c.n_pages) {
+            lost = true;
+            page = 0;
+          }
+          const int64_t at = slot_offset(a.c, page, first_of(kt, i)) * 2;
+          kp = kb + at;
+          vp = vb + at;
         }
-        const int64_t at = slot_offset(a.c, page, first_of(kt, i)) * 2;
-        kr[i] = *(const u32x4 *)(kb + at + lane_at);
-        vr[i] = *(const u32x4 *)(vb + at + lane_at);
+        const int64_t more = PAGES == 2 ? (int64_t)(i * (256 / CH)) * a.c.slot_stride * 2 : 0;
+        kr[i] = *(const u32x4 *)(kp + more + lane_at);
+        vr[i] = *(const u32x4 *)(vp + more + lane_at);
       } else {
         const int slot = min(kt + my_row + i * (256 / CH), k1 - 1);
         int page = page_of(a.c, t.b, slot);
@@ -589,15 +598,17 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
     look(kt + 2 * kChunkStep);
     floatx16 s[2];
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
+    for (int y = 0; y < 2; ++y)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[y][e] = 0.f;
+    // (the two sums take turns: a product waits for the one before it on the same sum)
 #pragma unroll
-      for (int st = 0; st < KST; ++st) {
+    for (int st = 0; st < KST; ++st)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
         const u32x4 f = *(const u32x4 *)(s_k[buf] + y * 32 * RB + (k_at ^ (st * 32)));
         s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, q[st]), s[y], 0, 0, 0);
       }
-    }
     float x[32];
 #pragma unroll
     for (int e = 0; e < 32; ++e) x[e] = s[e / 16][e % 16];
@@ -915,7 +926,12 @@ template <typename T, int DH, bool MASKED>
 static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t st) {
   const dim3 grid((unsigned)(p.tiles * p.splits * a.c.n_kv)), block(kPaThreads);
   if constexpr (sizeof(T) == 2)
-    if (p.rows == kChunkRows) hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED>), grid, block, 0, st, a, p.splits, p.run);
+    if (p.rows == kChunkRows) {
+      const bool small = a.c.slot_stride < (1 << 24);  // a row's offset in its page in 32 bits
+      if (small && a.c.page_shift >= 6) hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED, 2>), grid, block, 0, st, a, p.splits, p.run);
+      else if (small && a.c.page_shift >= 3) hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED, 1>), grid, block, 0, st, a, p.splits, p.run);
+      else hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED, 0>), grid, block, 0, st, a, p.splits, p.run);
+    }
   const bool one_page = a.c.page_shift >= 5 && a.c.slot_stride < (1 << 24);
   if (p.rows == 16 && one_page) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 1, MASKED, true>), grid, block, 0, st, a, p.splits, p.run);
   else if (p.rows == 16) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 1, MASKED, false>), grid, block, 0, st, a, p.splits, p.run);
