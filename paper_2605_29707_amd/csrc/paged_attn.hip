@@ -899,7 +899,10 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
 PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv, int max_new, int max_len, bool accumulate) {
   const int G = nq / n_kv;
   PagedAttnPlan p;
-  p.rows = (long)max_new * G <= 16 ? 16 : (bf16 && (long)max_new * G > 32 ? kChunkRows : 32);
+  // Up to 16 rows a kernel whose waves take every fourth 32 slots; for bf16 above that the chunks' (at one row a head it takes
+  // 634 us for 64 sequences of 4096 to 16384 slots, the first 500; one of 8192: 22.9 and 16.7.  At 32 rows two tiles of the first
+  // take 74 us for 32 sequences of 2048, 70 the chunks').
+  p.rows = (long)max_new * G <= 16 ? 16 : (bf16 ? kChunkRows : 32);
   // tiles of rows: at most one part-filled for each sequence, and no more than every sequence's longest
   const long busy = tokens < batch ? tokens : batch;
   p.tiles = std::min((long)tokens * G / p.rows + busy, busy * (((long)max_new * G + p.rows - 1) / p.rows));
@@ -908,16 +911,15 @@ PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv
   p.scores_rows = max_new * G;
   p.scores_steps = (max_len + 31) / 32;
   if (!accumulate || p.rows != 16 || (double)p.scores_steps * 128 * p.scores_rows * batch * n_kv > 1e9) p.scores_steps = 0;
-  // Runs of whole 128 slots, as few as give each CU two workgroups (one sequence of 8192 slots 17.8 us, 22.8 with runs of
+  // Runs of whole steps (a workgroup's 128 slots or 64), as few as give each CU two workgroups (one sequence of 8192 slots 17.8 us, 22.8 with runs of
   // 128; 64 of 1000 54 us, 65 with 128).  With few rows runs of more than 1024 are cut further, so that sequences of different
   // lengths end together (64 of 4096 to 16385 slots, weights and all: 622 us, 681 in runs of 8320).
-  const long groups = p.tiles * n_kv;
-  const int pieces = (int)(((long)max_len + 127) / 128);
-  const long target = 512;
+  const long groups = p.tiles * n_kv, target = 512;
+  const int whole = p.rows == kChunkRows ? kChunkStep : 128, pieces = (int)(((long)max_len + whole - 1) / whole);
   long want = (target - 1 + groups) / groups;
   if (p.rows == 16) want = std::max(want, std::min((8191 + groups) / groups, (long)max_len / 1024));
   const int splits = (int)std::min(want, (long)std::min(pieces, 128));
-  p.run = (pieces + splits - 1) / splits * 128;
+  p.run = (pieces + splits - 1) / splits * whole;
   p.splits = (int)(((long)max_len + p.run - 1) / p.run);
   return p;
 }
@@ -935,8 +937,10 @@ static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t 
   const bool one_page = a.c.page_shift >= 5 && a.c.slot_stride < (1 << 24);
   if (p.rows == 16 && one_page) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 1, MASKED, true>), grid, block, 0, st, a, p.splits, p.run);
   else if (p.rows == 16) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 1, MASKED, false>), grid, block, 0, st, a, p.splits, p.run);
-  else if (p.rows == 32 && one_page) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, true>), grid, block, 0, st, a, p.splits, p.run);
-  else if (p.rows == 32) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, false>), grid, block, 0, st, a, p.splits, p.run);
+  if constexpr (sizeof(T) == 4) {
+    if (p.rows == 32 && one_page) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, true>), grid, block, 0, st, a, p.splits, p.run);
+    else if (p.rows == 32) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, false>), grid, block, 0, st, a, p.splits, p.run);
+  }
   if (p.splits > 8)
     hipLaunchKernelGGL((paged_attn_join_kernel<T, DH, 4>), dim3((unsigned)((long)a.tokens * a.nq)), block, 0, st, a, p.rows, p.run);
   else if (p.splits > 1)
