@@ -487,11 +487,12 @@ class PagedCache:
 
 def _heads(cache: PagedCache, name, t, tokens=None, heads=None):
     """(tokens, heads, token stride) of a [tokens, heads, head_dim] tensor whose tokens' heads are dense."""
-    if t.dim() != 3 or t.shape[2] != cache.head_dim or t.dtype != cache.dtype or t.get_device() != cache.device \
-            or (tokens is not None and t.shape[0] != tokens) or (heads is not None and t.shape[1] != heads):
+    sh = t.shape
+    if len(sh) != 3 or sh[2] != cache.head_dim or t.dtype is not cache.dtype or t.get_device() != cache.device \
+            or (tokens is not None and sh[0] != tokens) or (heads is not None and sh[1] != heads):
         raise DominoError(DOMINO_ERR_INVALID_ARG,
                           f"{name} must be [tokens, heads, head_dim] of the cache's type, on its device")
-    (n, h, dh), (ld, lh, one) = t.shape, t.stride()
+    (n, h, dh), (ld, lh, one) = sh, t.stride()
     if one != 1 or (h > 1 and lh != dh):
         raise DominoError(DOMINO_ERR_INVALID_ARG, f"{name} must have dense heads")
     return n, h, ld if n > 1 else h * dh

@@ -893,6 +893,126 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
   }
 }
 
+// The same for bf16: a workgroup has 256 slots, 64 a wave, whose rows of k stay in registers; the call's rows pass through two LDS
+// buffers 32 at a time (with their lse and the last slot that they see), in order.
+constexpr int kWeightSlots = 256;
+
+template <int DH, bool MASKED>
+__global__ __launch_bounds__(256, 2) void paged_chunk_weights_kernel(PagedAttnArgs a, int slabs) {
+  constexpr int RB = DH * 2, CH = RB / 16, KST = DH / 16, LPT = 32 * CH / 256;
+  __shared__ __align__(16) char s_q[2][32 * RB];
+  __shared__ float s_ls[2][32];
+  __shared__ int s_lim[2][32];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, r = lane & 31;
+  const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv / slabs, slab = blockIdx.x / a.c.n_kv % slabs * kWeightSlots;
+  SeqRange s;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || slab >= s.len) return;
+  s.start = __builtin_amdgcn_readfirstlane(s.start);
+  s.n = __builtin_amdgcn_readfirstlane(s.n);
+  s.len = __builtin_amdgcn_readfirstlane(s.len);
+  const int G = a.nq / a.c.n_kv, n0 = s.len - s.n, rows = s.n * G, kt = slab + wave * 64;
+  const char *kb = a.c.k + (a.layer * a.c.layer_stride + kvh * a.c.head_stride) * 2;
+  u32x4 k[2][KST];
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const int slot = min(kt + 32 * y + r, s.len - 1);
+    const char *p = kb + slot_offset(a.c, max(page_of(a.c, b, slot), 0), slot) * 2;
+#pragma unroll
+    for (int st = 0; st < KST; ++st) k[y][st] = *(const u32x4 *)(p + st * 32 + h * 16);
+  }
+  const float sc = a.scale * kLog2e;
+  const int my_row = tid / CH, my_col = tid % CH;
+  u32x4 qr[LPT];
+  float ls = 0.f;
+  int lim = 0;
+  auto load = [&](int row0) {
+#pragma unroll
+    for (int i = 0; i < LPT; ++i) {
+      const int row = min(row0 + my_row + i * (256 / CH), rows - 1);
+      qr[i] = *(const u32x4 *)((const char *)a.q + ((int64_t)(s.start + row / G) * a.q_stride + (int64_t)(kvh * G + row % G) * DH) * 2 + my_col * 16);
+    }
+    if (tid < 32) {
+      const int row = min(row0 + tid, rows - 1);
+      lim = n0 + row / G;
+      ls = a.lse[(int64_t)(s.start + row / G) * a.nq + kvh * G + row % G] * kLog2e;
+      if (row0 + tid >= rows || ls == -INFINITY) ls = INFINITY;  // its weights are 0
+    }
+  };
+  auto swz = [](int x) { return CH == 16 ? x & 15 : (x >> 1) & 7; };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < LPT; ++i) {
+      const int x = my_row + i * (256 / CH);
+      *(u32x4 *)(s_q[buf] + x * RB + (my_col ^ swz(x)) * 16) = qr[i];
+    }
+    if (tid < 32) {
+      s_ls[buf][tid] = ls;
+      s_lim[buf][tid] = lim;
+    }
+  };
+  float sum[32] = {};
+  const int q_at = r * RB + (h ^ swz(r)) * 16;
+  // the first tile with a row that sees slot `slab`
+  const int first = MASKED ? 0 : max(0, slab - n0) * G / 32 * 32;
+  load(first);
+  store(0);
+  __syncthreads();
+  int buf = 0;
+  for (int row0 = first; row0 < rows; row0 += 32, buf ^= 1) {
+    const bool more = row0 + 32 < rows;
+    if (more) load(row0 + 32);
+    floatx16 x[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[y][e] = 0.f;
+#pragma unroll
+    for (int st = 0; st < KST; ++st) {
+      const u32x4 f = *(const u32x4 *)(s_q[buf] + (q_at ^ (st * 32)));
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        x[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[y][st]), __builtin_bit_cast(bf16x8, f), x[y], 0, 0, 0);
+    }
+    const float ml = s_ls[buf][r];
+    float w[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) w[e] = fast_exp2(fmaf(x[e / 16][e % 16], sc, -ml));
+    if (kt + 64 > (MASKED ? n0 : n0 + row0 / G + 1) || row0 + 32 > rows) {
+      const int last = s_lim[buf][r];
+      const uint8_t *mrow = MASKED ? a.mask + (int64_t)(s.start + last - n0) * a.mask_ld : nullptr;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const int slot = kt + 32 * (e / 16) + 8 * (e % 16 / 4) + 4 * h + e % 4;
+        bool seen = slot <= last;
+        if (MASKED) seen = (slot < n0) | (mrow[max(0, min(slot, s.len - 1) - n0)] != 0);
+        seen &= (ml != INFINITY) & (slot < s.len);
+        w[e] = seen ? w[e] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 32; ++e) sum[e] += w[e];
+    if (more) store(buf ^ 1);
+    __syncthreads();
+  }
+  // over the 32 rows of a lane half; lane r then has the r-th of its half's 32 slots
+  float mine = 0.f;
+#pragma unroll
+  for (int e = 0; e < 32; ++e) {
+    float v = sum[e];
+    v += row_ror<8>(v);
+    v += row_ror<4>(v);
+    v += row_ror<2>(v);
+    v += row_ror<1>(v);
+    v += __shfl_xor(v, 16, 64);
+    mine = r == e ? v : mine;
+  }
+  const int slot = kt + 32 * (r / 16) + 8 * (r % 16 / 4) + 4 * h + r % 4;
+  if (slot < s.len) {
+    const int page = page_of(a.c, b, slot);
+    if (page >= 0) a.c.weights[weight_offset(a.c, a.layer, page, kvh, slot)] += mine;
+  }
+}
+
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
@@ -949,8 +1069,10 @@ static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t 
     const int slabs = (a.max_len + 1023) / 1024;
     hipLaunchKernelGGL(paged_weights_of_scores_kernel, dim3((unsigned)((long)slabs * a.c.batch * a.c.n_kv)), block, 0, st, a, slabs);
   } else if (a.accumulate) {
-    const int slabs = (a.max_len + kPaWaves * kPaStep - 1) / (kPaWaves * kPaStep);
-    hipLaunchKernelGGL((paged_weights_kernel<T, DH, MASKED>), dim3((unsigned)((long)slabs * a.c.batch * a.c.n_kv)), block, 0, st, a, slabs);
+    const int each = sizeof(T) == 2 ? kWeightSlots : kPaWaves * kPaStep, slabs = (a.max_len + each - 1) / each;
+    const dim3 all((unsigned)((long)slabs * a.c.batch * a.c.n_kv));
+    if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((paged_chunk_weights_kernel<DH, MASKED>), all, block, 0, st, a, slabs);
+    else hipLaunchKernelGGL((paged_weights_kernel<T, DH, MASKED>), all, block, 0, st, a, slabs);
   }
 }
 template <typename T, int DH>
