@@ -1497,7 +1497,7 @@ domino_status check_tokens(const domino_paged_cache *c, int32_t layer, int32_t t
 }
 struct PagedAttnLayout {
   PagedAttnPlan plan;
-  size_t lse, ml, o, scores, bytes;
+  size_t lse, ml, o, scores, part_w, bytes;
 };
 domino_status paged_attn_layout(const domino_paged_cache *c, int32_t tokens, int32_t n_q_heads, int32_t max_new, int32_t max_len,
                                 int32_t accumulate, PagedAttnLayout &w) {
@@ -1517,7 +1517,8 @@ domino_status paged_attn_layout(const domino_paged_cache *c, int32_t tokens, int
   w.ml = w.lse + (accumulate ? align_up(rows * 4) : 0);
   w.o = w.ml + (w.plan.splits > 1 ? align_up(rows * w.plan.splits * 8) : 0);
   w.scores = w.o + (w.plan.splits > 1 ? align_up(rows * w.plan.splits * c->head_dim * 4) : 0);
-  w.bytes = w.scores + align_up((size_t)w.plan.scores_steps * w.plan.scores_rows * 128 * c->batch * c->n_kv_heads);
+  w.part_w = w.scores + align_up((size_t)w.plan.scores_steps * w.plan.scores_rows * 128 * c->batch * c->n_kv_heads);
+  w.bytes = w.part_w + align_up((size_t)w.plan.part_w * 4);
   return DOMINO_OK;
 }
 domino_status check_evict(const domino_paged_cache *c, int32_t max_len, int32_t budget) {
@@ -1670,6 +1671,7 @@ domino_status domino_paged_attention(const domino_paged_cache *cache, int32_t la
   a.part_o = w.plan.splits > 1 ? (float *)(ws + w.o) : nullptr;
   a.scores = w.plan.scores_steps ? (float *)(ws + w.scores) : nullptr;
   a.scores_steps = w.plan.scores_steps;
+  a.part_w = (float *)(ws + w.part_w);
   a.scores_rows = w.plan.scores_rows;
   a.accumulate = accumulate != 0;
   a.err = (int32_t *)workspace;

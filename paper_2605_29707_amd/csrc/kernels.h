@@ -397,6 +397,7 @@ struct PagedAttnArgs {
   float *part_ml;    // [splits][tokens][nq][2]: maximum (base 2) and sum
   float *scores;     // [batch][n_kv][scores_steps][scores_rows][32] base-2 scores, where the weights come from them
   int scores_steps, scores_rows;
+  float *part_w;     // [batch][n_kv][parts][whole slabs of slots] sums of the weights, where workgroups share a slab
   int accumulate;
   int32_t *err;
 };
@@ -406,6 +407,8 @@ struct PagedAttnPlan {
   long tiles;      // tiles that hold rows, at most
   int splits, run; // a sequence's slots are cut into runs of `run`
   int scores_steps, scores_rows;  // steps 0: no scores are kept
+  int parts;       // workgroups that share a slab of slots, for the weights from k
+  long part_w;     // and the sums that they leave
 };
 PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv, int max_new, int max_len,
                               bool accumulate);

@@ -894,17 +894,19 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
 }
 
 // The same for bf16: a workgroup has 256 slots, 64 a wave, whose rows of k stay in registers; the call's rows pass through two LDS
-// buffers 32 at a time (with their lse and the last slot that they see), in order.
+// buffers 32 at a time (with their lse and the last slot that they see), in order.  Where the slots make few workgroups, `parts` of them
+// share a slab's rows, every parts-th 32, and leave their sums to the next kernel.
 constexpr int kWeightSlots = 256;
 
 template <int DH, bool MASKED>
-__global__ __launch_bounds__(256, 2) void paged_chunk_weights_kernel(PagedAttnArgs a, int slabs) {
+__global__ __launch_bounds__(256, 2) void paged_chunk_weights_kernel(PagedAttnArgs a, int slabs, int parts) {
   constexpr int RB = DH * 2, CH = RB / 16, KST = DH / 16, LPT = 32 * CH / 256;
   __shared__ __align__(16) char s_q[2][32 * RB];
   __shared__ float s_ls[2][32];
   __shared__ int s_lim[2][32];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, r = lane & 31;
-  const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv / slabs, slab = blockIdx.x / a.c.n_kv % slabs * kWeightSlots;
+  const int kvh = blockIdx.x % a.c.n_kv, part = blockIdx.x / a.c.n_kv % parts, rest = blockIdx.x / a.c.n_kv / parts;
+  const int b = rest / slabs, slab = rest % slabs * kWeightSlots;
   SeqRange s;
   if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || slab >= s.len) return;
   s.start = __builtin_amdgcn_readfirstlane(s.start);
@@ -953,14 +955,14 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_weights_kernel(PagedAttnAr
   float sum[32] = {};
   const int q_at = r * RB + (h ^ swz(r)) * 16;
   // the first tile with a row that sees slot `slab`
-  const int first = MASKED ? 0 : max(0, slab - n0) * G / 32 * 32;
+  const int first = (MASKED ? 0 : max(0, slab - n0) * G / 32 * 32) + 32 * part, ahead = 32 * parts;
   load(first);
   store(0);
   __syncthreads();
   int buf = 0;
-  for (int row0 = first; row0 < rows; row0 += 32, buf ^= 1) {
-    const bool more = row0 + 32 < rows;
-    if (more) load(row0 + 32);
+  for (int row0 = first; row0 < rows; row0 += ahead, buf ^= 1) {
+    const bool more = row0 + ahead < rows;
+    if (more) load(row0 + ahead);
     floatx16 x[2];
 #pragma unroll
     for (int y = 0; y < 2; ++y)
@@ -1007,10 +1009,25 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_weights_kernel(PagedAttnAr
     mine = r == e ? v : mine;
   }
   const int slot = kt + 32 * (r / 16) + 8 * (r % 16 / 4) + 4 * h + r % 4;
-  if (slot < s.len) {
+  if (parts > 1) {
+    a.part_w[((int64_t)(b * a.c.n_kv + kvh) * parts + part) * slabs * kWeightSlots + slot] = mine;
+  } else if (slot < s.len) {
     const int page = page_of(a.c, b, slot);
     if (page >= 0) a.c.weights[weight_offset(a.c, a.layer, page, kvh, slot)] += mine;
   }
+}
+
+__global__ __launch_bounds__(kWeightSlots) void paged_weights_join_kernel(PagedAttnArgs a, int slabs, int parts) {
+  const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv / slabs;
+  const int slot = blockIdx.x / a.c.n_kv % slabs * kWeightSlots + threadIdx.x;
+  SeqRange s;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || slot >= s.len) return;
+  const int page = page_of(a.c, b, slot);
+  if (page < 0) return;
+  const float *p = a.part_w + (int64_t)(b * a.c.n_kv + kvh) * parts * slabs * kWeightSlots + slot;
+  float sum = 0.f;
+  for (int x = 0; x < parts; ++x) sum += p[(int64_t)x * slabs * kWeightSlots];
+  a.c.weights[weight_offset(a.c, a.layer, page, kvh, slot)] += sum;
 }
 
 // ---------------------------------------------------------------------------
@@ -1031,6 +1048,12 @@ PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv
   p.scores_rows = max_new * G;
   p.scores_steps = (max_len + 31) / 32;
   if (!accumulate || p.rows != 16 || (double)p.scores_steps * 128 * p.scores_rows * batch * n_kv > 1e9) p.scores_steps = 0;
+  // else, for bf16, from k by workgroups of 256 slots: as many share a slab's rows as give each CU two
+  const long slabs = ((long)max_len + kWeightSlots - 1) / kWeightSlots * batch * n_kv;
+  p.parts = 1;
+  if (accumulate && bf16 && !p.scores_steps && slabs < 512)
+    p.parts = (int)std::min((511 + slabs) / slabs, std::min(16L, ((long)max_new * G + 63) / 64));
+  p.part_w = p.parts > 1 ? slabs * kWeightSlots * p.parts : 0;
   // Runs of whole steps (a workgroup's 128 slots or 64), as few as give each CU two workgroups (one sequence of 8192 slots 17.8 us, 22.8 with runs of
   // 128; 64 of 1000 54 us, 65 with 128).  With few rows runs of more than 1024 are cut further, so that sequences of different
   // lengths end together (64 of 4096 to 16385 slots, weights and all: 622 us, 681 in runs of 8320).
@@ -1070,9 +1093,11 @@ static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t 
     hipLaunchKernelGGL(paged_weights_of_scores_kernel, dim3((unsigned)((long)slabs * a.c.batch * a.c.n_kv)), block, 0, st, a, slabs);
   } else if (a.accumulate) {
     const int each = sizeof(T) == 2 ? kWeightSlots : kPaWaves * kPaStep, slabs = (a.max_len + each - 1) / each;
-    const dim3 all((unsigned)((long)slabs * a.c.batch * a.c.n_kv));
-    if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((paged_chunk_weights_kernel<DH, MASKED>), all, block, 0, st, a, slabs);
-    else hipLaunchKernelGGL((paged_weights_kernel<T, DH, MASKED>), all, block, 0, st, a, slabs);
+    const dim3 all((unsigned)((long)slabs * a.c.batch * a.c.n_kv)), cut(all.x * p.parts);
+    if constexpr (sizeof(T) == 2) {
+      hipLaunchKernelGGL((paged_chunk_weights_kernel<DH, MASKED>), cut, block, 0, st, a, slabs, p.parts);
+      if (p.parts > 1) hipLaunchKernelGGL(paged_weights_join_kernel, all, dim3(kWeightSlots), 0, st, a, slabs, p.parts);
+    } else hipLaunchKernelGGL((paged_weights_kernel<T, DH, MASKED>), all, block, 0, st, a, slabs);
   }
 }
 template <typename T, int DH>
