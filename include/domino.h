@@ -511,8 +511,8 @@ domino_status domino_sample_logits(int32_t rows, int32_t vocab, const void *logi
  *  head_dim        64 or 128
  * For the calls below
  *  seq_starts      device int32 [batch + 1]: rows [seq_starts[b], seq_starts[b + 1]) of the
- *                  packed new tokens are sequence b's (none: the sequence waits).  Rows behind the
- *                  last sequence are left as they are
+ *                  packed new tokens are sequence b's (none: the sequence waits).  Rows before the
+ *                  first sequence and behind the last are left as they are
  *  kv_lens         device int32 [batch]: slots in use, the new tokens' own included (they are
  *                  the last ones).  A sequence whose starts and lengths disagree, or pass the
  *                  limits that the call was given, is left out: DOMINO_DEV_BAD_CTX_LEN

@@ -48,7 +48,7 @@ DEVI bool seq_range(const int32_t *starts, const int32_t *lens, int b, int token
 }
 
 // The sequence of packed row t, found by a whole wave (the same t in every lane): a lane loads a sequence's starts and length.  False for
-// rows behind the last sequence, and where the starts are out of order or the lengths disagree (which sets the error word).
+// rows before the first sequence or behind the last, and where the starts are out of order or the lengths disagree (which sets the error word).
 DEVI bool seq_of_token(const int32_t *starts, const int32_t *lens, int batch, int t, int tokens, int max_new, int max_len, int32_t *err,
                        int &b, SeqRange &s) {
   const int lane = threadIdx.x & 63;
@@ -61,7 +61,7 @@ DEVI bool seq_of_token(const int32_t *starts, const int32_t *lens, int batch, in
     const int first = __builtin_amdgcn_readlane(lo, ended), end = __builtin_amdgcn_readlane(hi, ended);
     if (!check_range(first, end, __builtin_amdgcn_readlane(len, ended), tokens, max_new, max_len, err, s)) return false;
     if (t >= first && t < end) return true;
-    if (err) raise_error(err, DEV_BAD_CTX_LEN);
+    if (err && b > 0) raise_error(err, DEV_BAD_CTX_LEN);
     return false;
   }
   return false;

@@ -142,6 +142,9 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedAppen
 // ---------------------------------------------------------------------------
 constexpr int kMoveThreads = 256;
 
+// PER items of 16 bytes a thread: what bounds it is how many workgroups a CU holds, so the usual few rows take few registers (32 trees
+// of depth 15, 36 layers: 19.6 us with 4, 26.9 with the 16 that 63 rows of 128 fp32 values need).
+template <int PER>
 __global__ __launch_bounds__(kMoveThreads) void paged_commit_kernel(PagedView c, int nn, int max_depth,
                                                                     const int32_t *__restrict__ ctx_lens,
                                                                     const int32_t *__restrict__ accept_len,
@@ -185,18 +188,20 @@ __global__ __launch_bounds__(kMoveThreads) void paged_commit_kernel(PagedView c,
   }
   if (lead) new_lens[b] = n + 1 + a;
   if (a == 0) return;
-  const int esz = c.bf16 ? 2 : 4, row16 = c.dh * esz / 16, items = 2 * a * row16;
-  constexpr int PER = 63 * 2 * 32 / kMoveThreads + 1;  // 63 rows of 128 fp32 values, k and v
+  const int esz = c.bf16 ? 2 : 4, shift = __builtin_ctz(c.dh * esz / 16), half = a << shift, items = 2 * half;  // (8, 16 or 32 items a row)
   const int64_t base = (layer * c.layer_stride + head * c.head_stride) * esz;
+  // item `it`: 16 bytes of a row of k, then of v; its place from `rows`' offset of the row
+  auto place = [&](int it, const int64_t *rows) {
+    const int rem = it < half ? it : it - half;
+    return (it < half ? c.k : c.v) + base + rows[rem >> shift] * esz + (rem & ((1 << shift) - 1)) * 16;
+  };
+  auto moves = [&](int it) { return it < items && from[(it < half ? it : it - half) >> shift] >= 0; };
   u32x4 v[PER];
 #pragma unroll
   for (int q = 0; q < PER; ++q) {
     const int it = tid + q * kMoveThreads;
     v[q] = u32x4{0, 0, 0, 0};
-    if (it < items) {
-      const int isv = it / (a * row16), rem = it % (a * row16), d = rem / row16;
-      if (from[d] >= 0) v[q] = *(const u32x4 *)((isv ? c.v : c.k) + base + from[d] * esz + (rem % row16) * 16);
-    }
+    if (q * kMoveThreads < items && moves(it)) v[q] = *(const u32x4 *)place(it, from);
   }
   float w = 0.f;
   if (c.weights && tid < a && from[tid] >= 0) w = c.weights[w_from[tid]];
@@ -207,10 +212,7 @@ __global__ __launch_bounds__(kMoveThreads) void paged_commit_kernel(PagedView c,
 #pragma unroll
   for (int q = 0; q < PER; ++q) {
     const int it = tid + q * kMoveThreads;
-    if (it < items) {
-      const int isv = it / (a * row16), rem = it % (a * row16), d = rem / row16;
-      if (from[d] >= 0) *(u32x4 *)((isv ? c.v : c.k) + base + to[d] * esz + (rem % row16) * 16) = v[q];
-    }
+    if (q * kMoveThreads < items && moves(it)) *(u32x4 *)place(it, to) = v[q];
   }
   if (c.weights && tid < a && from[tid] >= 0) c.weights[w_to[tid]] = w;
 }
@@ -621,12 +623,12 @@ __global__ __launch_bounds__(kMoveThreads) void paged_evict_gather_kernel(PagedE
     }
   }
   __syncthreads();
-  const int esz = c.bf16 ? 2 : 4, row16 = c.dh * esz / 16;
+  const int esz = c.bf16 ? 2 : 4, shift = __builtin_ctz(c.dh * esz / 16), half = rows << shift;
   const int64_t base = (layer * c.layer_stride + head * c.head_stride) * esz;
-  for (int it = tid; it < 2 * rows * row16; it += kMoveThreads) {
-    const int isv = it / (rows * row16), rem = it % (rows * row16), d = rem / row16;
+  for (int it = tid; it < 2 * half; it += kMoveThreads) {
+    const int rem = it < half ? it : it - half, d = rem >> shift;
     if (from[d] < 0) continue;
-    char *p = (isv ? c.v : c.k) + base + (rem % row16) * 16;
+    char *p = (it < half ? c.k : c.v) + base + (rem & ((1 << shift) - 1)) * 16;
     *(u32x4 *)(p + to[d] * esz) = *(const u32x4 *)(p + from[d] * esz);
   }
 }
@@ -648,8 +650,12 @@ void launch_paged_append(const PagedAppendArgs &a, hipStream_t st) {
 
 void launch_paged_commit(const PagedView &c, int n_nodes, int max_depth, const int32_t *ctx_lens, const int32_t *accept_len,
                          const int32_t *accepted, int32_t *new_lens, int32_t *err, hipStream_t st) {
-  hipLaunchKernelGGL(paged_commit_kernel, dim3(c.n_layers * c.batch * c.n_kv), dim3(kMoveThreads), 0, st, c, n_nodes, max_depth,
-                     ctx_lens, accept_len, accepted, new_lens, err);
+  const dim3 grid(c.n_layers * c.batch * c.n_kv), block(kMoveThreads);
+  const int items = 2 * max_depth * (c.dh * (c.bf16 ? 2 : 4) / 16);
+  if (items <= 4 * kMoveThreads)
+    hipLaunchKernelGGL(paged_commit_kernel<4>, grid, block, 0, st, c, n_nodes, max_depth, ctx_lens, accept_len, accepted, new_lens, err);
+  else
+    hipLaunchKernelGGL(paged_commit_kernel<16>, grid, block, 0, st, c, n_nodes, max_depth, ctx_lens, accept_len, accepted, new_lens, err);
 }
 
 void launch_paged_evict(const PagedEvictArgs &a, hipStream_t st) {

@@ -145,6 +145,72 @@ def check_attention(c, q, news, lens, layer=0, scale=None, mask=None, max_new=No
     return out, lse
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("most", [1, 3, 40])
+def test_many_sequences(dtype, most):
+    """More sequences than a wave has lanes, some of them waiting, the rows of all in one call."""
+    rng = np.random.RandomState(most)
+    news = rng.randint(0, most + 1, 150)
+    news[[0, 63, 64, 65, 149]] = [0, most, 0, most, 1]
+    lens = news + rng.randint(0, 90, 150)
+    c = Pages(lens, page=4, nkv=2, dh=64, dtype=dtype, weights=True, seed=most)
+    q = tokens(news.sum() + 2, 4, 64, dtype, 1, scale=2.0)
+    check_attention(c, q, list(news), list(lens), accumulate=True, tail=2)
+    # and their append
+    x, out, ws = tokens(news.sum() + 2, 8, 64, dtype, 2), torch.zeros_like(q), c.workspace(16)
+    old_k, old_v, old_w = c.copies()
+    bd.domino_paged_append(c.cache, x[:, :4], x[:, 4:6], x[:, 6:], out, i32(starts_of(news)), i32(lens), ws)
+    no_error(ws)
+    assert torch.equal(out[:-2], x[:-2, :4]) and (out[-2:] == 0).all()
+    for b, at in enumerate(starts_of(news)[:-1]):
+        p, r = po.cells(c.table, b, np.arange(lens[b] - news[b], lens[b]), 4)
+        old_k[0, p, r], old_v[0, p, r] = (x[at:at + news[b], s].float().cpu().numpy() for s in (slice(4, 6), slice(6, 8)))
+        old_w[0, p, :, r] = 0
+    for got, want in zip(c.copies(), (old_k, old_v, old_w)):
+        np.testing.assert_array_equal(got, want)
+
+
+def test_one_kv_head_for_many_query_heads():
+    for news in ([1, 1], [3, 70]):
+        c = Pages([90, 300], page=16, nkv=1, dh=128, weights=True)
+        check_attention(c, tokens(sum(news), 160, 128, "bf16", 3), news, [90, 300], accumulate=True)
+
+
+def test_rows_before_the_first_sequence():
+    c = Pages([40, 9], page=8, nkv=2, dh=64)
+    x, ws = tokens(9, 8, 64, "bf16", 1), c.workspace(1 << 20)
+    out = torch.full((9, 4, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    bd.domino_paged_append(c.cache, x[:, :4], x[:, 4:6], x[:, 6:], out, i32([3, 5, 8]), i32([40, 9]), ws)
+    assert torch.equal(out[3:8], x[3:8, :4]) and (out[:3] == 7).all() and (out[8:] == 7).all()
+    att = torch.full((9, 4, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    bd.domino_paged_attention(c.cache, out, att, i32([3, 5, 8]), i32([40, 9]), 3, 40, ws)
+    no_error(ws)
+    want = torch.empty(5, 4, 64, dtype=torch.bfloat16, device=DEV)
+    bd.domino_paged_attention(c.cache, out[3:8], want, i32([0, 2, 5]), i32([40, 9]), 3, 40, ws)
+    assert torch.equal(att[3:8], want) and (att[:3] == 7).all() and (att[8:] == 7).all()
+
+
+def test_append_of_many_tokens():
+    """From 1024 tokens on a workgroup has all heads of a token."""
+    lens, news = [1500, 700], [1500, 33]
+    c, d = (Pages(lens, page=64, nkv=2, dh=128, seed=1, weights=True) for _ in range(2))
+    x = tokens(1533, 24, 128, "bf16", 1)
+    freq = dev(bd.domino_rope_frequencies(128, 1e6)[0])
+    outs = [torch.empty(1533, 20, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    ws = c.workspace(16)
+    bd.domino_paged_append(c.cache, x[:, :20], x[:, 20:22], x[:, 22:], outs[0], i32([0, 1500, 1533]), i32(lens), ws, frequencies=freq)
+    for lo in range(0, 1533, 500):        # in pieces, with the positions of the whole
+        hi = min(lo + 500, 1533)
+        cut = [max(0, min(hi, 1500) - lo), max(0, hi - max(lo, 1500))]
+        done = [min(hi, 1500), 667 + max(0, hi - 1500)]
+        y = x[lo:hi]
+        bd.domino_paged_append(d.cache, y[:, :20], y[:, 20:22], y[:, 22:], outs[1][lo:hi], i32(starts_of(cut)), i32(done), ws, frequencies=freq)
+    no_error(ws)
+    assert torch.equal(outs[0], outs[1])
+    for a, b in ((c.k, d.k), (c.v, d.v), (c.w, d.w)):
+        assert torch.equal(a.nan_to_num(), b.nan_to_num())
+
+
 SHAPES = [  # lens, news, heads, kv heads, page
     ([1], [1], 1, 1, 1), ([1, 2, 3], [1, 2, 3], 4, 2, 1), ([33, 128, 129, 127], [1, 1, 1, 1], 8, 2, 16),
     ([40, 5, 300], [0, 5, 7], 6, 3, 8), ([257, 31], [16, 16], 16, 1, 32), ([700, 65, 64], [61, 33, 64], 8, 2, 64),
