@@ -165,11 +165,12 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream(stream):
+def _stream(stream, device=None):
+    """device: the current one, where the caller knows it."""
     if stream is None:
         import torch
         # the handle alone: a Stream object costs 3 us, as much as a launch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -530,7 +531,7 @@ def domino_paged_append(cache: PagedCache, q, k, v, q_out, seq_starts, kv_lens, 
         cache.ref, int(layer), n, nq, _ptr(q), lq, _ptr(k), lk, _ptr(v), lv, _ptr(q_out), lo, _ptr(seq_starts),
         _ptr(kv_lens), _ptr(positions), _ptr(frequencies), 0 if frequencies is None else 2 * frequencies.numel(),
         int(bool(interleaved)), float(rope_scale), _ptr(q_norm), _ptr(k_norm), float(rms_eps), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream(stream)))
+        workspace.numel() * workspace.element_size(), _stream(stream, dev)))
 
 
 def domino_paged_attention_workspace_bytes(cache: PagedCache, tokens, n_q_heads, max_new, max_len, accumulate=False) -> int:
@@ -565,7 +566,7 @@ def domino_paged_attention(cache: PagedCache, q, out, seq_starts, kv_lens, max_n
     _check(load().domino_paged_attention(
         cache.ref, int(layer), n, nq, int(max_new), int(max_len), _ptr(q), lq, _ptr(out), lo, _ptr(seq_starts),
         _ptr(kv_lens), float(cache.head_dim ** -0.5 if scale is None else scale), _ptr(mask), mask_ld, _ptr(lse),
-        int(bool(accumulate)), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+        int(bool(accumulate)), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream, dev)))
 
 
 def domino_paged_evict_workspace_bytes(cache: PagedCache, max_len, budget) -> int:
@@ -591,7 +592,7 @@ def domino_paged_evict(cache: PagedCache, kv_lens, new_lens, max_len, budget, wo
     _check(load().domino_paged_evict(
         cache.ref, _ptr(kv_lens), _ptr(new_lens), int(max_len), int(budget), int(sink), int(recent), _ptr(new_table),
         0 if new_table is None else new_table.shape[1], _ptr(kept), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream(stream)))
+        workspace.numel() * workspace.element_size(), _stream(stream, dev)))
 
 
 def domino_paged_commit(cache: PagedCache, n_nodes, ctx_lens, accept_len, accepted_nodes, new_ctx_lens, workspace,
@@ -608,7 +609,7 @@ def domino_paged_commit(cache: PagedCache, n_nodes, ctx_lens, accept_len, accept
     _check_device(dev, workspace)
     _check(load().domino_paged_commit(
         cache.ref, int(n_nodes), depth, _ptr(ctx_lens), _ptr(accept_len), _ptr(accepted_nodes), _ptr(new_ctx_lens),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream, dev)))
 
 
 def domino_build_tree(topk_ids, anchor, ctx_lens, node_token, node_parent, node_depth, node_pos,

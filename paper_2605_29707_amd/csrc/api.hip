@@ -1667,6 +1667,7 @@ domino_status domino_paged_attention(const domino_paged_cache *cache, int32_t la
   a.mask_ld = mask_ld;
   a.scale = scale;
   a.lse = lse ? lse : (accumulate ? (float *)(ws + w.lse) : nullptr);
+  a.run_shift = w.plan.run_shift;
   a.part_ml = w.plan.splits > 1 ? (float *)(ws + w.ml) : nullptr;
   a.part_o = w.plan.splits > 1 ? (float *)(ws + w.o) : nullptr;
   a.scores = w.plan.scores_steps ? (float *)(ws + w.scores) : nullptr;

@@ -393,6 +393,7 @@ struct PagedAttnArgs {
   int64_t mask_ld;
   float scale;
   float *lse;        // [tokens][nq] or null (needed with accumulate)
+  int run_shift;     // a sequence is cut into 2^run_shift runs where that makes them shorter than the launch's
   float *part_o;     // [splits][tokens][nq][dh], null: one split
   float *part_ml;    // [splits][tokens][nq][2]: maximum (base 2) and sum
   float *scores;     // [batch][n_kv][scores_steps][scores_rows][32] base-2 scores, where the weights come from them
@@ -406,6 +407,7 @@ struct PagedAttnPlan {
   int rows;        // query rows (new tokens x query heads of a kv head) of a workgroup's tile
   long tiles;      // tiles that hold rows, at most
   int splits, run; // a sequence's slots are cut into runs of `run`
+  int run_shift;   // or into 2^run_shift shorter ones
   int scores_steps, scores_rows;  // steps 0: no scores are kept
   int parts;       // workgroups that share a slab of slots, for the weights from k
   long part_w;     // and the sums that they leave

@@ -2,6 +2,7 @@
 //   o_r = sum_s p_rs v_s,  p_rs = exp(scale q_r k_s - lse_r) over the slots s that row r sees
 // Rows are the new tokens of a sequence times the query heads of one kv head: row i G + h.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "mfma.h"
@@ -54,6 +55,17 @@ DEVI bool find_tile(const PagedAttnArgs &a, int tile, int M, int32_t *err, Tile 
   }
   return found;
 }
+
+// The length of a sequence's runs, a multiple of `whole` slots: the launch's, or shorter where the sequence is so much shorter than max_len that
+// 2^run_shift runs of it (as many as give each CU two workgroups) are.  A caller that captures a graph gives the longest length that it will ever have.
+DEVI int run_of(const PagedAttnArgs &a, int len, int run, int whole) {
+  const int part = (len + (1 << a.run_shift) - 1) >> a.run_shift;  // (len < 2^30, run_shift at most 7)
+  return min(run, (part + whole - 1) & ~(whole - 1));
+}
+
+// The run of the at-th workgroup of a kv head.  Tiles' first runs, the ones that short sequences have, are an odd number of workgroups
+// apart: workgroups are handed to the CUs in turn, and 64 sequences of 2000 slots in a launch for 32768, 16 apart, took 249 us (106 by themselves).
+DEVI int split_of(int at, int tile, int splits) { return (splits & 1 ? at : at + tile) % splits; }
 
 // Operands of the two products.  Scores: S^T = K Q^T in tiles of 16 slots x 16 rows, lane (g, r) = 16 g + r with
 // the scores of row r and slots 4 g .. 4 g + 3.  That is the second operand of O^T = V^T P^T as it stands,
@@ -217,9 +229,10 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
   __shared__ __align__(16) char lds[MERGE > VBYTES ? MERGE : VBYTES];
   __shared__ float s_m[kPaWaves][M], s_l[kPaWaves][M];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
-  const int kvh = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % splits;
+  const int kvh = blockIdx.x % a.c.n_kv, tile = blockIdx.x / a.c.n_kv / splits, split = split_of(blockIdx.x / a.c.n_kv, tile, splits);
   Tile t;
-  if (!find_tile(a, blockIdx.x / a.c.n_kv / splits, M, blockIdx.x == gridDim.x - 1 ? a.err : nullptr, t)) return;
+  if (!find_tile(a, tile, M, blockIdx.x == gridDim.x - 1 ? a.err : nullptr, t)) return;
+  run = run_of(a, t.s.len, run, kPaWaves * kPaStep);
   const int k0 = split * run, k1 = min(t.vis, k0 + run);
   if (k0 >= k1) return;
   const int G = a.nq / a.c.n_kv, n0 = t.s.len - t.s.n;
@@ -475,9 +488,10 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
   __shared__ __align__(16) char s_k[2][TILE], s_v[2][TILE];
   __shared__ uint64_t s_odd[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, r = lane & 31;
-  const int kvh = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % splits;
+  const int kvh = blockIdx.x % a.c.n_kv, tile = blockIdx.x / a.c.n_kv / splits, split = split_of(blockIdx.x / a.c.n_kv, tile, splits);
   Tile t;
-  if (!find_tile(a, blockIdx.x / a.c.n_kv / splits, kChunkRows, blockIdx.x == gridDim.x - 1 ? a.err : nullptr, t)) return;
+  if (!find_tile(a, tile, kChunkRows, blockIdx.x == gridDim.x - 1 ? a.err : nullptr, t)) return;
+  run = run_of(a, t.s.len, run, kChunkStep);
   const int k0 = split * run, k1 = min(t.vis, k0 + run);
   if (k0 >= k1) return;
   const int G = a.nq / a.c.n_kv, n0 = t.s.len - t.s.n;
@@ -733,6 +747,7 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, i
   int b;
   SeqRange s;
   if (!seq_of_token(a.starts, a.lens, a.c.batch, tok, a.tokens, a.max_new, a.max_len, nullptr, b, s)) return;
+  run = run_of(a, s.len, run, M == kChunkRows ? kChunkStep : kPaWaves * kPaStep);
   const int row = (tok - s.start) * G + head % G, last = (min((row / M + 1) * M, s.n * G) - 1) / G;
   const int vis = a.mask ? s.len : s.len - s.n + last + 1, runs = (vis + run - 1) / run;
   const int64_t step = (int64_t)a.tokens * a.nq;
@@ -815,7 +830,7 @@ __global__ __launch_bounds__(256) void paged_weights_of_scores_kernel(PagedAttnA
       const float ls = a.lse[row] * kLog2e;
       const floatx4 x = *(const floatx4 *)(scores_at(a, b, kvh, slot, i * G + h) + slot % 32);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += ls == -INFINITY ? 0.f : fast_exp2(x[e] - ls);
+      for (int e = 0; e < 4; ++e) sum[e] += ls == -INFINITY || x[e] == -INFINITY ? 0.f : fast_exp2(x[e] - ls);  // (a hidden slot, also where lse is NaN)
     }
   if (a.c.page_shift >= 2 && slot + 4 <= s.len) {
     const int page = page_of(a.c, b, slot);
@@ -1054,16 +1069,32 @@ PagedAttnPlan plan_paged_attn(bool bf16, int tokens, int batch, int nq, int n_kv
   if (accumulate && bf16 && !p.scores_steps && slabs < 512)
     p.parts = (int)std::min((511 + slabs) / slabs, std::min(16L, ((long)max_new * G + 63) / 64));
   p.part_w = p.parts > 1 ? slabs * kWeightSlots * p.parts : 0;
-  // Runs of whole steps (a workgroup's 128 slots or 64), as few as give each CU two workgroups (one sequence of 8192 slots 17.8 us, 22.8 with runs of
-  // 128; 64 of 1000 54 us, 65 with 128).  With few rows runs of more than 1024 are cut further, so that sequences of different
-  // lengths end together (64 of 4096 to 16385 slots, weights and all: 622 us, 681 in runs of 8320).
-  const long groups = p.tiles * n_kv, target = 512;
+  // A sequence is cut into runs of whole steps (a workgroup's 128 slots or 64), as few as give each CU two workgroups (one where the
+  // products of 32 fp32 rows bound them: a tree of 61 nodes over 4000 slots 54 us in 4 runs, 63 in 8).
+  const long groups = p.tiles * n_kv, target = p.rows == 32 ? 256 : 512;
   const int whole = p.rows == kChunkRows ? kChunkStep : 128, pieces = (int)(((long)max_len + whole - 1) / whole);
-  long want = (target - 1 + groups) / groups;
+  long want = std::min((target - 1 + groups) / groups, (long)pieces);
+  if (p.rows == 16) {
+    // The join takes 32 runs in one round (one sequence of 8000 slots 14.7 us in 32 runs, 17.8 in 63), and a wave's two or
+    // four steps less than the join does (32 sequences of 250 slots 10.3 us, 14.1 in two runs).
+    want = pieces <= (bf16 ? 4 : 2) ? 1 : std::min(want, 32L);
+  } else {
+    // Each run costs a row's fp32 sums, written and read (0.5 ns), a step 1.3 us (4 of fp32): together least at sqrt(steps x 2600 / rows) runs;
+    // halved from `want` to within a factor of sqrt(2) of that, so that workgroups still fill the CUs evenly.  Two trees of 500 nodes
+    // 21 us in one run, 44 in two; one of 61 over 4000 slots 26 in 8, 30 in 32.
+    const double best = std::sqrt((bf16 ? 2600. : 8000.) * pieces / ((double)tokens * nq));
+    while (want > 1 && want > 1.414 * best) want = (want + 1) / 2;
+    if (want > 8 && want < 12) want = 8;  // (what a wave of the join takes in one round)
+  }
+  const long fill = want;
+  // With few rows runs of more than 1024 are cut further, so that sequences of different
+  // lengths end together (64 of 4096 to 16385 slots, weights and all: 622 us, 681 in runs of 8320).
   if (p.rows == 16) want = std::max(want, std::min((8191 + groups) / groups, (long)max_len / 1024));
   const int splits = (int)std::min(want, (long)std::min(pieces, 128));
   p.run = (pieces + splits - 1) / splits * whole;
   p.splits = (int)(((long)max_len + p.run - 1) / p.run);
+  p.run_shift = 0;
+  while ((2L << p.run_shift) <= std::min(fill, (long)p.splits)) ++p.run_shift;
   return p;
 }
 
@@ -1084,7 +1115,8 @@ static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t 
     if (p.rows == 32 && one_page) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, true>), grid, block, 0, st, a, p.splits, p.run);
     else if (p.rows == 32) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, false>), grid, block, 0, st, a, p.splits, p.run);
   }
-  if (p.splits > 8)
+  // (rows of 128 runs: one sequence's next token 32 runs 14.7 us by four waves a row, 21.5 by one; 6400 rows 12 runs 102 and 94)
+  if (p.splits > 8 && (long)a.tokens * a.nq <= 128L * p.splits)
     hipLaunchKernelGGL((paged_attn_join_kernel<T, DH, 4>), dim3((unsigned)((long)a.tokens * a.nq)), block, 0, st, a, p.rows, p.run);
   else if (p.splits > 1)
     hipLaunchKernelGGL((paged_attn_join_kernel<T, DH, 1>), dim3((unsigned)(((long)a.tokens * a.nq + 3) / 4)), block, 0, st, a, p.rows, p.run);

@@ -176,6 +176,19 @@ def test_one_kv_head_for_many_query_heads():
         check_attention(c, tokens(sum(news), 160, 128, "bf16", 3), news, [90, 300], accumulate=True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news", [[1, 1, 1, 1], [3, 0, 1, 4], [70, 1, 2, 33]])
+@pytest.mark.parametrize("nq,nkv", [(4, 1), (4, 4), (32, 1)])
+def test_lengths_far_below_the_limit(dtype, news, nq, nkv):
+    """max_len as a captured graph has it: sequences are a small part of it, and cut into other runs than the longest would be."""
+    lens = [1100, 1, 129, 640]
+    c = Pages(lens, page=16, nkv=nkv, dh=64, dtype=dtype, weights=True, seed=nkv, room=20000)
+    q = tokens(sum(news), nq, 64, dtype, 2, scale=2.0)
+    check_attention(c, q, news, lens, max_new=80, max_len=20000, accumulate=True)
+    mask = (torch.rand(sum(news), 80, generator=torch.Generator().manual_seed(3)) < 0.4).to(torch.uint8)
+    check_attention(c, q, news, lens, max_new=max(news), max_len=20000, accumulate=True, mask=mask.to(DEV))
+
+
 def test_rows_before_the_first_sequence():
     c = Pages([40, 9], page=8, nkv=2, dh=64)
     x, ws = tokens(9, 8, 64, "bf16", 1), c.workspace(1 << 20)
@@ -251,6 +264,29 @@ def test_what_is_hidden_may_be_anything(dtype, ctx, new):
     out, _ = check_visible(c, q, news, lens, last)
     # ... and rows that see them are NaN
     assert torch.isnan(out[last:]).any(-1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("new", [3, 40])
+def test_a_row_of_nan_gives_nothing_to_what_it_does_not_see(dtype, masked, new):
+    """The weights of the slots that it sees become NaN, those of later tokens are what the other rows give."""
+    c = Pages([50 + new], page=8, nkv=2, dh=64, dtype=dtype, weights=True, stale="", seed=new)
+    q = tokens(new, 4, 64, dtype, 1)
+    slots = np.arange(50 + new)
+    pg, r = po.cells(c.table, 0, slots, 8)
+    mask = torch.tril(torch.ones(new, new, dtype=torch.uint8)).to(DEV) if masked else None
+    ws = c.workspace(bd.domino_paged_attention_workspace_bytes(c.cache, new, 4, new, 50 + new, True))
+    starts, lens, out, got = i32([0, new]), i32([50 + new]), torch.empty_like(q), []
+    for bad in (False, True):
+        c.w.zero_()
+        if bad:
+            q[1] = float("nan")
+        bd.domino_paged_attention(c.cache, q, out, starts, lens, new, 50 + new, ws, mask=mask, accumulate=True)
+        no_error(ws)
+        got.append(c.w[0].cpu().numpy()[pg, :, r])
+    assert np.isnan(got[1][:52]).all() and np.array_equal(got[1][52:], got[0][52:])
+    assert torch.isnan(out[1]).all() and not torch.isnan(out[[0, 2]]).any()
 
 
 def check_visible(c, q, news, lens, rows):
