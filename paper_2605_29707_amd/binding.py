@@ -165,12 +165,11 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream(stream, device=None):
-    """device: the current one, where the caller knows it."""
+def _stream(stream):
     if stream is None:
         import torch
         # the handle alone: a Stream object costs 3 us, as much as a launch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -364,7 +363,7 @@ def _rows(logits):
 
 def _check_array(name, t, device, dtype, n):
     """An optional per-row array: dense, of `dtype`, n elements, on the logits' device (an index, -1 a CPU's)."""
-    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device):
+    if t is not None and (t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device):
         raise DominoError(DOMINO_ERR_INVALID_ARG,
                           f"{name} must be a contiguous {dtype} tensor of {n} elements on the logits' device")
 
@@ -477,6 +476,7 @@ class PagedCache:
         if weights is not None and tuple(weights.shape[-3:]) != (pages, nkv, size):
             raise bad("weights must be [layers, pages, n_kv, page_size]")
         self.k, self.v, self.page_table, self.weights, self.device, self.dtype = k, v, page_table, weights, dev, k.dtype
+        self.int32, self.torch_c = torch.int32, torch._C
         self.n_layers, self.page_size, self.n_kv, self.head_dim, self.batch = layers, size, nkv, dh, page_table.shape[0]
         self.struct = domino_paged_cache(
             k=_ptr(k), v=_ptr(v), weights=_ptr(weights), page_table=_ptr(page_table), layer_stride=strides[0],
@@ -484,6 +484,16 @@ class PagedCache:
             page_size=size, n_kv_heads=nkv, head_dim=dh, batch=page_table.shape[0], max_pages=page_table.shape[1],
             dtype=DOMINO_BF16 if k.dtype is torch.bfloat16 else DOMINO_F32)
         self.ref = C.byref(self.struct)
+
+
+def _launch(cache: PagedCache, workspace, stream):
+    """(workspace, its bytes, stream) of a call on the cache's device, which has to be the current one."""
+    dev, capi = cache.device, cache.torch_c
+    if dev < 0 or dev != capi._cuda_getDevice():
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "the cache must be on the current GPU")
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise DominoError(DOMINO_ERR_INVALID_ARG, "workspace must be a contiguous tensor on the cache's device")
+    return workspace.data_ptr(), workspace.nbytes, capi._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
 
 def _heads(cache: PagedCache, name, t, tokens=None, heads=None):
@@ -513,8 +523,7 @@ def domino_paged_append(cache: PagedCache, q, k, v, q_out, seq_starts, kv_lens, 
                         stream=None):
     """q, q_out [tokens, n_q, head_dim], k, v [tokens, n_kv, head_dim]; frequencies fp64 on the device, two elements of a
     head for each."""
-    import torch
-    dev, i32 = cache.device, torch.int32
+    dev, i32 = cache.device, cache.int32
     n, nq, lq = _heads(cache, "q", q)
     _, _, lk = _heads(cache, "k", k, n, cache.n_kv)
     _, _, lv = _heads(cache, "v", v, n, cache.n_kv)
@@ -523,15 +532,14 @@ def domino_paged_append(cache: PagedCache, q, k, v, q_out, seq_starts, kv_lens, 
     _check_array("kv_lens", kv_lens, dev, i32, cache.batch)
     _check_array("positions", positions, dev, i32, n)
     if frequencies is not None:
+        import torch
         _check_array("frequencies", frequencies, dev, torch.float64, frequencies.numel())
     _check_array("q_norm", q_norm, dev, cache.dtype, cache.head_dim)
     _check_array("k_norm", k_norm, dev, cache.dtype, cache.head_dim)
-    _check_device(dev, workspace)
     _check(load().domino_paged_append(
-        cache.ref, int(layer), n, nq, _ptr(q), lq, _ptr(k), lk, _ptr(v), lv, _ptr(q_out), lo, _ptr(seq_starts),
+        cache.ref, int(layer), n, nq, q.data_ptr(), lq, k.data_ptr(), lk, v.data_ptr(), lv, q_out.data_ptr(), lo, _ptr(seq_starts),
         _ptr(kv_lens), _ptr(positions), _ptr(frequencies), 0 if frequencies is None else 2 * frequencies.numel(),
-        int(bool(interleaved)), float(rope_scale), _ptr(q_norm), _ptr(k_norm), float(rms_eps), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream(stream, dev)))
+        int(bool(interleaved)), float(rope_scale), _ptr(q_norm), _ptr(k_norm), float(rms_eps), *_launch(cache, workspace, stream)))
 
 
 def domino_paged_attention_workspace_bytes(cache: PagedCache, tokens, n_q_heads, max_new, max_len, accumulate=False) -> int:
@@ -546,14 +554,15 @@ def domino_paged_attention(cache: PagedCache, q, out, seq_starts, kv_lens, max_n
                            mask=None, lse=None, accumulate=False, stream=None):
     """q, out [tokens, n_q, head_dim]; scale None: head_dim ** -0.5; mask uint8 or bool with dense rows, [tokens, >= max_new]
     or [batch, n, n] of sequences that all have n new tokens; lse fp32 [tokens, n_q]."""
-    import torch
-    dev, i32 = cache.device, torch.int32
+    dev, i32 = cache.device, cache.int32
     n, nq, lq = _heads(cache, "q", q)
     _, _, lo = _heads(cache, "out", out, n, nq)
     _check_array("seq_starts", seq_starts, dev, i32, cache.batch + 1)
     _check_array("kv_lens", kv_lens, dev, i32, cache.batch)
-    _check_array("lse", lse, dev, torch.float32, n * nq)
     mask_ld = 0
+    if lse is not None or mask is not None:
+        import torch
+        _check_array("lse", lse, dev, torch.float32, n * nq)
     if mask is not None:
         if mask.dim() == 3 and mask.is_contiguous():
             mask = mask.view(-1, mask.shape[2])
@@ -562,11 +571,10 @@ def domino_paged_attention(cache: PagedCache, q, out, seq_starts, kv_lens, max_n
             raise DominoError(DOMINO_ERR_INVALID_ARG,
                               "mask must be uint8 or bool rows of at least max_new, one for each token, on the cache's device")
         mask_ld = mask.stride(0) if n > 1 else mask.shape[1]
-    _check_device(dev, workspace)
     _check(load().domino_paged_attention(
-        cache.ref, int(layer), n, nq, int(max_new), int(max_len), _ptr(q), lq, _ptr(out), lo, _ptr(seq_starts),
+        cache.ref, int(layer), n, nq, int(max_new), int(max_len), q.data_ptr(), lq, out.data_ptr(), lo, _ptr(seq_starts),
         _ptr(kv_lens), float(cache.head_dim ** -0.5 if scale is None else scale), _ptr(mask), mask_ld, _ptr(lse),
-        int(bool(accumulate)), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream, dev)))
+        int(bool(accumulate)), *_launch(cache, workspace, stream)))
 
 
 def domino_paged_evict_workspace_bytes(cache: PagedCache, max_len, budget) -> int:
@@ -579,8 +587,7 @@ def domino_paged_evict_workspace_bytes(cache: PagedCache, max_len, budget) -> in
 def domino_paged_evict(cache: PagedCache, kv_lens, new_lens, max_len, budget, workspace, sink=0, recent=0, new_table=None,
                        kept=None, stream=None):
     """new_table int32 [batch, pages]; kept int32 [layers, batch, n_kv, budget]."""
-    import torch
-    dev, i32 = cache.device, torch.int32
+    dev, i32 = cache.device, cache.int32
     _check_array("kv_lens", kv_lens, dev, i32, cache.batch)
     _check_array("new_lens", new_lens, dev, i32, cache.batch)
     _check_array("kept", kept, dev, i32, cache.n_layers * cache.batch * cache.n_kv * int(budget))
@@ -588,17 +595,14 @@ def domino_paged_evict(cache: PagedCache, kv_lens, new_lens, max_len, budget, wo
         if new_table.dim() != 2:
             raise DominoError(DOMINO_ERR_INVALID_ARG, "new_table must be [batch, pages]")
         _check_array("new_table", new_table, dev, i32, cache.batch * new_table.shape[1])
-    _check_device(dev, workspace)
     _check(load().domino_paged_evict(
         cache.ref, _ptr(kv_lens), _ptr(new_lens), int(max_len), int(budget), int(sink), int(recent), _ptr(new_table),
-        0 if new_table is None else new_table.shape[1], _ptr(kept), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream(stream, dev)))
+        0 if new_table is None else new_table.shape[1], _ptr(kept), *_launch(cache, workspace, stream)))
 
 
 def domino_paged_commit(cache: PagedCache, n_nodes, ctx_lens, accept_len, accepted_nodes, new_ctx_lens, workspace,
                         stream=None):
-    import torch
-    dev, i32 = cache.device, torch.int32
+    dev, i32 = cache.device, cache.int32
     if accepted_nodes.dim() != 2:
         raise DominoError(DOMINO_ERR_INVALID_ARG, "accepted_nodes must be [batch, max_depth]")
     depth = accepted_nodes.shape[1]
@@ -606,10 +610,9 @@ def domino_paged_commit(cache: PagedCache, n_nodes, ctx_lens, accept_len, accept
     _check_array("accept_len", accept_len, dev, i32, cache.batch)
     _check_array("accepted_nodes", accepted_nodes, dev, i32, cache.batch * depth)
     _check_array("new_ctx_lens", new_ctx_lens, dev, i32, cache.batch)
-    _check_device(dev, workspace)
     _check(load().domino_paged_commit(
-        cache.ref, int(n_nodes), depth, _ptr(ctx_lens), _ptr(accept_len), _ptr(accepted_nodes), _ptr(new_ctx_lens),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream, dev)))
+        cache.ref, int(n_nodes), depth, _ptr(ctx_lens), _ptr(accept_len), accepted_nodes.data_ptr(), _ptr(new_ctx_lens),
+        *_launch(cache, workspace, stream)))
 
 
 def domino_build_tree(topk_ids, anchor, ctx_lens, node_token, node_parent, node_depth, node_pos,

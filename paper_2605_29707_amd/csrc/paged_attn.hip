@@ -1122,8 +1122,9 @@ static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t 
     if (p.rows == 32 && one_page) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, true>), grid, block, 0, st, a, p.splits, p.run);
     else if (p.rows == 32) hipLaunchKernelGGL((paged_attn_kernel<T, DH, 2, MASKED, false>), grid, block, 0, st, a, p.splits, p.run);
   }
-  // (rows of 128 runs: one sequence's next token 32 runs 14.7 us by four waves a row, 21.5 by one; 6400 rows 12 runs 102 and 94)
-  if (p.splits > 8 && (long)a.tokens * a.nq <= 128L * p.splits)
+  // Four waves a row where rows are few beside the runs (one sequence's next token, 32 runs: 14.7 us, 21.5 with one wave a row; 64 of them, 15 runs:
+  // 9.1 and 11.1; 6400 rows of a chunk in 12 runs 102 and 94).
+  if (p.splits > 8 && (long)a.tokens * a.nq <= (p.rows == 16 ? 256L : 128L) * p.splits)
     hipLaunchKernelGGL((paged_attn_join_kernel<T, DH, 4>), dim3((unsigned)((long)a.tokens * a.nq)), block, 0, st, a, p.rows, p.run);
   else if (p.splits > 1)
     hipLaunchKernelGGL((paged_attn_join_kernel<T, DH, 1>), dim3((unsigned)(((long)a.tokens * a.nq + 3) / 4)), block, 0, st, a, p.rows, p.run);
