@@ -493,28 +493,48 @@ __global__ __launch_bounds__(kSelThreads) void paged_evict_phase_kernel(PagedEvi
       prefix = state[phase - 2].x;
       need = state[phase - 2].y;
     }
-    for (int i = threadIdx.x; i < 2048; i += kSelThreads) {  // the digit that the last phase counted
-      uint32_t sum = 0;
-      for (int x = 0; x < used; ++x) sum += counted[(size_t)x * 2048 + i];
-      hist[i] = sum;
+    // the digit that the last phase counted: all slices' counts, and of them this slice's, or in the end those of the slices before.
+    // (Eight slices' loads at a time, of both digits: one by one they took 5 us of a phase's 12.5, 11 of the last one's 19.)
+    constexpr int PER = 2048 / kSelThreads, U = 8;
+    uint32_t all[PER] = {}, part[PER] = {};
+    for (int x0 = 0; x0 < used; x0 += U) {
+      uint32_t v[U][PER];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < PER; ++k) v[u][k] = counted[(size_t)min(x0 + u, used - 1) * 2048 + k * kSelThreads + threadIdx.x];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = x0 + u;
+        const bool mine = phase < 3 ? x == slice : x < slice;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+          all[k] += x < used ? v[u][k] : 0;
+          part[k] += x < used && mine ? v[u][k] : 0;
+        }
+      }
     }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) hist[k * kSelThreads + threadIdx.x] = all[k];
     __syncthreads();
     next_digit(hist, phase - 1, prefix, need);
     if (slice == 0 && threadIdx.x == 0 && phase < 3) state[phase - 1] = make_uint2(prefix, need);
     const int bin = prefix & ((1u << digit_bits(phase - 1)) - 1);
-    // keys above it: this slice's, or in the end those of the slices before
+    __shared__ uint32_t s_equal;
     uint32_t above = 0;
-    for (int x = phase < 3 ? slice : 0; x < (phase < 3 ? slice + 1 : slice); ++x)
-      for (int i = threadIdx.x; i < 2048; i += kSelThreads) above += i > bin ? counted[(size_t)x * 2048 + i] : 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int i = k * kSelThreads + threadIdx.x;
+      above += i > bin ? part[k] : 0;
+      if (i == bin) s_equal = part[k];
+    }
+    if (phase == 3)
+      for (int x = threadIdx.x; x < slice; x += kSelThreads) above += sums[x];
     above = block_sum(above);
     if (phase < 3) {
       if (threadIdx.x == 0) sums[slice] = (phase == 1 ? 0 : sums[slice]) + above;
     } else {
-      before.x = above;
-      for (int x = 0; x < slice; ++x) {
-        before.x += sums[x];
-        before.y += counted[(size_t)x * 2048 + bin];
-      }
+      before = make_uint2(above, s_equal);
     }
   }
   if (phase < 3) {

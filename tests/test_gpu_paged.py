@@ -375,6 +375,26 @@ def test_evict_long(page, values, new_pages):
         np.testing.assert_array_equal(got, want)
 
 
+@pytest.mark.parametrize("values", ["random", "few"])
+def test_evict_ten_slices(values):
+    """More slices than a phase adds up at a time."""
+    lens, budget = [150001, 1 << 17, 2000], 20001
+    c = Pages(lens, page=256, nkv=1, dh=64, weights=True, stale="", seed=1)
+    if values == "few":
+        c.w.copy_(torch.randint(0, 3, c.w.shape, generator=torch.Generator().manual_seed(9)))
+    k, v, w = c.copies()
+    want_lens, want_kept = po.evict(k, v, w, c.table, np.asarray(lens), budget, 3, 777, None)
+    kept, out = torch.full((1, 3, 1, budget), 9, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    ws = c.workspace(bd.domino_paged_evict_workspace_bytes(c.cache, 150001, budget)).fill_(77)
+    ws[:16] = 0
+    bd.domino_paged_evict(c.cache, i32(lens), out, 150001, budget, ws, sink=3, recent=777, kept=kept)
+    no_error(ws)
+    np.testing.assert_array_equal(out.cpu().numpy(), want_lens)
+    np.testing.assert_array_equal(kept.cpu().numpy(), want_kept)
+    for got, want in zip(c.copies(), (k, v, w)):
+        np.testing.assert_array_equal(got, want)
+
+
 @pytest.mark.parametrize("dtype,dh,order,page,weights", [("bf16", 128, "slot", 16, True), ("bf16", 64, "head", 1, False),
                                                           ("f32", 128, "head", 32, True), ("f32", 64, "slot", 8, True)])
 @pytest.mark.parametrize("nodes,depth", [(61, 15), (16, 15), (2, 1), (1024, 63)])
