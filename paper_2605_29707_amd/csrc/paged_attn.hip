@@ -488,7 +488,7 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
 constexpr int kChunkRows = 128, kChunkStep = 64;
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-// PAGES, how a step's 64 slots lie in pages: 2, in one; 1, those of a wave's load (64 / (items a row) neighbours) do; 0, anyhow.
+// PAGES, how a step's 64 slots lie in pages: 3, in one; 2, in two of 32; 1, those of a wave's load (64 / (items a row) neighbours) in one; 0, anyhow.
 template <int DH, bool MASKED, int PAGES>
 __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, int splits, int run) {
   constexpr int RB = DH * 2, CH = RB / 16, KST = DH / 16, DT = DH / 32, LPT = kChunkStep * CH / 256, TILE = kChunkStep * RB;
@@ -520,15 +520,15 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
 
   // This thread's items of a step: 16 bytes of row (tid + 256 i) / CH.  Where a load's rows lie in one page its address is a scalar and
   // a lane's offset, and the page's number is loaded a step before the rows.
-  constexpr int NEAR = 64 / CH, LOOKS = PAGES == 2 ? 1 : LPT;
+  constexpr int NEAR = 64 / CH, EACH = PAGES >= 2 ? (PAGES == 3 ? kChunkStep : 32) : 256 / CH, LOOKS = kChunkStep / EACH;  // rows a page number is for
   const int my_row = tid / CH, my_col = tid % CH;
-  const uint32_t lane_at = PAGES ? (uint32_t)(PAGES == 2 ? my_row : lane / CH) * (uint32_t)a.c.slot_stride * 2 + my_col * 16 : 0;
+  const uint32_t lane_at = PAGES ? (uint32_t)(PAGES >= 2 ? my_row : lane / CH) * (uint32_t)a.c.slot_stride * 2 + my_col * 16 : 0;
   bool lost = false;
   u32x4 kr[LPT], vr[LPT];
   int ahead[LOOKS];
   // the first slot of a load's rows; behind the run, of the last one
   auto first_of = [&](int kt, int i) {
-    return PAGES == 2 ? min(kt, (k1 - 1) & ~(kChunkStep - 1)) : min(kt + wave * NEAR + i * (256 / CH), (k1 - 1) & ~(NEAR - 1));
+    return PAGES >= 2 ? min(kt + i * EACH, (k1 - 1) & ~(EACH - 1)) : min(kt + wave * NEAR + i * EACH, (k1 - 1) & ~(NEAR - 1));
   };
   auto look = [&](int kt) {
     if constexpr (PAGES != 0) {
@@ -541,17 +541,18 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
 #pragma unroll
     for (int i = 0; i < LPT; ++i) {
       if constexpr (PAGES != 0) {
-        if (i < LOOKS) {
-          int page = __builtin_amdgcn_readfirstlane(ahead[i]);
+        constexpr int LOADS = EACH / (256 / CH);  // with one page number
+        if (i % LOADS == 0) {
+          int page = __builtin_amdgcn_readfirstlane(ahead[i / LOADS]);
           if ((unsigned)page >= (unsigned)a.c.n_pages) {
             lost = true;
             page = 0;
           }
-          const int64_t at = slot_offset(a.c, page, first_of(kt, i)) * 2;
+          const int64_t at = slot_offset(a.c, page, first_of(kt, i / LOADS)) * 2;
           kp = kb + at;
           vp = vb + at;
         }
-        const int64_t more = PAGES == 2 ? (int64_t)(i * (256 / CH)) * a.c.slot_stride * 2 : 0;
+        const int64_t more = (int64_t)(i % LOADS * (256 / CH)) * a.c.slot_stride * 2;
         kr[i] = *(const u32x4 *)(kp + more + lane_at);
         vr[i] = *(const u32x4 *)(vp + more + lane_at);
       } else {
@@ -1111,7 +1112,8 @@ static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t 
   if constexpr (sizeof(T) == 2)
     if (p.rows == kChunkRows) {
       const bool small = a.c.slot_stride < (1 << 24);  // a row's offset in its page in 32 bits
-      if (small && a.c.page_shift >= 6) hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED, 2>), grid, block, 0, st, a, p.splits, p.run);
+      if (small && a.c.page_shift >= 6) hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED, 3>), grid, block, 0, st, a, p.splits, p.run);
+      else if (small && a.c.page_shift == 5) hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED, 2>), grid, block, 0, st, a, p.splits, p.run);
       else if (small && a.c.page_shift >= 3) hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED, 1>), grid, block, 0, st, a, p.splits, p.run);
       else hipLaunchKernelGGL((paged_chunk_kernel<DH, MASKED, 0>), grid, block, 0, st, a, p.splits, p.run);
     }

@@ -8,7 +8,7 @@ from test_kernel_resources import kernels  # noqa: F401  (the fixture)
 
 # (name, instantiations, most registers, most scratch): 256 registers leave two waves a SIMD, 128 four
 @pytest.mark.parametrize("pattern,count,regs,spill", [
-    (r"dk::paged_chunk_kernel<", 12, 256, 16),
+    (r"dk::paged_chunk_kernel<", 16, 256, 16),
     (r"dk::paged_chunk_weights_kernel<", 4, 256, 0),
     (r"dk::paged_attn_kernel<bf16_t, \d+, 1", 8, 256, 0),
     (r"dk::paged_evict_(select|phase)_kernel<", 4, 128, 0),
