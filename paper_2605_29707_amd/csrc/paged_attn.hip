@@ -639,11 +639,30 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
     if (kt + kChunkStep > clear) {
 #pragma unroll
       for (int w = 0; w < 4; ++w) odd |= s_odd[buf][w];
+      // the mask of four neighbouring slots at a time, from a place in the row that keeps the load inside of it
+      uint32_t four[8];
+      if (MASKED && t.s.n >= 4) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int first = kt + 32 * (u / 4) + 8 * (u % 4) + 4 * h - n0, from = min(max(first, 0), t.s.n - 4);
+          __builtin_memcpy(&four[u], mrow + from, 4);
+          const int off = min(max(first - from, -4), 4) * 8;  // (bytes of slots before the new ones or behind the last are not looked at)
+          four[u] = (uint32_t)(off < 0 ? (uint64_t)four[u] << -off : (uint64_t)four[u] >> off);
+        }
+      } else if (MASKED) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          four[u] = 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            four[u] |= (uint32_t)mrow[min(max(kt + 32 * (u / 4) + 8 * (u % 4) + 4 * h + c - n0, 0), t.s.n - 1)] << (8 * c);
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
         const int slot = kt + 32 * (e / 16) + 8 * (e % 16 / 4) + 4 * h + e % 4;
         bool seen = slot <= lim;
-        if (MASKED) seen = (slot < n0) | (mrow[max(0, min(slot, t.s.len - 1) - n0)] != 0);
+        if (MASKED) seen = (slot < n0) | ((four[e / 4] >> (8 * (e % 4)) & 0xff) != 0);
         seen &= slot < k1;
         x[e] = seen ? x[e] : -INFINITY;
         dark |= x[e] == -INFINITY ? 1u << e : 0u;
