@@ -496,17 +496,17 @@ def _launch(cache: PagedCache, workspace, stream):
     return workspace.data_ptr(), workspace.nbytes, capi._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
 
-def _heads(cache: PagedCache, name, t, tokens=None, heads=None):
-    """(tokens, heads, token stride) of a [tokens, heads, head_dim] tensor whose tokens' heads are dense."""
-    sh = t.shape
-    if len(sh) != 3 or sh[2] != cache.head_dim or t.dtype is not cache.dtype or t.get_device() != cache.device \
-            or (tokens is not None and sh[0] != tokens) or (heads is not None and sh[1] != heads):
+def _heads(cache: PagedCache, name, t, shape=None):
+    """A [tokens, heads, head_dim] tensor whose tokens' heads are dense: (its shape, token stride)."""
+    sh, dh = t.shape, cache.head_dim
+    if (sh != shape if shape is not None else len(sh) != 3 or sh[2] != dh) or t.dtype is not cache.dtype \
+            or t.get_device() != cache.device:
         raise DominoError(DOMINO_ERR_INVALID_ARG,
                           f"{name} must be [tokens, heads, head_dim] of the cache's type, on its device")
-    (n, h, dh), (ld, lh, one) = sh, t.stride()
-    if one != 1 or (h > 1 and lh != dh):
+    ld, lh, one = t.stride()
+    if one != 1 or (lh != dh and sh[1] > 1):
         raise DominoError(DOMINO_ERR_INVALID_ARG, f"{name} must have dense heads")
-    return n, h, ld if n > 1 else h * dh
+    return sh, ld if sh[0] > 1 else sh[1] * dh
 
 
 def domino_rope_frequencies(rotary_dim, theta, scaling=DOMINO_ROPE_NONE, factor=1.0, original_ctx=0, beta_fast=32.0,
@@ -524,13 +524,15 @@ def domino_paged_append(cache: PagedCache, q, k, v, q_out, seq_starts, kv_lens, 
     """q, q_out [tokens, n_q, head_dim], k, v [tokens, n_kv, head_dim]; frequencies fp64 on the device, two elements of a
     head for each."""
     dev, i32 = cache.device, cache.int32
-    n, nq, lq = _heads(cache, "q", q)
-    _, _, lk = _heads(cache, "k", k, n, cache.n_kv)
-    _, _, lv = _heads(cache, "v", v, n, cache.n_kv)
-    _, _, lo = _heads(cache, "q_out", q_out, n, nq)
+    shape, lq = _heads(cache, "q", q)
+    n, nq, dh = shape
+    own, lk = _heads(cache, "k", k, (n, cache.n_kv, dh))
+    _, lv = _heads(cache, "v", v, own)
+    _, lo = _heads(cache, "q_out", q_out, shape)
     _check_array("seq_starts", seq_starts, dev, i32, cache.batch + 1)
     _check_array("kv_lens", kv_lens, dev, i32, cache.batch)
-    _check_array("positions", positions, dev, i32, n)
+    if positions is not None:
+        _check_array("positions", positions, dev, i32, n)
     if frequencies is not None:
         import torch
         _check_array("frequencies", frequencies, dev, torch.float64, frequencies.numel())
@@ -555,8 +557,9 @@ def domino_paged_attention(cache: PagedCache, q, out, seq_starts, kv_lens, max_n
     """q, out [tokens, n_q, head_dim]; scale None: head_dim ** -0.5; mask uint8 or bool with dense rows, [tokens, >= max_new]
     or [batch, n, n] of sequences that all have n new tokens; lse fp32 [tokens, n_q]."""
     dev, i32 = cache.device, cache.int32
-    n, nq, lq = _heads(cache, "q", q)
-    _, _, lo = _heads(cache, "out", out, n, nq)
+    shape, lq = _heads(cache, "q", q)
+    n, nq, _ = shape
+    _, lo = _heads(cache, "out", out, shape)
     _check_array("seq_starts", seq_starts, dev, i32, cache.batch + 1)
     _check_array("kv_lens", kv_lens, dev, i32, cache.batch)
     mask_ld = 0

@@ -323,36 +323,26 @@ DEVI void slice_count(const Slice &s, int pass, uint32_t prefix, uint32_t *hist)
   __syncthreads();
 }
 
-// From the top digit down: the one where the running count reaches `need`, by 64 groups of 32 and then in one of them; it joins the
-// prefix, and what lies above it leaves `need`.  (All counts together are over `need`: more slots have a choice than stay.)
+// From the top digit down: the one where the running count reaches `need`; it joins the prefix, and what lies above it leaves `need`.
+// A thread has two digits, and the waves' sums meet in LDS.  (All counts together are over `need`: more slots have a choice than stay.)
 DEVI void next_digit(const uint32_t *hist, int pass, uint32_t &prefix, uint32_t &need) {
-  __shared__ uint32_t s_bin, s_above;
-  const int lane = threadIdx.x & 63;
-  if (threadIdx.x < 64) {
-    uint32_t mine = 0;
-    for (int i = 0; i < 32; ++i) mine += hist[2047 - (lane * 32 + ((i + lane) & 31))];  // (rotated: one bank each)
-    auto running = [&](uint32_t v) {
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t u = __shfl_up(v, o, 64);
-        if (lane >= o) v += u;
-      }
-      return v;
-    };
-    const uint32_t incl = running(mine);
-    const int group = max(__ffsll((unsigned long long)__ballot(incl >= need)) - 1, 0);
-    const uint32_t before = __shfl(incl - mine, group, 64);
-    const uint32_t h = lane < 32 ? hist[2047 - (group * 32 + lane)] : 0, upto = before + running(h);
-    const int bin = max(__ffsll((unsigned long long)__ballot(upto >= need)) - 1, 0);
-    if (lane == bin) {
-      s_bin = 2047 - (group * 32 + bin);
-      s_above = upto - h;
-    }
+  static_assert(kSelThreads * 2 == 2048, "two digits a thread");
+  __shared__ uint32_t s_sum[kSelWaves], s_bin, s_above;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, low = 2046 - 2 * (int)threadIdx.x;
+  const uint2 two = *(const uint2 *)(hist + low);
+  const uint32_t mine = two.x + two.y, incl = wave_running_sum(mine);
+  if (lane == 63) s_sum[wave] = incl;
+  __syncthreads();
+  const uint32_t before = __builtin_amdgcn_readlane(wave_running_sum(lane < wave ? s_sum[lane] : 0), 63);
+  const uint32_t upto = before + incl, above = upto - mine;
+  if ((above < need && upto >= need) || (low == 0 && upto < need)) {
+    const bool high = above + two.y >= need;
+    s_bin = low + high;
+    s_above = high ? above : above + two.y;
   }
   __syncthreads();
   prefix = (prefix << digit_bits(pass)) | s_bin;
   need -= s_above;
-  __syncthreads();
 }
 
 // bit masks over the lanes of a step's slots that stay for sure, and of those that equal the last key that does
@@ -440,7 +430,7 @@ __global__ __launch_bounds__(kSelThreads) void paged_evict_select_kernel(PagedEv
   int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
   const int n = a.lens[b];
   if (evict_trivial(a, b, layer == 0 && head == 0, n, kept)) return;
-  __shared__ uint32_t hist[2048];
+  __shared__ __align__(8) uint32_t hist[2048];
   Slice s;
   slice_load<TINY_PAGES>(a, b, layer, head, 0, n, s);
   uint32_t prefix = 0, need = s.m;
@@ -482,7 +472,7 @@ __global__ __launch_bounds__(kSelThreads) void paged_evict_phase_kernel(PagedEvi
   const int n = a.lens[b];
   if (phase == 0 && slice == 0 && evict_trivial(a, b, layer == 0 && head == 0, n, kept)) return;
   if (n <= a.budget || n > a.max_len || slice * kEvictSlice >= n) return;
-  __shared__ uint32_t hist[2048];
+  __shared__ __align__(8) uint32_t hist[2048];
   const int used = (n + kEvictSlice - 1) / kEvictSlice;
   Slice s;
   slice_load<TINY_PAGES>(a, b, layer, head, slice, n, s);
