@@ -554,41 +554,59 @@ DEVI void evict_in_place(const PagedEvictArgs &a, int b, int layer, int head, co
   const PagedView &c = a.c;
   const int tid = threadIdx.x;
   bool lost = false;
-  for (int r0 = 0; r0 < count; r0 += ROWS) {
-    u32x4 v[PER];
-    float w[PER];
-    int64_t to[PER];
+  // where this thread's items of a round are (bytes, or elements of the weights), and go to; -1: they stay.  A round's places are found while
+  // the rows of the one before are on their way: nothing that they follow from is moved.
+  int64_t from[PER], to[PER];
+  auto find = [&](int r0) {
+    int s[PER];
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      s[q] = 0;
+      if (r0 + q * (kMoveThreads / ITEMS) < count) s[q] = kept[min(r0 + (tid + q * kMoveThreads) / ITEMS, count - 1)];
+    }
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
       const int it = tid + q * kMoveThreads, i = r0 + it / ITEMS;
-      to[q] = -1;
-      v[q] = u32x4{0, 0, 0, 0};
-      w[q] = 0.f;
-      if (i >= count) continue;
-      const int s = kept[i];
-      if (s <= i) continue;  // it stays
-      const int pf = page_of(c, b, s), pt = page_of(c, b, i);
+      to[q] = from[q] = -1;
+      if (i >= count || s[q] <= i) continue;  // (its own place: it stays)
+      const int pf = page_of(c, b, s[q]), pt = page_of(c, b, i);
       if (pf < 0 || pt < 0) {
         lost = true;
         continue;
       }
       if (WEIGHTS) {
-        w[q] = c.weights[weight_offset(c, layer, pf, head, s)];
+        from[q] = weight_offset(c, layer, pf, head, s[q]);
         to[q] = weight_offset(c, layer, pt, head, i);
       } else {
         const int64_t col = (slice * kSlice16 + it % ITEMS) * 16;
-        v[q] = *(const u32x4 *)(data + base + slot_offset(c, pf, s) * esz + col);
+        from[q] = base + slot_offset(c, pf, s[q]) * esz + col;
         to[q] = base + slot_offset(c, pt, i) * esz + col;
       }
     }
+  };
+  find(0);
+  for (int r0 = 0; r0 < count; r0 += ROWS) {
+    u32x4 v[PER];
+    float w[PER];
+    int64_t at[PER];
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      v[q] = u32x4{0, 0, 0, 0};
+      w[q] = 0.f;
+      at[q] = to[q];
+      if (at[q] < 0) continue;
+      if (WEIGHTS) w[q] = c.weights[from[q]];
+      else v[q] = *(const u32x4 *)(data + from[q]);
+    }
+    if (r0 + ROWS < count) find(r0 + ROWS);
 #pragma unroll
     for (int q = 0; q < PER; ++q) __asm__ volatile("" ::"v"(v[q]), "v"(w[q]));  // every load has arrived
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
-      if (to[q] < 0) continue;
-      if (WEIGHTS) c.weights[to[q]] = w[q];
-      else *(u32x4 *)(data + to[q]) = v[q];
+      if (at[q] < 0) continue;
+      if (WEIGHTS) c.weights[at[q]] = w[q];
+      else *(u32x4 *)(data + at[q]) = v[q];
     }
     __syncthreads();
   }
