@@ -403,12 +403,11 @@ DEVI void slice_write(const Slice &s, uint32_t prefix, uint32_t need, uint2 befo
 // the waves' sums of the workgroup added up before this one's
 DEVI uint2 sums_before(uint2 mine) {
   __shared__ uint2 s_sum[kSelWaves];
-  const int wave = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 0) s_sum[wave] = mine;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane == 0) s_sum[wave] = mine;
   __syncthreads();
-  uint2 before = make_uint2(0, 0);
-  for (int w = 0; w < wave; ++w) before = make_uint2(before.x + s_sum[w].x, before.y + s_sum[w].y);
-  return before;
+  const uint2 s = lane < wave ? s_sum[lane] : make_uint2(0, 0);
+  return make_uint2(__builtin_amdgcn_readlane(wave_running_sum(s.x), 63), __builtin_amdgcn_readlane(wave_running_sum(s.y), 63));
 }
 
 // Sequences with nothing to choose: new length and kept slots.  True for those.
@@ -446,14 +445,12 @@ __global__ __launch_bounds__(kSelThreads) void paged_evict_select_kernel(PagedEv
 // The sum of `v` over a workgroup's threads.
 DEVI uint32_t block_sum(uint32_t v) {
   __shared__ uint32_t s_v[kSelWaves];
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  const int lane = threadIdx.x & 63;
+  v = wave_running_sum(v);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) s_v[threadIdx.x >> 6] = v;
+  if (lane == 63) s_v[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = 0;
-  for (int w = 0; w < kSelWaves; ++w) v += s_v[w];
-  return v;
+  return __builtin_amdgcn_readlane(wave_running_sum(lane < kSelWaves ? s_v[lane] : 0), 63);
 }
 
 // The same over several slices, phase by phase: 0 to 2 count a digit, 3 writes.  Between them a head's slices leave `parts`
