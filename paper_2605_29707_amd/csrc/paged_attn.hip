@@ -219,7 +219,8 @@ DEVI float *scores_at(const PagedAttnArgs &a, int b, int kvh, int slot, int row)
 constexpr int kPaThreads = 256, kPaWaves = 4, kPaStep = 32;
 
 // A workgroup has a tile of 16 NT rows and a run of slots, a wave every fourth 32 slots of it; the waves' results are
-// joined in LDS.  Bound by the cache's bytes where rows are few.
+// joined in LDS.  Bound by the cache's bytes where rows are few (64 sequences of 4096 to 16385 slots, 32 heads on 8: 500 us, 5.4 TB/s),
+// by the products' rate with 32 fp32 rows.
 template <typename T, int DH, int NT, bool MASKED, bool ONE_PAGE>
 __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a, int splits, int run) {
   using O = Ops<T, DH>;
@@ -484,6 +485,7 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
 // A wave reads every row of k and v from LDS once: as many bytes a clock as the products of 32 rows take.  In both
 // buffers a row's 16-byte items are permuted by the row, so that neither read has bank conflicts: k's 16 rows of one item,
 // v's eight rows of 32 bytes.
+// Bound by the products: 4096 tokens after 12288, 32 heads on 8, 983 to 1069 us by the card, 0.90 to 0.98 PFLOP/s.
 // ---------------------------------------------------------------------------
 constexpr int kChunkRows = 128, kChunkStep = 64;
 typedef float floatx16 __attribute__((ext_vector_type(16)));
@@ -937,7 +939,8 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
 
 // The same for bf16: a workgroup has 256 slots, 64 a wave, whose rows of k stay in registers; the call's rows pass through two LDS
 // buffers 32 at a time (with their lse and the last slot that they see), in order.  Where the slots make few workgroups, `parts` of them
-// share a slab's rows, every parts-th 32, and leave their sums to the next kernel.
+// share a slab's rows, every parts-th 32, and leave their sums to the next kernel.  Bound by the products and their exponentials: 4096 tokens
+// after 12288 take 1814 us in all, 1000 without the weights.
 constexpr int kWeightSlots = 256;
 
 template <int DH, bool MASKED>
