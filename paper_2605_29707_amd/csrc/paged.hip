@@ -543,12 +543,10 @@ __global__ __launch_bounds__(kSelThreads) void paged_evict_phase_kernel(PagedEvi
 // Rows kept[i] move to slot i.  In place, a workgroup has one column slice of one head's keys or values (or the head's
 // weights) and goes up the slots in rounds: kept[i] >= i, so a round writes no slot that a later one reads, and reads all of its own
 // before it writes.  To new pages there is no such order: a workgroup has a stretch of rows (1.97 GB read and written 403 us, 4.9 TB/s).
-constexpr int kSlice16 = 4;  // 16-byte items of a row's slice
-
-template <bool WEIGHTS>
+template <bool WEIGHTS, int SLICE>  // SLICE: 16-byte items of a row's slice
 DEVI void evict_in_place(const PagedEvictArgs &a, int b, int layer, int head, const int32_t *kept, int count, char *data,
                          int64_t base, int esz, int slice) {
-  constexpr int PER = 8, ITEMS = WEIGHTS ? 1 : kSlice16, ROWS = kMoveThreads * PER / ITEMS;
+  constexpr int PER = 8, ITEMS = WEIGHTS ? 1 : SLICE, ROWS = kMoveThreads * PER / ITEMS;
   const PagedView &c = a.c;
   const int tid = threadIdx.x;
   bool lost = false;
@@ -576,7 +574,7 @@ DEVI void evict_in_place(const PagedEvictArgs &a, int b, int layer, int head, co
         from[q] = weight_offset(c, layer, pf, head, s[q]);
         to[q] = weight_offset(c, layer, pt, head, i);
       } else {
-        const int64_t col = (slice * kSlice16 + it % ITEMS) * 16;
+        const int64_t col = (slice * SLICE + it % ITEMS) * 16;
         from[q] = base + slot_offset(c, pf, s[q]) * esz + col;
         to[q] = base + slot_offset(c, pt, i) * esz + col;
       }
@@ -611,19 +609,20 @@ DEVI void evict_in_place(const PagedEvictArgs &a, int b, int layer, int head, co
   if (lost) raise_error(a.err, DEV_BAD_PAGE);
 }
 
+template <int SLICE>
 __global__ __launch_bounds__(kMoveThreads) void paged_evict_in_place_kernel(PagedEvictArgs a) {
   const PagedView &c = a.c;
   const int head = blockIdx.x % c.n_kv, b = (blockIdx.x / c.n_kv) % c.batch, layer = blockIdx.x / c.n_kv / c.batch;
   const int n = a.lens[b];
   if (n <= a.budget || n > a.max_len) return;
   const int32_t *kept = a.kept + (size_t)blockIdx.x * a.budget;
-  const int esz = c.bf16 ? 2 : 4, slices = c.dh * esz / 16 / kSlice16;
+  const int esz = c.bf16 ? 2 : 4, slices = c.dh * esz / 16 / SLICE;
   const int part = blockIdx.y;  // slices of k, slices of v, weights
   const int64_t base = (layer * c.layer_stride + head * c.head_stride) * esz;
   if (part < 2 * slices)
-    evict_in_place<false>(a, b, layer, head, kept, a.budget, part < slices ? c.k : c.v, base, esz, part % slices);
+    evict_in_place<false, SLICE>(a, b, layer, head, kept, a.budget, part < slices ? c.k : c.v, base, esz, part % slices);
   else
-    evict_in_place<true>(a, b, layer, head, kept, a.budget, nullptr, 0, 0, 0);
+    evict_in_place<true, SLICE>(a, b, layer, head, kept, a.budget, nullptr, 0, 0, 0);
 }
 
 __global__ __launch_bounds__(kMoveThreads) void paged_evict_gather_kernel(PagedEvictArgs a) {
@@ -701,8 +700,13 @@ void launch_paged_evict(const PagedEvictArgs &a, hipStream_t st) {
     hipLaunchKernelGGL(paged_evict_gather_kernel, dim3(heads, (min(a.budget, a.max_len) + kEvictMoveRows - 1) / kEvictMoveRows),
                        dim3(kMoveThreads), 0, st, a);
   } else {
-    const int slices = a.c.dh * (a.c.bf16 ? 2 : 4) / 16 / kSlice16;
-    hipLaunchKernelGGL(paged_evict_in_place_kernel, dim3(heads, 2 * slices + 1), dim3(kMoveThreads), 0, st, a);
+    // Narrow slices, whose rounds have more rows, where there are few workgroups: 9000 bf16 slots of 8 heads to 8000 50 us (64 with wide
+    // slices), of 32 heads 77 (72 wide).
+    const int wide = a.c.dh * (a.c.bf16 ? 2 : 4) / 64;
+    if (heads * wide < 128)
+      hipLaunchKernelGGL(paged_evict_in_place_kernel<2>, dim3(heads, 4 * wide + 1), dim3(kMoveThreads), 0, st, a);
+    else
+      hipLaunchKernelGGL(paged_evict_in_place_kernel<4>, dim3(heads, 2 * wide + 1), dim3(kMoveThreads), 0, st, a);
   }
 }
 

@@ -375,6 +375,23 @@ def test_evict_long(page, values, new_pages):
         np.testing.assert_array_equal(got, want)
 
 
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+def test_evict_many_heads_in_place(dtype, dh):
+    """More workgroups than where rows are cut into narrow slices, over several rounds."""
+    lens, budget = [900, 33, 1700, 1300], 1201
+    c = Pages(lens, page=16, nkv=8, dh=dh, dtype=dtype, layers=2, weights=True, stale="", seed=dh)
+    k, v, w = c.copies()
+    want_lens, want_kept = po.evict(k, v, w, c.table, np.asarray(lens), budget, 3, 77, None)
+    kept, out = torch.full((2, 4, 8, budget), 9, dtype=torch.int32, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    ws = c.workspace(bd.domino_paged_evict_workspace_bytes(c.cache, 1700, budget))
+    bd.domino_paged_evict(c.cache, i32(lens), out, 1700, budget, ws, sink=3, recent=77, kept=kept)
+    no_error(ws)
+    np.testing.assert_array_equal(out.cpu().numpy(), want_lens)
+    np.testing.assert_array_equal(kept.cpu().numpy(), want_kept)
+    for got, want in zip(c.copies(), (k, v, w)):
+        np.testing.assert_array_equal(got, want)
+
+
 @pytest.mark.parametrize("values", ["random", "few"])
 def test_evict_ten_slices(values):
     """More slices than a phase adds up at a time."""
