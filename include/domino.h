@@ -515,7 +515,9 @@ domino_status domino_sample_logits(int32_t rows, int32_t vocab, const void *logi
  *                  first sequence and behind the last are left as they are
  *  kv_lens         device int32 [batch]: slots in use, the new tokens' own included (they are
  *                  the last ones).  A sequence whose starts and lengths disagree, or pass the
- *                  limits that the call was given, is left out: DOMINO_DEV_BAD_CTX_LEN
+ *                  limits that the call was given, is left out (its rows, slots and weights are as they were),
+ *                  and so are the first one whose starts go down (seq_starts[b + 1] < seq_starts[b]) and all
+ *                  behind it: DOMINO_DEV_BAD_CTX_LEN
  *  a table entry of a slot in use that is not in [0, n_pages) sets DOMINO_DEV_BAD_PAGE: nothing is
  *                  written to such a slot, and what is read from it is undefined
  *  sequences may share pages that a call only reads; a page that a call writes (weights

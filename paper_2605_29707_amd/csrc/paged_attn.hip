@@ -28,12 +28,16 @@ struct Tile {
 DEVI bool find_tile(const PagedAttnArgs &a, int tile, int M, int32_t *err, Tile &t) {
   const int lane = threadIdx.x & 63, G = a.nq / a.c.n_kv;
   int base = 0;
-  bool found = false;
+  bool found = false, down = false;  // down: from here on sequences are left out (starts_ascend)
   for (int s0 = 0; s0 < a.c.batch && (!found || err); s0 += 64) {
     SeqRange s{0, 0, 0};
     const int i = min(s0 + lane, a.c.batch - 1);
-    const bool live = seq_range(a.starts, a.lens, i, a.tokens, a.max_new, a.max_len, err, s) && s0 + lane < a.c.batch;
+    const int lo = a.starts[i], hi = a.starts[i + 1], len = a.lens[i];
+    bool live = check_range(lo, hi, len, a.tokens, a.max_new, a.max_len, err, s) && s0 + lane < a.c.batch;
     if (found) continue;
+    const uint64_t drops = __ballot(hi < lo);
+    live = live && !down && !(drops & ((1ull << lane) - 1));
+    down |= drops != 0;
     // (a launch has fewer than 2^24 tiles, and `base` stays at most `tile`: nothing passes 32 bits)
     const int n = live ? min((int)(((int64_t)s.n * G + M - 1) / M), 1 << 24) : 0, upto = base + wave_running_sum(n);
     const uint64_t here = __ballot(upto > tile);
@@ -849,8 +853,9 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, i
 __global__ __launch_bounds__(256) void paged_weights_of_scores_kernel(PagedAttnArgs a, int slabs) {
   const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv / slabs;
   const int slot = (blockIdx.x / a.c.n_kv % slabs * 256 + threadIdx.x) * 4;
+  const bool ascend = starts_ascend(a.starts, b);
   SeqRange s;
-  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || slot >= s.len) return;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || !ascend || slot >= s.len) return;
   const int G = a.nq / a.c.n_kv;
   floatx4 sum{0.f, 0.f, 0.f, 0.f};
   for (int i = 0; i < s.n; ++i)
@@ -886,8 +891,9 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
   const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv / slabs;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kt = (blockIdx.x / a.c.n_kv % slabs * kPaWaves + wave) * kPaStep;
+  const bool ascend = starts_ascend(a.starts, b);
   SeqRange s;
-  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || kt >= s.len) return;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || !ascend || kt >= s.len) return;
   const int G = a.nq / a.c.n_kv, n0 = s.len - s.n, rows = s.n * G;
   const int page = page_of(a.c, b, min(kt + (lane & 31), s.len - 1));
   const char *kb = a.c.k + (a.layer * a.c.layer_stride + kvh * a.c.head_stride) * ESZ;
@@ -952,8 +958,9 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_weights_kernel(PagedAttnAr
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, r = lane & 31;
   const int kvh = blockIdx.x % a.c.n_kv, part = blockIdx.x / a.c.n_kv % parts, rest = blockIdx.x / a.c.n_kv / parts;
   const int b = rest / slabs, slab = rest % slabs * kWeightSlots;
+  const bool ascend = starts_ascend(a.starts, b);
   SeqRange s;
-  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || slab >= s.len) return;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || !ascend || slab >= s.len) return;
   s.start = __builtin_amdgcn_readfirstlane(s.start);
   s.n = __builtin_amdgcn_readfirstlane(s.n);
   s.len = __builtin_amdgcn_readfirstlane(s.len);
@@ -1065,8 +1072,9 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_weights_kernel(PagedAttnAr
 __global__ __launch_bounds__(kWeightSlots) void paged_weights_join_kernel(PagedAttnArgs a, int slabs, int parts) {
   const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv / slabs;
   const int slot = blockIdx.x / a.c.n_kv % slabs * kWeightSlots + threadIdx.x;
+  const bool ascend = starts_ascend(a.starts, b);
   SeqRange s;
-  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || slot >= s.len) return;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || !ascend || slot >= s.len) return;
   const int page = page_of(a.c, b, slot);
   if (page < 0) return;
   const float *p = a.part_w + (int64_t)(b * a.c.n_kv + kvh) * parts * slabs * kWeightSlots + slot;
