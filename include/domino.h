@@ -582,7 +582,13 @@ domino_status domino_paged_append(const domino_paged_cache *cache, int32_t layer
                                   int32_t rotary_dim, int32_t interleaved, float rope_scale, const void *q_norm,
                                   const void *k_norm, float rms_eps, void *workspace, size_t workspace_bytes, void *stream);
 
-/* Bytes of workspace domino_paged_attention needs (0 for arguments that it refuses). */
+/*
+ * Bytes of workspace domino_paged_attention needs with these very arguments (0 for arguments that it refuses).  A smaller call
+ * may need far more: few rows are cut into more runs, and their weights come from scores that are kept (batch 64, 32 heads on 8,
+ * max_len 16384, accumulate: 4096 tokens with max_new 4096 0.5 MB, 64 tokens with max_new 1 151 MB, 256 with max_new 4 605 MB).
+ * A workspace for several kinds of call has the greatest of their sizes.  A server whose batches vary asks once for each kind: it
+ * passes the rows that its buffers hold as `tokens` and its limits as max_new and max_len, whatever the sequences have in a call.
+ */
 size_t domino_paged_attention_workspace_bytes(const domino_paged_cache *cache, int32_t tokens, int32_t n_q_heads,
                                               int32_t max_new, int32_t max_len, int32_t accumulate);
 

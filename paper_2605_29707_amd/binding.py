@@ -545,6 +545,8 @@ def domino_paged_append(cache: PagedCache, q, k, v, q_out, seq_starts, kv_lens, 
 
 
 def domino_paged_attention_workspace_bytes(cache: PagedCache, tokens, n_q_heads, max_new, max_len, accumulate=False) -> int:
+    """For these very arguments: a call with fewer tokens or a smaller max_new may need more, so a workspace for several kinds of
+    call has the greatest of their sizes."""
     n = load().domino_paged_attention_workspace_bytes(cache.ref, int(tokens), int(n_q_heads), int(max_new), int(max_len),
                                                       int(bool(accumulate)))
     if n == 0:
