@@ -1696,6 +1696,9 @@ domino_status domino_paged_evict(const domino_paged_cache *cache, const int32_t 
   if (sink < 0 || recent < 0 || (int64_t)sink + recent > budget) return fail(DOMINO_ERR_INVALID_ARG, "sink and recent must be >= 0 and at most budget together");
   if (new_table && (int64_t)new_pages * cache->page_size < budget)
     return fail(DOMINO_ERR_INVALID_ARG, "new_pages * page_size must be at least budget");
+  const int64_t heads = (int64_t)cache->n_layers * cache->batch * cache->n_kv_heads;
+  if (!new_table && heads * evict_in_place_parts(cache->head_dim, cache->dtype == DOMINO_BF16, (int)heads) > kMaxBlocks)
+    return fail(DOMINO_ERR_UNSUPPORTED, "n_layers * batch * n_kv_heads does not fit a launch in place");
   if (domino_status s = check_paged_workspace(workspace, workspace_bytes, domino_paged_evict_workspace_bytes(cache, max_len, budget)); s != DOMINO_OK) return s;
   PagedEvictArgs a;
   a.c = paged_view(cache);

@@ -700,13 +700,9 @@ void launch_paged_evict(const PagedEvictArgs &a, hipStream_t st) {
     hipLaunchKernelGGL(paged_evict_gather_kernel, dim3(heads, (min(a.budget, a.max_len) + kEvictMoveRows - 1) / kEvictMoveRows),
                        dim3(kMoveThreads), 0, st, a);
   } else {
-    // Narrow slices, whose rounds have more rows, where there are few workgroups: 9000 bf16 slots of 8 heads to 8000 50 us (64 with wide
-    // slices), of 32 heads 77 (72 wide).
-    const int wide = a.c.dh * (a.c.bf16 ? 2 : 4) / 64;
-    if (heads * wide < 128)
-      hipLaunchKernelGGL(paged_evict_in_place_kernel<2>, dim3(heads, 4 * wide + 1), dim3(kMoveThreads), 0, st, a);
-    else
-      hipLaunchKernelGGL(paged_evict_in_place_kernel<4>, dim3(heads, 2 * wide + 1), dim3(kMoveThreads), 0, st, a);
+    const int wide = a.c.dh * (a.c.bf16 ? 2 : 4) / 64, parts = evict_in_place_parts(a.c.dh, a.c.bf16, heads);
+    if (parts == 4 * wide + 1) hipLaunchKernelGGL(paged_evict_in_place_kernel<2>, dim3(heads, parts), dim3(kMoveThreads), 0, st, a);
+    else hipLaunchKernelGGL(paged_evict_in_place_kernel<4>, dim3(heads, parts), dim3(kMoveThreads), 0, st, a);
   }
 }
 

@@ -30,3 +30,28 @@ for acc, kinds in ((1, [(4096, 4096), (64, 1), (256, 4)]), (0, [(4096, 4096), (6
         assert attend(*k, acc, max(sizes)) == 0
 assert [round(need(*k, 1) / 1e5) for k in ((4096, 4096), (64, 1), (256, 4))] == [5, 1513, 6051]   # the header's figures, in 0.1 MB
 ''', tmp_path)
+
+
+def test_the_most_heads_fit_a_grid(tmp_path):
+    """Eviction over as many heads as are accepted, in place and to new pages: no grid of 2^32 threads or more; what would need one
+    is refused."""
+    host_stub.run(CACHE + '''
+def check(st):
+    """Launched within the limits, or refused before any launch."""
+    out = [r for r in h.log() if r[0] == "launch"]
+    for r in out:
+        assert int(r[2]) * int(r[3]) * int(r[4]) * int(r[5]) < 2**32 and int(r[3]) <= 65535, r
+    assert (len(out) > 0) == (st == 0) and st in (0, -3), (st, out, bd.last_error())
+    return st == 0
+h.log()
+took = {}
+for dtype in (0, 1):
+    for dh in (64, 128):
+        for layers in (1, 16, 32, 60, 61, 63, 64):
+            for table in (None, F):
+                c = cache(n_layers=layers, batch=2048, max_pages=15, dtype=dtype, head_dim=dh)
+                n = lib.domino_paged_evict_workspace_bytes(c, 960, 100)
+                took[dtype, dh, layers, table] = check(lib.domino_paged_evict(c, F, F + 64, 960, 100, 0, 0, table, 1 << 10, None, F, n, None))
+assert took[0, 128, 60, None] and not took[0, 128, 61, None] and not took[0, 128, 64, None]
+assert all(v for k, v in took.items() if k[:2] != (0, 128) or k[3] or k[2] <= 60)
+''', tmp_path)
