@@ -665,7 +665,7 @@ template <typename T, int DH>
 static void append_of(const PagedAppendArgs &a, hipStream_t st) {
   constexpr int GROUPS = kAppendThreads / (DH / 8);
   const int heads = a.nq + 2 * a.c.n_kv;
-  const int ys = a.tokens < 1024 ? (heads + GROUPS - 1) / GROUPS : 1;
+  const int ys = a.tokens < 1024 ? min((heads + GROUPS - 1) / GROUPS, 16383) : 1;  // (a grid holds 1023 x 16383 workgroups of 256)
   hipLaunchKernelGGL((paged_append_kernel<T, DH>), dim3(a.tokens, ys), dim3(kAppendThreads), 0, st, a);
 }
 void launch_paged_append(const PagedAppendArgs &a, hipStream_t st) {

@@ -55,3 +55,16 @@ for dtype in (0, 1):
 assert took[0, 128, 60, None] and not took[0, 128, 61, None] and not took[0, 128, 64, None]
 assert all(v for k, v in took.items() if k[:2] != (0, 128) or k[3] or k[2] <= 60)
 ''', tmp_path)
+
+
+def test_an_append_of_many_heads_fits_a_grid(tmp_path):
+    host_stub.run(CACHE + '''
+h.log()
+for tokens in (1, 600, 1023):
+    for heads in (8, 1 << 19):
+        c = cache(n_kv_heads=heads, max_pages=1)
+        assert lib.domino_paged_append(c, 0, tokens, heads, F, heads * 128, F, heads * 128, F, heads * 128, F, heads * 128, F, F, None,
+                                       None, 0, 0, 1.0, None, None, 0.0, F, 16, None) == 0, bd.last_error()
+        (r,) = [r for r in h.log() if r[0] == "launch"]
+        assert int(r[2]) == tokens and int(r[3]) <= 65535 and tokens * int(r[3]) * int(r[5]) < 2**32, r
+''', tmp_path)
