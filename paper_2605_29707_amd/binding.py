@@ -24,7 +24,7 @@ DOMINO_F32, DOMINO_BF16 = 0, 1
 
 DEV_BAD_TOKEN, DEV_BAD_CTX_LEN, DEV_BAD_TREE, DEV_BARRIER_TIMEOUT, DEV_BAD_PARAM, DEV_BAD_PAGE = 1, 2, 4, 8, 16, 32
 
-DOMINO_ROPE_NONE, DOMINO_ROPE_LINEAR, DOMINO_ROPE_NTK, DOMINO_ROPE_YARN = 0, 1, 2, 3
+DOMINO_ROPE_NONE, DOMINO_ROPE_LINEAR, DOMINO_ROPE_NTK, DOMINO_ROPE_YARN, DOMINO_ROPE_YARN_INDEX = 0, 1, 2, 3, 4
 DOMINO_PAGED_WORKSPACE_BYTES = 16
 
 KERNEL_CLASSES = ["embed", "norm", "qkv", "rope", "attn", "wo", "gateup", "down", "lmhead", "w1h",
@@ -511,7 +511,8 @@ def _heads(cache: PagedCache, name, t, shape=None):
 
 def domino_rope_frequencies(rotary_dim, theta, scaling=DOMINO_ROPE_NONE, factor=1.0, original_ctx=0, beta_fast=32.0,
                             beta_slow=1.0):
-    """(fp64 numpy array [rotary_dim / 2], rope_scale)."""
+    """(fp64 numpy array [rotary_dim / 2], rope_scale).  A checkpoint's YaRN parameters are for DOMINO_ROPE_YARN_INDEX;
+    DOMINO_ROPE_YARN is the rule as its paper prints it."""
     f, scale = np.empty(max(int(rotary_dim), 0) // 2, dtype=np.float64), C.c_float(0)
     _check(load().domino_rope_frequencies(int(rotary_dim), float(theta), int(scaling), float(factor), int(original_ctx),
                                           float(beta_fast), float(beta_slow), f.ctypes.data, C.byref(scale)))

@@ -1554,21 +1554,27 @@ domino_status domino_rope_frequencies(int32_t rotary_dim, double theta, domino_r
   if (!frequencies || !rope_scale) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
   if (rotary_dim < 2 || rotary_dim > 128 || rotary_dim % 2) return fail(DOMINO_ERR_INVALID_ARG, "rotary_dim must be even, in [2, 128]");
   if (!(theta > 1.0) || !std::isfinite(theta)) return fail(DOMINO_ERR_INVALID_ARG, "theta must be above 1 and finite");
-  if (scaling < DOMINO_ROPE_NONE || scaling > DOMINO_ROPE_YARN) return fail(DOMINO_ERR_INVALID_ARG, "unknown scaling");
+  if (scaling < DOMINO_ROPE_NONE || scaling > DOMINO_ROPE_YARN_INDEX) return fail(DOMINO_ERR_INVALID_ARG, "unknown scaling");
   if (scaling != DOMINO_ROPE_NONE && (!(factor >= 1.0) || !std::isfinite(factor)))
     return fail(DOMINO_ERR_INVALID_ARG, "factor must be at least 1 and finite");
   if (scaling == DOMINO_ROPE_NTK && rotary_dim < 4) return fail(DOMINO_ERR_INVALID_ARG, "DOMINO_ROPE_NTK needs a rotary_dim of at least 4");
-  if (scaling == DOMINO_ROPE_YARN && (original_ctx < 1 || !(beta_slow > 0.0) || !(beta_fast > beta_slow) || !std::isfinite(beta_fast)))
-    return fail(DOMINO_ERR_INVALID_ARG, "DOMINO_ROPE_YARN needs original_ctx >= 1 and finite beta_fast > beta_slow > 0");
-  const double d = rotary_dim;
+  const bool yarn = scaling == DOMINO_ROPE_YARN || scaling == DOMINO_ROPE_YARN_INDEX;
+  if (yarn && (original_ctx < 1 || !(beta_slow > 0.0) || !(beta_fast > beta_slow) || !std::isfinite(beta_fast)))
+    return fail(DOMINO_ERR_INVALID_ARG, "YaRN needs original_ctx >= 1 and finite beta_fast > beta_slow > 0");
+  const double d = rotary_dim, turn = 6.283185307179586;
+  // the index of a pair that makes r turns in original_ctx positions
+  auto index_of = [&](double r) { return d * std::log(original_ctx / (turn * r)) / (2.0 * std::log(theta)); };
+  const double first = yarn ? std::max(std::floor(index_of(beta_fast)), 0.0) : 0.0;
+  const double last = yarn ? std::min(std::ceil(index_of(beta_slow)), d - 1.0) : 0.0;
   if (scaling == DOMINO_ROPE_NTK) theta *= std::pow(factor, d / (d - 2.0));
-  *rope_scale = scaling == DOMINO_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  *rope_scale = yarn ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
   for (int i = 0; i < rotary_dim / 2; ++i) {
     double f = std::pow(theta, -2.0 * i / d);
     if (scaling == DOMINO_ROPE_LINEAR) f /= factor;
-    if (scaling == DOMINO_ROPE_YARN) {
-      const double turns = original_ctx * f / 6.283185307179586;
-      const double keep = std::min(1.0, std::max(0.0, (turns - beta_slow) / (beta_fast - beta_slow)));
+    if (yarn) {
+      const double turns = original_ctx * f / turn;
+      double keep = std::min(1.0, std::max(0.0, (turns - beta_slow) / (beta_fast - beta_slow)));
+      if (scaling == DOMINO_ROPE_YARN_INDEX) keep = i <= first ? 1.0 : (i >= last ? 0.0 : (last - i) / (last - first));
       f = f * keep + f / factor * (1.0 - keep);
     }
     frequencies[i] = f;
