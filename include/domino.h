@@ -603,7 +603,8 @@ size_t domino_paged_attention_workspace_bytes(const domino_paged_cache *cache, i
  * Every row sees the slots before the new ones; of the new ones token i sees 0 .. i, or with
  * a mask those with mask[t][j] != 0 (t its packed row, j the other's place among the
  * sequence's new tokens; the diagonal counts for nothing by itself).  A row that sees no slot with a score above -inf
- * has output 0 and lse -inf.
+ * has output 0 and lse -inf.  What k and v hold in a slot that a row does not see counts for nothing in it; in one that it sees
+ * v counts with its weight, 0 among them: values that are not finite leave NaN or an infinity in their columns, NaN leaves NaN.
  *  max_new, max_len  at least every sequence's new tokens and slots; they choose the launch
  *  q, out          device [tokens][n_q_heads][head_dim], storage type, tokens *_stride apart, 16-byte rows; not the same memory.
  *                  n_q_heads a multiple of n_kv_heads

@@ -367,6 +367,7 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = sx[nt][e] * sc;
+      uint32_t dark = 0;  // hidden among this lane's eight (a score of -inf hides nothing: 0 times NaN is NaN in whole steps too)
       if (!whole) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -375,6 +376,7 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
           if (MASKED) seen = (slot < n0) | (mrow[nt][max(0, min(slot, t.s.len - 1) - n0)] != 0);
           seen &= slot < k1;
           x[e] = seen ? x[e] : -INFINITY;
+          dark |= seen ? 0u : 1u << e;
         }
       }
       // (64 sequences' next tokens: 500 us without, 540 with all of them stored to one place, 615 in earnest: the 82 MB of writes between the reads)
@@ -383,14 +385,9 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
         *(floatx4 *)to = floatx4{x[0], x[1], x[2], x[3]};
         *(floatx4 *)(to + 16) = floatx4{x[4], x[5], x[6], x[7]};
       }
-      uint32_t dark = 0;  // hidden among this lane's eight
       float top = x[0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-      if (odd) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dark |= x[e] == -INFINITY ? 1u << e : 0u;
-      }
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float mn = fmaxf(m[nt], top), ms = mn == -INFINITY ? 0.f : mn;
@@ -455,14 +452,15 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
     }
     const int tok = t.s.start + row / G, head = kvh * G + row % G;
     const int64_t at = ((int64_t)split * a.tokens + tok) * a.nq + head;
-    const float inv = a.part_o ? 1.f : (sum == 0.f ? 0.f : 1.f / sum);
+    const bool none = !a.part_o && sum == 0.f;  // no score above -inf: 0 whatever v holds
+    const float inv = a.part_o ? 1.f : 1.f / sum;
 #pragma unroll
     for (int cc = 0; cc < DH / 64; ++cc) {
       const int c = cc * 64 + c0 * 4;
       floatx4 y{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < kPaWaves; ++w) y += *(const floatx4 *)(om + (w * 16 + rr) * LD + c) * f[w];
-      y *= inv;
+      y = none ? floatx4{0.f, 0.f, 0.f, 0.f} : y * inv;
       if (a.part_o) {
         *(floatx4 *)(a.part_o + at * DH + c) = y;
       } else {
@@ -671,7 +669,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
         if (MASKED) seen = (slot < n0) | ((four[e / 4] >> (8 * (e % 4)) & 0xff) != 0);
         seen &= slot < k1;
         x[e] = seen ? x[e] : -INFINITY;
-        dark |= x[e] == -INFINITY ? 1u << e : 0u;
+        dark |= seen ? 0u : 1u << e;
       }
     }
     float top = x[0];
@@ -749,6 +747,12 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a, in
   const int qh = kvh * G + row % G;
   const int64_t at = ((int64_t)split * a.tokens + tok) * a.nq + qh;
   const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (!a.part_o && l == 0.f) {  // no score above -inf: 0 whatever v holds
+#pragma unroll
+    for (int y = 0; y < DT; ++y)
+#pragma unroll
+      for (int c = 0; c < 16; ++c) o[y][c] = 0.f;
+  }
 #pragma unroll
   for (int y = 0; y < DT; ++y)
 #pragma unroll
@@ -841,10 +845,10 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, i
       for (int e = 0; e < E; ++e) y[e] += s_y[w][lane * E + e] * f;
     }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = 1.f / sum;
   T *dst = (T *)a.out + (int64_t)tok * a.o_stride + (int64_t)head * DH + lane * E;
 #pragma unroll
-  for (int e = 0; e < E; ++e) store_as(dst + e, y[e] * inv);
+  for (int e = 0; e < E; ++e) store_as(dst + e, sum == 0.f ? 0.f : y[e] * inv);  // (no score above -inf: 0 whatever v holds)
   if (lane == 0 && a.lse) a.lse[at] = (top + log2f(sum)) * kLn2;
 }
 
