@@ -53,3 +53,48 @@ def test_a_score_of_minus_infinity_hides_nothing(dtype, masked, ctx, new):
     c.v.fill_(float("nan"))
     out, lse = attend(c, q, n, mask)
     assert (out == 0).all() and (lse == -INF).all()
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("new", [3, 40])           # the kernel of few rows; the chunks' (of fp32 two tiles of 16)
+@pytest.mark.parametrize("ctx", [13, 2500])        # one run; several
+@pytest.mark.parametrize("page", [1, 8, 32, 64])   # a page's lookup by slots, loads, halves of a step and steps
+def test_values_that_are_not_finite(dtype, dh, masked, new, ctx, page):
+    """Single values of new tokens: in the rows that see their slot NaN or the infinity stands in their column, every other number
+    is that of a call on finite values."""
+    n = ctx + new
+    c = Pages([n], page=page, nkv=2, dh=dh, dtype=dtype, seed=page, stale="")
+    q = tokens(new, 4, dh, dtype, 1)
+    sees = torch.tril(torch.ones(new, new, dtype=torch.bool))
+    mask = None
+    if masked:     # siblings: tokens that some earlier and some later rows do not see
+        sees = (torch.rand(new, new, generator=torch.Generator().manual_seed(new)) < 0.6) & sees | torch.eye(new, dtype=torch.bool)
+        sees[new - 1] = True
+        mask = sees.to(torch.uint8).to(DEV)
+    odd = [(new // 2, 3, float("nan")), (new // 2 + 1, dh // 2 + 1, INF), (new - 1, dh - 1, -INF), (0, 5, INF)]
+    want, want_lse = attend(c, q, n, mask)
+    want = want.clone()
+    for token, col, value in odd:
+        put(c, c.v[..., col], ctx + token, value)
+        want[sees[:, token].to(DEV), :, col] = value
+    out, lse = attend(c, q, n, mask)
+    assert torch.equal(lse, want_lse)
+    assert torch.equal(out.nan_to_num(123.0, 1e38, -1e38), want.nan_to_num(123.0, 1e38, -1e38))
+
+
+@pytest.mark.parametrize("dtype,dh,page", [("bf16", 64, 8), ("bf16", 128, 64), ("f32", 128, 32), ("f32", 64, 1)])
+@pytest.mark.parametrize("new", [1, 40])
+def test_values_of_the_context_that_are_not_finite(dtype, dh, page, new):
+    """Every row sees them, in steps without a mask: their columns hold no finite number, the others what they held."""
+    n = 700 + new
+    c = Pages([n], page=page, nkv=2, dh=dh, dtype=dtype, seed=page, stale="")
+    q = tokens(new, 4, dh, dtype, 1)
+    want, want_lse = attend(c, q, n)
+    for slot, col, value in ((5, 3, float("nan")), (300, 17, INF), (699, dh - 1, -INF)):
+        put(c, c.v[..., col], slot, value)
+    out, lse = attend(c, q, n)
+    cols = torch.zeros(dh, dtype=torch.bool, device=DEV)
+    cols[[3, 17, dh - 1]] = True
+    assert torch.equal(lse, want_lse) and torch.equal(out[..., ~cols], want[..., ~cols])
+    assert not torch.isfinite(out[..., cols]).any() and torch.isnan(out[..., 3]).all()
