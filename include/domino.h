@@ -648,7 +648,7 @@ domino_status domino_paged_evict(const domino_paged_cache *cache, const int32_t 
  * [d, n_nodes), else DOMINO_DEV_BAD_TREE; a sequence with that, lengths out of range or a bad page is left
  * unchanged (new_ctx_lens[b] = ctx_lens[b]).
  *  max_depth       the row stride of accepted_nodes, in [1, 63]; n_nodes in [1, 1024]
- *  ctx_lens        device int32 [batch]: slots before node 0's; new_ctx_lens device int32 [batch], not ctx_lens
+ *  ctx_lens        device int32 [batch]: slots before node 0's; new_ctx_lens device int32 [batch], apart from the arrays that are read
  */
 domino_status domino_paged_commit(const domino_paged_cache *cache, int32_t n_nodes, int32_t max_depth,
                                   const int32_t *ctx_lens, const int32_t *accept_len, const int32_t *accepted_nodes,

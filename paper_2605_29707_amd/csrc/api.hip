@@ -1735,7 +1735,8 @@ domino_status domino_paged_commit(const domino_paged_cache *cache, int32_t n_nod
   if (n_nodes < 1 || n_nodes > 1024) return fail(DOMINO_ERR_INVALID_ARG, "n_nodes must be in [1, 1024]");
   if (max_depth < 1 || max_depth > 63) return fail(DOMINO_ERR_INVALID_ARG, "max_depth must be in [1, 63]");
   if (!ctx_lens || !accept_len || !accepted_nodes || !new_ctx_lens) return fail(DOMINO_ERR_INVALID_ARG, "a required pointer is NULL");
-  if (ctx_lens == new_ctx_lens) return fail(DOMINO_ERR_INVALID_ARG, "new_ctx_lens must not alias ctx_lens");
+  if (new_ctx_lens == ctx_lens || new_ctx_lens == accept_len || new_ctx_lens == accepted_nodes)  // one workgroup writes what all read
+    return fail(DOMINO_ERR_INVALID_ARG, "new_ctx_lens must not alias ctx_lens, accept_len or accepted_nodes");
   if ((int64_t)cache->n_layers * cache->batch * cache->n_kv_heads > kMaxBlocks)
     return fail(DOMINO_ERR_UNSUPPORTED, "n_layers * batch * n_kv_heads must be at most %ld", kMaxBlocks);
   if (domino_status s = check_paged_workspace(workspace, workspace_bytes, DOMINO_PAGED_WORKSPACE_BYTES); s != DOMINO_OK) return s;

@@ -68,3 +68,12 @@ for tokens in (1, 600, 1023):
         (r,) = [r for r in h.log() if r[0] == "launch"]
         assert int(r[2]) == tokens and int(r[3]) <= 65535 and tokens * int(r[3]) * int(r[5]) < 2**32, r
 ''', tmp_path)
+
+
+def test_commit_writes_no_array_that_it_reads(tmp_path):
+    host_stub.run(CACHE + '''
+for ctx, acc, path, new in ((1, 2, 3, 1), (1, 2, 3, 2), (1, 2, 3, 3), (1, 2, 3, 4)):
+    h.log()
+    st = lib.domino_paged_commit(cache(), 61, 15, F * ctx, F * acc, F * path, F * new, F, 16, None)
+    assert (st, len(h.log())) == ((0, 1) if new == 4 else (-1, 0)), (new, st)
+''', tmp_path)
