@@ -49,9 +49,15 @@ template <typename T, int DH>
 __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedAppendArgs a) {
   constexpr int LPH = DH / 8, GROUPS = kAppendThreads / LPH;
   const int t = blockIdx.x, j = threadIdx.x % LPH, grp = threadIdx.x / LPH;
+  const int room = a.c.max_pages << a.c.page_shift;
+  if (t == a.tokens) {  // one workgroup more than there are rows looks at all sequences, also those that have no row
+    SeqRange all;
+    for (int i = threadIdx.x; i < a.c.batch; i += kAppendThreads) seq_range(a.starts, a.lens, i, a.tokens, a.tokens, room, a.err, all);
+    return;
+  }
   int b;
   SeqRange s;
-  if (!seq_of_token(a.starts, a.lens, a.c.batch, t, a.tokens, a.tokens, a.c.max_pages << a.c.page_shift, a.err, b, s)) return;
+  if (!seq_of_token(a.starts, a.lens, a.c.batch, t, a.tokens, a.tokens, room, b, s)) return;
   const int slot = s.len - s.n + (t - s.start);
   const int page = page_of(a.c, b, slot);
   if (page < 0) raise_error(a.err, DEV_BAD_PAGE);
@@ -665,8 +671,8 @@ template <typename T, int DH>
 static void append_of(const PagedAppendArgs &a, hipStream_t st) {
   constexpr int GROUPS = kAppendThreads / (DH / 8);
   const int heads = a.nq + 2 * a.c.n_kv;
-  const int ys = a.tokens < 1024 ? min((heads + GROUPS - 1) / GROUPS, 16383) : 1;  // (a grid holds 1023 x 16383 workgroups of 256)
-  hipLaunchKernelGGL((paged_append_kernel<T, DH>), dim3(a.tokens, ys), dim3(kAppendThreads), 0, st, a);
+  const int ys = a.tokens < 1024 ? min((heads + GROUPS - 1) / GROUPS, 16383) : 1;  // (a grid holds 1024 x 16383 workgroups of 256)
+  hipLaunchKernelGGL((paged_append_kernel<T, DH>), dim3(a.tokens + 1, ys), dim3(kAppendThreads), 0, st, a);
 }
 void launch_paged_append(const PagedAppendArgs &a, hipStream_t st) {
   if (a.c.bf16) a.c.dh == 128 ? append_of<bf16_t, 128>(a, st) : append_of<bf16_t, 64>(a, st);

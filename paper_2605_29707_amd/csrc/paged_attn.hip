@@ -783,7 +783,7 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, i
   const int tok = (int)(at / a.nq), head = (int)(at % a.nq), G = a.nq / a.c.n_kv;
   int b;
   SeqRange s;
-  if (!seq_of_token(a.starts, a.lens, a.c.batch, tok, a.tokens, a.max_new, a.max_len, nullptr, b, s)) return;
+  if (!seq_of_token(a.starts, a.lens, a.c.batch, tok, a.tokens, a.max_new, a.max_len, b, s)) return;
   run = run_of(a, s.len, run, M == kChunkRows ? kChunkStep : kPaWaves * kPaStep);
   const int row = (tok - s.start) * G + head % G, last = (min((row / M + 1) * M, s.n * G) - 1) / G;
   const int vis = a.mask ? s.len : s.len - s.n + last + 1, runs = (vis + run - 1) / run;
@@ -962,9 +962,8 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_weights_kernel(PagedAttnAr
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, r = lane & 31;
   const int kvh = blockIdx.x % a.c.n_kv, part = blockIdx.x / a.c.n_kv % parts, rest = blockIdx.x / a.c.n_kv / parts;
   const int b = rest / slabs, slab = rest % slabs * kWeightSlots;
-  const bool ascend = starts_ascend(a.starts, b);
   SeqRange s;
-  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || !ascend || slab >= s.len) return;
+  if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || slab >= s.len || !starts_ascend(a.starts, b)) return;
   s.start = __builtin_amdgcn_readfirstlane(s.start);
   s.n = __builtin_amdgcn_readfirstlane(s.n);
   s.len = __builtin_amdgcn_readfirstlane(s.len);
