@@ -381,7 +381,8 @@ struct PagedEvictArgs {
 constexpr int kEvictSlice = 16384;  // slots of a head that one workgroup chooses from
 constexpr int kEvictMoveRows = 64;  // rows of a head that a workgroup moves to new pages
 // Workgroups of a head whose rows move in place: column slices of k, of v, and its weights.  Narrow slices, whose rounds have more rows, where
-// there are few workgroups: 9000 bf16 slots of 8 heads to 8000 50 us (64 with wide slices), of 32 heads 77 (72 wide).
+// there are few workgroups.  Calls of 9000 slots to 8000, bf16 heads of 128: 8 heads 56 us (69 with wide slices), 16 60 (71), 32 118 (116 wide),
+// 64 192 (163); fp32 crosses between 8 and 16 heads (63 and 78, 119 and 116), heads of 64 bf16 values between 32 and 64.
 inline int evict_in_place_parts(int dh, bool bf16, int heads) {
   const int wide = dh * (bf16 ? 2 : 4) / 64;  // slices of four 16-byte items
   return heads * wide < 128 ? 4 * wide + 1 : 2 * wide + 1;

@@ -11,7 +11,7 @@ namespace dk {
 // halves, the eight that they are paired with, so nothing passes between lanes but a head's sum of squares.
 // Per pair (x, y) at angle a = position * frequency: (x cos a - y sin a, y cos a + x sin a).  The angle is a number of
 // turns in fp64, taken modulo one before it is rounded: positions in the millions keep fp32's accuracy.
-// Bound by the rows' bytes, each read and written once: 9384 tokens of 32 + 2 x 8 heads of 128 bf16 values 58 us, 4.0 TB/s; one token 4.8.
+// Bound by the rows' bytes, each read and written once: 9384 tokens of 32 + 2 x 8 heads of 128 bf16 values 56 us, 4.1 TB/s; one token 4.9.
 constexpr int kAppendThreads = 256;
 
 template <typename T>
@@ -238,7 +238,7 @@ DEVI uint32_t weight_key(float w) {
 // between them.  A workgroup has a slice of 16384 slots, a wave 1024 of them, whose keys it keeps in registers (16 a lane).  The m-th
 // greatest key is found by three counts over its digits (11, 11 and 10 bits): kept are the keys above it and the first `need` that
 // equal it.  Then every wave counts the kept slots of its stretch, and writes them behind those of the waves before it.
-//   one slice    one launch: bound by the chain of its steps (1100 slots 8 us, 384 heads of up to 16384 36)
+//   one slice    one launch: bound by the chain of its steps (1100 slots 8.7 us, 384 heads of up to 16384 36)
 //   more slices  a launch for each count and one that writes; a slice's counts are its own, and the next launch adds them up.
 //                (100003 slots of 16 heads in one workgroup each took 125 us: bound by its instructions)
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;

@@ -16,7 +16,7 @@ typedef __attribute__((ext_vector_type(4))) short short4v;
 
 DEVI float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// One 16-row tile's place: sequence, lengths, first row, what it sees.
+// A tile's place (16, 32 or 128 rows, as planned): sequence, lengths, first row, what it sees.
 struct Tile {
   int b, row0, rows, vis;  // rows: of the sequence; vis: no row of the tile sees a slot from here on
   SeqRange s;
@@ -68,7 +68,8 @@ DEVI int run_of(const PagedAttnArgs &a, int len, int run, int whole) {
 }
 
 // The run of the at-th workgroup of a kv head.  Tiles' first runs, the ones that short sequences have, are an odd number of workgroups
-// apart: workgroups are handed to the CUs in turn, and 64 sequences of 2000 slots in a launch for 32768, 16 apart, took 249 us (106 by themselves).
+// apart: workgroups are handed to the CUs in turn, and 64 sequences of 2000 slots in a launch for 32768, 16 apart, took 249 us (130 so,
+// 97 in a launch for 2000).
 DEVI int split_of(int at, int tile, int splits) { return (splits & 1 ? at : at + tile) % splits; }
 
 // Operands of the two products.  Scores: S^T = K Q^T in tiles of 16 slots x 16 rows, lane (g, r) = 16 g + r with
@@ -379,7 +380,8 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_kernel(PagedAttnArgs a,
           dark |= seen ? 0u : 1u << e;
         }
       }
-      // (64 sequences' next tokens: 500 us without, 540 with all of them stored to one place, 615 in earnest: the 82 MB of writes between the reads)
+      // (Whole calls, 64 sequences' next tokens with their weights: 536 us without these stores, 540 with all of them to one place, 615 in earnest:
+      // the 82 MB of writes between the reads.)
       if (NT == 1 && a.scores && t.row0 + r < t.rows) {
         float *to = scores_at(a, t.b, kvh, kt, r) + 4 * g;
         *(floatx4 *)to = floatx4{x[0], x[1], x[2], x[3]};
@@ -885,12 +887,12 @@ __global__ __launch_bounds__(256) void paged_weights_of_scores_kernel(PagedAttnA
   }
 }
 
-// weights[slot] += the sum over the call's rows of p: a wave has 32 slots of one kv head and goes over every row that may
-// see them, in order (so the sum is the same every time).
-template <typename T, int DH, bool MASKED>
+// weights[slot] += the sum over the call's rows of p, for fp32: a wave has 32 slots of one kv head and goes over every row that may
+// see them, in order (so the sum is the same every time).  Bound by the products of few waves: 1024 tokens after 4096, 32 heads on 8, 625 us,
+// 62 TFLOP/s, with 1280 waves on 1024 SIMDs.
+template <int DH, bool MASKED>
 __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs a, int slabs) {
-  using O = Ops<T, DH>;
-  constexpr int ESZ = sizeof(T);
+  using O = Ops<float, DH>;
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
   const int kvh = blockIdx.x % a.c.n_kv, b = blockIdx.x / a.c.n_kv / slabs;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -900,12 +902,12 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
   if (!seq_range(a.starts, a.lens, b, a.tokens, a.max_new, a.max_len, nullptr, s) || !ascend || kt >= s.len) return;
   const int G = a.nq / a.c.n_kv, n0 = s.len - s.n, rows = s.n * G;
   const int page = page_of(a.c, b, min(kt + (lane & 31), s.len - 1));
-  const char *kb = a.c.k + (a.layer * a.c.layer_stride + kvh * a.c.head_stride) * ESZ;
+  const char *kb = a.c.k + (a.layer * a.c.layer_stride + kvh * a.c.head_stride) * 4;
   u32x4 k[2][O::KST];
 #pragma unroll
   for (int tt = 0; tt < 2; ++tt) {
     const int x = 16 * tt + r;
-    const char *p = kb + slot_offset(a.c, max(__shfl(page, x, 64), 0), min(kt + x, s.len - 1)) * ESZ;
+    const char *p = kb + slot_offset(a.c, max(__shfl(page, x, 64), 0), min(kt + x, s.len - 1)) * 4;
 #pragma unroll
     for (int st = 0; st < O::KST; ++st) k[tt][st] = O::row_frag(p, st, g);
   }
@@ -916,14 +918,14 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
   for (int row0 = first; row0 < rows; row0 += 16) {
     const int row = min(row0 + r, rows - 1), i = row / G, head = kvh * G + row % G;
     const int64_t tok = s.start + i;
-    const char *p = (const char *)a.q + (tok * a.q_stride + (int64_t)head * DH) * ESZ;
+    const char *p = (const char *)a.q + (tok * a.q_stride + (int64_t)head * DH) * 4;
     u32x4 q[O::KST];
 #pragma unroll
     for (int st = 0; st < O::KST; ++st) q[st] = O::row_frag(p, st, g);
     const float ls = a.lse[tok * a.nq + head] * kLog2e;
     const bool live = row0 + r < rows && ls != -INFINITY;
     float x[8];
-    score8<T, DH>(k, q, x);
+    score8<float, DH>(k, q, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int slot = kt + 16 * (e / 4) + 4 * g + e % 4;
@@ -950,7 +952,7 @@ __global__ __launch_bounds__(kPaThreads) void paged_weights_kernel(PagedAttnArgs
 // The same for bf16: a workgroup has 256 slots, 64 a wave, whose rows of k stay in registers; the call's rows pass through two LDS
 // buffers 32 at a time (with their lse and the last slot that they see), in order.  Where the slots make few workgroups, `parts` of them
 // share a slab's rows, every parts-th 32, and leave their sums to the next kernel.  Bound by the products and their exponentials: 4096 tokens
-// after 12288 take 1814 us in all, 1000 without the weights.
+// after 12288 take 1664 to 1814 us in all by the card, 983 to 1069 without the weights (this kernel 682: 0.71 PFLOP/s).
 constexpr int kWeightSlots = 256;
 
 template <int DH, bool MASKED>
@@ -1172,7 +1174,7 @@ static void attn_of(const PagedAttnArgs &a, const PagedAttnPlan &p, hipStream_t 
     if constexpr (sizeof(T) == 2) {
       hipLaunchKernelGGL((paged_chunk_weights_kernel<DH, MASKED>), cut, block, 0, st, a, slabs, p.parts);
       if (p.parts > 1) hipLaunchKernelGGL(paged_weights_join_kernel, all, dim3(kWeightSlots), 0, st, a, slabs, p.parts);
-    } else hipLaunchKernelGGL((paged_weights_kernel<T, DH, MASKED>), all, block, 0, st, a, slabs);
+    } else hipLaunchKernelGGL((paged_weights_kernel<DH, MASKED>), all, block, 0, st, a, slabs);
   }
 }
 template <typename T, int DH>
